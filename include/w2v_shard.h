@@ -322,6 +322,32 @@ int w2v_topk_cosine(const float* queries_dev, uint32_t Q, const float* cands_dev
                     uint32_t* out_count_dev, void* workspace_dev, size_t workspace_bytes,
                     void* stream);
 
+/* ---- layer norm of rows, and its gradients ---------------------------------------------------------
+ * For vectors read in their context: y = (x - mean) rstd gain + offset for each of `rows` rows of d
+ * elements, rstd = (mean((x - mean)^2) + eps)^-1/2.  Rows are of `type` (W2V_T_*) and start every
+ * x_stride / y_stride elements (outputs: at least d); gain_dev and offset_dev are fp32 [d] (NULL: 1 and
+ * 0).  mean_dev and rstd_dev receive the rows' statistics, fp32 [rows] (NULL: not wanted).  y may be x.
+ * All sums are fp32, in an order fixed by the shape; results repeat bit for bit.
+ *
+ * The backward call takes the statistics that the forward call left, and the gradient dy of the result:
+ * dx (may be dy or x), and, summed over the rows in fp32, dgain_dev and doffset_dev [d] (either may
+ * be NULL).  workspace_dev: 256-byte aligned device memory of w2v_layer_norm_backward_workspace(type, rows, d)
+ * bytes, contents irrelevant before and after.  Neither call allocates or synchronises.
+ * 1 <= d <= W2V_NORM_D_MAX; rows < 2^40 (no rows: nothing is done, but the column gradients are zero). */
+#define W2V_T_F32  0
+#define W2V_T_F16  1
+#define W2V_T_BF16 2
+#define W2V_NORM_D_MAX 16384
+int w2v_layer_norm(int type, const void* x_dev, uint64_t x_stride, uint64_t rows, uint32_t d,
+                   const float* gain_dev, const float* offset_dev, float eps, void* y_dev,
+                   uint64_t y_stride, float* mean_dev, float* rstd_dev, void* stream);
+size_t w2v_layer_norm_backward_workspace(int type, uint64_t rows, uint32_t d);
+int w2v_layer_norm_backward(int type, const void* dy_dev, uint64_t dy_stride, const void* x_dev,
+                            uint64_t x_stride, uint64_t rows, uint32_t d, const float* gain_dev,
+                            const float* mean_dev, const float* rstd_dev, void* dx_dev,
+                            uint64_t dx_stride, float* dgain_dev, float* doffset_dev,
+                            void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* Seed of minibatch number h (the client picks a fresh seed per minibatch), a function of a master seed. */
 uint64_t w2v_minibatch_seed(uint64_t master_seed, uint64_t h);
 

@@ -50,7 +50,7 @@ static_assert(W2V_S_MAX <= ROW_PARTS_MAX, "an export moves all shards in one lau
 // ---------------------------------------------------------------------------------------------
 static thread_local std::string g_last_error;
 
-static int fail(int code, const char* fmt, ...) {
+int w2v::fail(int code, const char* fmt, ...) {
     char buf[512];
     va_list ap;
     va_start(ap, fmt);

@@ -5,6 +5,9 @@
 
 namespace w2v {
 
+// Keeps the text of the calling thread's last failure (w2v_last_error) and returns `code`.
+int fail(int code, const char* fmt, ...);
+
 // ---- counter-based generator (Philox4x32, 10 rounds; Salmon et al., SC'11) -----------------------
 // The fourth counter word separates the uses of the generator.
 enum : uint32_t { DOM_INIT = 1, DOM_TOKEN = 2, DOM_NEG = 4, DOM_MBSEED = 5 };

@@ -16,6 +16,7 @@ _lib = None
 
 PHASES = ["neg", "dot", "coeff", "sort", "uside", "wside", "apply", "pairs"]
 K_MAX, D_MAX, S_MAX = 64, 1024, 32
+NORM_D_MAX = 16384
 NOALLOC_SCRATCH_U32 = 1 << 21
 
 c_u32, c_u64, c_vp = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_void_p
@@ -62,6 +63,12 @@ _SIGNATURES = {
     "w2v_topk_cosine_workspace": (ctypes.c_size_t, [c_u32, c_u32, c_u32]),
     "w2v_topk_cosine": (ctypes.c_int, [c_vp, c_u32, c_vp, c_u32, c_u32, c_u32, ctypes.c_float, c_vp,
                                        c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
+    "w2v_layer_norm": (ctypes.c_int, [ctypes.c_int, c_vp, c_u64, c_u64, c_u32, c_vp, c_vp, ctypes.c_float,
+                                      c_vp, c_u64, c_vp, c_vp, c_vp]),
+    "w2v_layer_norm_backward_workspace": (ctypes.c_size_t, [ctypes.c_int, c_u64, c_u32]),
+    "w2v_layer_norm_backward": (ctypes.c_int, [ctypes.c_int, c_vp, c_u64, c_vp, c_u64, c_u64, c_u32, c_vp,
+                                               c_vp, c_vp, c_vp, c_u64, c_vp, c_vp, c_vp, ctypes.c_size_t,
+                                               c_vp]),
     "w2v_minibatch_seed": (c_u64, [c_u64, c_u64]),
     "w2v_shard_timing_enable": (ctypes.c_int, [c_vp, ctypes.c_int]),
     "w2v_shard_timing_read": (ctypes.c_int, [c_vp, c_vp, c_vp]),
@@ -386,3 +393,66 @@ def topk_cosine(queries, cands, K, tau=-2.0, round_candidates=32768, workspace=N
                                  _dev(count, IDX, "out_count"), c_vp(workspace.data_ptr()),
                                  workspace.numel(), _stream(stream)))
     return idx, score, count
+
+
+# -- vectors in context ------------------------------------------------------------------------------
+TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _on(stream, t):
+    """What is allocated for a call belongs to the stream the call runs on, and to the tensor's device."""
+    return torch.cuda.stream(torch.cuda.current_stream(t.device) if stream is None else stream)
+
+
+def _rows(t, like, name):
+    """A matrix of rows that lie anywhere, their elements side by side: (pointer, elements from row to row)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in TYPES and t.dim() == 2 and
+            (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= 0)):
+        raise TypeError("%s must be a CUDA matrix of float32, float16 or bfloat16 with dense rows" % name)
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError("%s differs in shape, type or device" % name)
+    return t.data_ptr(), max(t.stride(0), 0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vec(t, n, device, name):
+    if t is None:
+        return None
+    if t.shape != (n,) or t.device != device:
+        raise ValueError("%s must have %d entries on %s" % (name, n, device))
+    return _dev(t, torch.float32, name)
+
+
+def layer_norm(x, gain=None, offset=None, eps=1e-5, out=None, stream=None):
+    """(y, mean, rstd) of w2v_layer_norm for the rows of x [m, d]; gain and offset are float32 [d]."""
+    xp, xs = _rows(x, None, "x")
+    m, d = x.shape
+    with _on(stream, x) as _:
+        st = torch.cuda.current_stream(x.device)
+        y = torch.empty((m, d), dtype=x.dtype, device=x.device) if out is None else out
+        stats = torch.empty((2, m), dtype=torch.float32, device=x.device)
+        yp, ys = _rows(y, x, "out")
+        _check(lib().w2v_layer_norm(TYPES[x.dtype], xp, xs, m, d, _vec(gain, d, x.device, "gain"),
+                                    _vec(offset, d, x.device, "offset"), float(eps), yp, ys, stats.data_ptr(),
+                                    stats.data_ptr() + 4 * m, st.cuda_stream))
+    return y, stats[0], stats[1]
+
+
+def layer_norm_backward(dy, x, gain, mean, rstd, out=None, workspace=None, stream=None):
+    """(dx, dgain, doffset) of w2v_layer_norm_backward; gain may be None.  ``workspace``: optional uint8
+    device tensor to reuse."""
+    xp, xs = _rows(x, None, "x")
+    gp, gs = _rows(dy, x, "dy")
+    m, d = x.shape
+    with _on(stream, x) as _:
+        st = torch.cuda.current_stream(x.device)
+        dx = torch.empty((m, d), dtype=x.dtype, device=x.device) if out is None else out
+        columns = torch.empty((2, d), dtype=torch.float32, device=x.device)
+        if workspace is None:
+            workspace = torch.empty(int(lib().w2v_layer_norm_backward_workspace(TYPES[x.dtype], m, d)),
+                                    dtype=torch.uint8, device=x.device)
+        op, os_ = _rows(dx, x, "out")
+        _check(lib().w2v_layer_norm_backward(TYPES[x.dtype], gp, gs, xp, xs, m, d, _vec(gain, d, x.device, "gain"),
+                                             _vec(mean, m, x.device, "mean"), _vec(rstd, m, x.device, "rstd"), op,
+                                             os_, columns.data_ptr(), columns.data_ptr() + 4 * d,
+                                             workspace.data_ptr(), workspace.numel(), st.cuda_stream))
+    return dx, columns[0], columns[1]
