@@ -348,6 +348,65 @@ int w2v_layer_norm_backward(int type, const void* dy_dev, uint64_t dy_stride, co
                             uint64_t dx_stride, float* dgain_dev, float* doffset_dev,
                             void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/* ---- attention over texts: vectors of words in their context ------------------------------------------
+ * The bag-of-words hidden vector is the plain mean over a window.  Here each word weighs what its window
+ * shows it: with per-head rows q_i, k_j, v_j of `width` elements,
+ *     x_ij = scale q_i . k_j + bias[head][bucket(j - i)],   out_i = sum_j softmax_j(x_ij) v_j,
+ *     lse_i = log sum_j exp(x_ij)
+ * over the words j of the same text that word i is shown: i - left <= j <= i + right, or j one of the text's first
+ * `sinks` words and j <= i + right; not those whose keep_dev byte is 0 (words that subsampling dropped: they
+ * see, but are not seen), and not i itself if skip_self.  W2V_UNBOUNDED: no limit on that side (right = 0:
+ * causal).  A word that is shown nothing has out = 0 and lse = -infinity, and no part in any gradient.
+ * What lies in rows that are not shown to a word, infinities and NaN included, has no influence on it.
+ *
+ * tokens 0..n_tokens of texts sent_off_dev[n_sent + 1] as for w2v_make_pairs (offsets that break its rules are made
+ * harmless: no access leaves the tokens, the results then mean nothing).  Query heads h share the key head
+ * h / (heads / kv_heads).  Element c of head h of token i of a w2v_heads lies at p[i token_stride + h head_stride + c], p of
+ * `type` (W2V_T_*); outputs must not overlap themselves or inputs.  lse is fp32 [heads][n_tokens].
+ *
+ * bias_dev (NULL: none) is fp32 [heads][n_buckets]; bucket_dev[2 span + 1] gives the bucket of every distance
+ * j - i = -span..span, distances beyond take the outermost; a bucket >= n_buckets adds nothing.
+ * w2v_relative_buckets fills such a map (host memory): half of the buckets for words before (and the word itself),
+ * half for words after; in each, the first half for distances one by one, the rest by their logarithm up
+ * to span.
+ *
+ * Scores, softmax and sums are fp32; weights are rounded to `type` for the product with v.  No call allocates or
+ * synchronises; results repeat bit for bit.  Limits: 1 <= width <= W2V_HEAD_MAX, heads a multiple of kv_heads and at most
+ * 1024, sinks <= W2V_SINKS_MAX, 1 <= span <= W2V_SPAN_MAX, 1 <= n_buckets <= W2V_BUCKETS_MAX, scale finite and > 0,
+ * n_tokens heads < 2^38, n_tokens <= 2^31 - 2^12. */
+#define W2V_HEAD_MAX 128
+#define W2V_SINKS_MAX 64
+#define W2V_SPAN_MAX 1023
+#define W2V_BUCKETS_MAX 1024
+#define W2V_UNBOUNDED 0xFFFFFFFFu
+typedef struct w2v_heads { void* p; uint64_t token_stride, head_stride; } w2v_heads;
+typedef struct w2v_attend_spec {
+    int32_t type;
+    uint32_t heads, kv_heads, width;
+    uint32_t left, right, sinks, skip_self;
+    float scale;
+    uint32_t n_buckets, span;            /* read where bias_dev is not NULL */
+    const float* bias_dev;
+    const uint32_t* bucket_dev;
+} w2v_attend_spec;
+int w2v_relative_buckets(uint32_t n_buckets, uint32_t span, uint32_t* map_host);
+int w2v_attend(const w2v_attend_spec* spec, const w2v_heads* q, const w2v_heads* k, const w2v_heads* v,
+               const uint64_t* sent_off_dev, uint32_t n_sent, uint32_t n_tokens, const uint8_t* keep_dev,
+               const w2v_heads* out, float* lse_dev /* may be NULL */, void* stream);
+
+/* Its gradients, from out and lse as the forward call left them and the gradient dout of the outputs:
+ *     dx_ij = p_ij (dout_i . v_j - dout_i . out_i),  dq_i = scale sum_j dx_ij k_j,  dk_j = scale sum dx_ij q_i,
+ *     dv_j = sum p_ij dout_i,  dbias[head][b] = sum of dx_ij over the pairs whose distance has bucket b,
+ * dk and dv summed over the query heads that share them.  dbias_dev (NULL: not wanted) is fp32 [heads][n_buckets].
+ * workspace_dev: 256-byte aligned device memory of w2v_attend_backward_workspace bytes, contents irrelevant
+ * before and after. */
+size_t w2v_attend_backward_workspace(const w2v_attend_spec* spec, uint32_t n_tokens);
+int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads* dout, const w2v_heads* q,
+                        const w2v_heads* k, const w2v_heads* v, const w2v_heads* out, const float* lse_dev,
+                        const uint64_t* sent_off_dev, uint32_t n_sent, uint32_t n_tokens,
+                        const uint8_t* keep_dev, const w2v_heads* dq, const w2v_heads* dk, const w2v_heads* dv,
+                        float* dbias_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* Seed of minibatch number h (the client picks a fresh seed per minibatch), a function of a master seed. */
 uint64_t w2v_minibatch_seed(uint64_t master_seed, uint64_t h);
 

@@ -23,4 +23,33 @@ struct NormBackwardArgs {
 uint32_t norm_backward_parts(uint64_t rows, uint32_t d, uint32_t type);
 void launch_norm_backward(const NormBackwardArgs& a, uint32_t type, float* dgain, float* doffset, hipStream_t st);
 
+// ---- attention over texts --------------------------------------------------------------------------
+constexpr uint32_t HEAD_MAX = 128, SINKS_MAX = 64, SPAN_MAX = 1023;
+
+// Rows of heads: element c of head h of token i at p[i token + h head + c].
+struct Heads { const void* p; uint64_t token, head; };
+struct HeadsOut { void* p; uint64_t token, head; };
+
+struct AttendArgs {
+    Heads q, k, v;
+    const uint64_t* off; uint32_t n_sent, T;             // texts, tokens
+    uint32_t heads, kv_heads, group, width;              // group = heads / kv_heads
+    uint32_t left, right, sinks; bool skip_self;         // left, right <= T; no sinks where nothing falls out of the window
+    float scale, scale2;                                 // scale2 = scale log2 e
+    const uint8_t* keep;                                 // or null
+    const float* bias; const uint32_t* buckets; uint32_t n_buckets, span;      // bias may be null
+    HeadsOut o; float* lse;                              // lse [heads][T], may be null in the forward pass
+};
+void launch_attend(const AttendArgs& a, uint32_t type, hipStream_t st);
+
+struct BackwardArgs {
+    AttendArgs a;                                        // a.o and a.lse as the forward pass left them
+    Heads dout;
+    HeadsOut dq, dk, dv; float* dbias;                   // dbias [heads][n_buckets], may be null
+    float* delta;                                        // workspace: [heads][T] sums of dout o
+    float* by_distance;                                  // workspace: [heads][bias_parts][2 span + 1]
+};
+uint32_t attend_bias_parts(uint32_t T);
+void launch_attend_backward(const BackwardArgs& b, uint32_t type, hipStream_t st);
+
 }  // namespace w2v

@@ -3,12 +3,14 @@
 #include "../../include/w2v_shard.h"
 
 #include <cmath>
+#include <cstring>
 
 #include "common.h"
 #include "context.h"
 #include "elem.h"
 
 using namespace w2v;
+static_assert(W2V_HEAD_MAX == HEAD_MAX && W2V_SINKS_MAX == SINKS_MAX && W2V_SPAN_MAX == SPAN_MAX, "limits");
 static_assert(W2V_T_F32 == ELEM_F32 && W2V_T_F16 == ELEM_F16 && W2V_T_BF16 == ELEM_BF16, "element types");
 
 namespace {
@@ -87,5 +89,173 @@ extern "C" int w2v_layer_norm_backward(int type, const void* dy, uint64_t dy_str
     launch_norm_backward(NormBackwardArgs{dy, dy_stride, x, x_stride, rows, d, gain, mean, rstd, dx, dx_stride,
                                           columns ? (float*)workspace : nullptr},
                          (uint32_t)type, dgain, doffset, (hipStream_t)stream);
+    return launched();
+}
+
+// ---------------------------------------------------------------------------------------------
+// attention over texts
+// ---------------------------------------------------------------------------------------------
+namespace {
+
+int check_spec(const w2v_attend_spec* s) {
+    if (!s) return fail(W2V_ERR_NULL, "spec is NULL");
+    if (int rc = check_type(s->type)) return rc;
+    if (s->width == 0 || s->width > W2V_HEAD_MAX) return fail(W2V_ERR_ARG, "width = %u outside 1..%d", s->width, W2V_HEAD_MAX);
+    if (s->heads == 0 || s->kv_heads == 0 || s->heads > 1024 || s->heads % s->kv_heads)
+        return fail(W2V_ERR_ARG, "%u heads do not share %u", s->heads, s->kv_heads);
+    if (s->sinks > W2V_SINKS_MAX) return fail(W2V_ERR_ARG, "sinks = %u above %d", s->sinks, W2V_SINKS_MAX);
+    if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return fail(W2V_ERR_ARG, "scale must be finite and positive");
+    if (s->bias_dev) {
+        if (!s->bucket_dev) return fail(W2V_ERR_NULL, "bucket_dev is NULL");
+        if (s->span == 0 || s->span > W2V_SPAN_MAX) return fail(W2V_ERR_ARG, "span = %u outside 1..%d", s->span, W2V_SPAN_MAX);
+        if (s->n_buckets == 0 || s->n_buckets > W2V_BUCKETS_MAX)
+            return fail(W2V_ERR_ARG, "n_buckets = %u outside 1..%d", s->n_buckets, W2V_BUCKETS_MAX);
+    }
+    return W2V_OK;
+}
+
+int check_tokens(const w2v_attend_spec* s, const uint64_t* off, uint32_t n_sent, uint32_t n_tokens) {
+    if (n_tokens > 0x7FFFFFFFu - 4095u || (uint64_t)n_tokens * s->heads >= 1ull << 38)
+        return fail(W2V_ERR_ARG, "too many tokens; pass the texts in blocks");
+    if (n_tokens && n_sent == 0) return fail(W2V_ERR_ARG, "tokens without texts");
+    if (n_sent > 0x7FFFFFFFu) return fail(W2V_ERR_ARG, "too many texts");
+    if (n_tokens && !off) return fail(W2V_ERR_NULL, "sent_off_dev is NULL");
+    return W2V_OK;
+}
+
+int check_heads(const w2v_heads* x, const w2v_attend_spec* s, uint32_t heads, uint32_t rows, bool output, const char* name) {
+    if (!x || !x->p) return fail(W2V_ERR_NULL, "%s is NULL", name);
+    if (!aligned(x->p, elem_bytes(s->type))) return fail(W2V_ERR_ARG, "%s is not aligned to its elements", name);
+    if (x->token_stride >= STRIDE_MAX || x->head_stride >= STRIDE_MAX ||
+        (rows > 1 && x->token_stride > (1ull << 60) / rows))
+        return fail(W2V_ERR_ARG, "%s reaches too far", name);
+    if (!output) return W2V_OK;
+    // rows of one head, heads of one row: the nearer ones must not touch, nor the farther ones what lies between
+    const uint64_t by_row = rows > 1 ? x->token_stride : ~0ull, by_head = heads > 1 ? x->head_stride : ~0ull;
+    const uint64_t near = by_row < by_head ? by_row : by_head, far = by_row < by_head ? by_head : by_row;
+    const uint64_t count = by_row < by_head ? rows : heads;
+    if (near < s->width || (far != ~0ull && far < near * (count - 1) + s->width))
+        return fail(W2V_ERR_ARG, "rows of %s overlap", name);
+    return W2V_OK;
+}
+
+Heads heads_of(const w2v_heads* x) { return Heads{x->p, x->token_stride, x->head_stride}; }
+HeadsOut heads_out(const w2v_heads* x) { return HeadsOut{x->p, x->token_stride, x->head_stride}; }
+
+AttendArgs attend_args(const w2v_attend_spec* s, const w2v_heads* q, const w2v_heads* k, const w2v_heads* v,
+                       const uint64_t* off, uint32_t n_sent, uint32_t T, const uint8_t* keep, const w2v_heads* out,
+                       float* lse) {
+    AttendArgs a;
+    a.q = heads_of(q); a.k = heads_of(k); a.v = heads_of(v);
+    a.off = off; a.n_sent = n_sent; a.T = T;
+    a.heads = s->heads; a.kv_heads = s->kv_heads; a.group = s->heads / s->kv_heads; a.width = s->width;
+    a.left = s->left < T ? s->left : T; a.right = s->right < T ? s->right : T;
+    a.sinks = s->sinks; a.skip_self = s->skip_self != 0;
+    a.scale = s->scale; a.scale2 = s->scale * 1.4426950408889634f;
+    a.keep = keep;
+    a.bias = s->bias_dev; a.buckets = s->bucket_dev; a.n_buckets = s->n_buckets; a.span = s->span;
+    a.o = heads_out(out); a.lse = lse;
+    return a;
+}
+
+}  // namespace
+
+extern "C" int w2v_relative_buckets(uint32_t n_buckets, uint32_t span, uint32_t* map) {
+    if (!map) return fail(W2V_ERR_NULL, "map is NULL");
+    if (n_buckets < 2 || n_buckets > W2V_BUCKETS_MAX)
+        return fail(W2V_ERR_ARG, "n_buckets = %u outside 2..%d", n_buckets, W2V_BUCKETS_MAX);
+    if (span == 0 || span > W2V_SPAN_MAX) return fail(W2V_ERR_ARG, "span = %u outside 1..%d", span, W2V_SPAN_MAX);
+    const uint32_t half = n_buckets / 2, near = half / 2 ? half / 2 : 1, far = half - near;
+    uint32_t t = 0;                           // distances near (span / near)^(t / far) are where bucket near + t begins
+    for (uint32_t r = 0; r <= span; ++r) {
+        uint32_t b = r < half - 1 ? r : half - 1;
+        if (r >= near && far) {
+            // a distance that meets a border in exact arithmetic is past it: the quotients of the logarithms of two
+            // such numbers below 2^10 are farther than 1e-9 from the border or on it
+            while (t + 1 < far && far * std::log((double)r / near) >= (t + 1) * std::log((double)span / near) - 1e-9) ++t;
+            b = near + t;
+        }
+        map[span - r] = b;
+        if (r) map[span + r] = half + b;
+    }
+    return W2V_OK;
+}
+
+extern "C" int w2v_attend(const w2v_attend_spec* spec, const w2v_heads* q, const w2v_heads* k, const w2v_heads* v,
+                          const uint64_t* sent_off, uint32_t n_sent, uint32_t n_tokens, const uint8_t* keep,
+                          const w2v_heads* out, float* lse, void* stream) {
+    if (int rc = check_spec(spec)) return rc;
+    if (int rc = check_tokens(spec, sent_off, n_sent, n_tokens)) return rc;
+    if (n_tokens == 0) return W2V_OK;
+    if (int rc = check_heads(q, spec, spec->heads, n_tokens, false, "q")) return rc;
+    if (int rc = check_heads(k, spec, spec->kv_heads, n_tokens, false, "k")) return rc;
+    if (int rc = check_heads(v, spec, spec->kv_heads, n_tokens, false, "v")) return rc;
+    if (int rc = check_heads(out, spec, spec->heads, n_tokens, true, "out")) return rc;
+    launch_attend(attend_args(spec, q, k, v, sent_off, n_sent, n_tokens, keep, out, lse), (uint32_t)spec->type,
+                  (hipStream_t)stream);
+    return launched();
+}
+
+namespace {
+// The parts of the backward pass's workspace, each from a 256-byte border on.
+struct BackwardSpace {
+    size_t delta, by_distance, bytes;
+    BackwardSpace(const w2v_attend_spec* s, uint32_t T) {
+        size_t at = 0;
+        const auto part = [&](size_t count) {
+            const size_t from = at;
+            at += (count * sizeof(float) + 255) / 256 * 256;
+            return from;
+        };
+        delta = part((size_t)s->heads * T);
+        by_distance = part(s->bias_dev ? (size_t)s->heads * attend_bias_parts(T) * (2 * s->span + 1) : 0);
+        bytes = at;
+    }
+};
+}  // namespace
+
+extern "C" size_t w2v_attend_backward_workspace(const w2v_attend_spec* spec, uint32_t n_tokens) {
+    if (check_spec(spec) || n_tokens > 0x7FFFFFFFu - 4095u) return 0;
+    return BackwardSpace(spec, n_tokens).bytes;
+}
+
+extern "C" int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads* dout, const w2v_heads* q, const w2v_heads* k,
+                                   const w2v_heads* v, const w2v_heads* out, const float* lse, const uint64_t* sent_off,
+                                   uint32_t n_sent, uint32_t n_tokens, const uint8_t* keep, const w2v_heads* dq,
+                                   const w2v_heads* dk, const w2v_heads* dv, float* dbias, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    if (int rc = check_spec(spec)) return rc;
+    if (int rc = check_tokens(spec, sent_off, n_sent, n_tokens)) return rc;
+    if (dbias && !spec->bias_dev) return fail(W2V_ERR_ARG, "the gradient of a bias that was not given");
+    BackwardArgs b{};
+    if (n_tokens) {
+        const w2v_heads* of_query[] = {dout, q, out};
+        const w2v_heads* of_key[] = {k, v};
+        const char* names[] = {"dout", "q", "out", "k", "v"};
+        for (int n = 0; n < 3; ++n)
+            if (int rc = check_heads(of_query[n], spec, spec->heads, n_tokens, false, names[n])) return rc;
+        for (int n = 0; n < 2; ++n)
+            if (int rc = check_heads(of_key[n], spec, spec->kv_heads, n_tokens, false, names[3 + n])) return rc;
+        if (int rc = check_heads(dq, spec, spec->heads, n_tokens, true, "dq")) return rc;
+        if (int rc = check_heads(dk, spec, spec->kv_heads, n_tokens, true, "dk")) return rc;
+        if (int rc = check_heads(dv, spec, spec->kv_heads, n_tokens, true, "dv")) return rc;
+        if (!lse) return fail(W2V_ERR_NULL, "lse_dev is NULL");
+        const BackwardSpace space(spec, n_tokens);
+        if (!workspace) return fail(W2V_ERR_NULL, "workspace is NULL");
+        if (!aligned(workspace, 256)) return fail(W2V_ERR_ARG, "workspace must be 256-byte aligned");
+        if (workspace_bytes < space.bytes)
+            return fail(W2V_ERR_ARG, "workspace of %zu bytes is too small: %zu are needed", workspace_bytes, space.bytes);
+        b.a = attend_args(spec, q, k, v, sent_off, n_sent, n_tokens, keep, out, const_cast<float*>(lse));
+        b.dout = heads_of(dout);
+        b.dq = heads_out(dq); b.dk = heads_out(dk); b.dv = heads_out(dv);
+        b.delta = (float*)((char*)workspace + space.delta);
+        b.by_distance = (float*)((char*)workspace + space.by_distance);
+    } else if (dbias) {
+        b.a.heads = spec->heads; b.a.buckets = spec->bucket_dev; b.a.n_buckets = spec->n_buckets; b.a.span = spec->span;
+    } else {
+        return W2V_OK;
+    }
+    b.dbias = dbias;
+    launch_attend_backward(b, (uint32_t)spec->type, (hipStream_t)stream);
     return launched();
 }

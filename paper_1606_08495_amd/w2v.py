@@ -19,6 +19,9 @@ K_MAX, D_MAX, S_MAX = 64, 1024, 32
 NORM_D_MAX = 16384
 NOALLOC_SCRATCH_U32 = 1 << 21
 
+UNBOUNDED = 0xFFFFFFFF
+HEAD_MAX, SINKS_MAX, SPAN_MAX, BUCKETS_MAX = 128, 64, 1023, 1024
+
 c_u32, c_u64, c_vp = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_void_p
 
 _SIGNATURES = {
@@ -69,6 +72,11 @@ _SIGNATURES = {
     "w2v_layer_norm_backward": (ctypes.c_int, [ctypes.c_int, c_vp, c_u64, c_vp, c_u64, c_u64, c_u32, c_vp,
                                                c_vp, c_vp, c_vp, c_u64, c_vp, c_vp, c_vp, ctypes.c_size_t,
                                                c_vp]),
+    "w2v_relative_buckets": (ctypes.c_int, [c_u32, c_u32, c_vp]),
+    "w2v_attend": (ctypes.c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_u32, c_u32, c_vp, c_vp, c_vp, c_vp]),
+    "w2v_attend_backward_workspace": (ctypes.c_size_t, [c_vp, c_u32]),
+    "w2v_attend_backward": (ctypes.c_int, [c_vp] * 6 + [c_vp, c_vp, c_u32, c_u32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                                        ctypes.c_size_t, c_vp]),
     "w2v_minibatch_seed": (c_u64, [c_u64, c_u64]),
     "w2v_shard_timing_enable": (ctypes.c_int, [c_vp, ctypes.c_int]),
     "w2v_shard_timing_read": (ctypes.c_int, [c_vp, c_vp, c_vp]),
@@ -456,3 +464,108 @@ def layer_norm_backward(dy, x, gain, mean, rstd, out=None, workspace=None, strea
                                              os_, columns.data_ptr(), columns.data_ptr() + 4 * d,
                                              workspace.data_ptr(), workspace.numel(), st.cuda_stream))
     return dx, columns[0], columns[1]
+
+
+class Heads(ctypes.Structure):
+    """w2v_heads: rows of heads, element c of head h of token i at p[i token_stride + h head_stride + c]."""
+    _fields_ = [("p", c_vp), ("token_stride", c_u64), ("head_stride", c_u64)]
+
+
+class AttendSpec(ctypes.Structure):
+    """w2v_attend_spec."""
+    _fields_ = [("type", ctypes.c_int32), ("heads", c_u32), ("kv_heads", c_u32), ("width", c_u32), ("left", c_u32),
+                ("right", c_u32), ("sinks", c_u32), ("skip_self", c_u32), ("scale", ctypes.c_float),
+                ("n_buckets", c_u32), ("span", c_u32), ("bias_dev", c_vp), ("bucket_dev", c_vp)]
+
+
+def relative_buckets(n_buckets, span, device="cuda"):
+    """The bucket of every distance -span..span (w2v_relative_buckets), int32 [2 span + 1] on the device."""
+    m = np.empty(2 * max(int(span), 0) + 1, np.uint32)
+    _check(lib().w2v_relative_buckets(int(n_buckets), int(span), c_vp(m.ctypes.data)))
+    return as_index_tensor(m, device)
+
+
+def _heads(t, like, rows, heads, name):
+    """[rows, heads, width], the elements of a head side by side."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype == like.dtype and
+            t.device == like.device and t.shape == (rows, heads, like.shape[2])):
+        raise TypeError("%s must be a CUDA tensor [%d, %d, %d] of %s" % (name, rows, heads, like.shape[2], like.dtype))
+    a, b, c = t.stride()
+    if (c != 1 and t.shape[2] > 1) or a < 0 or b < 0:
+        raise ValueError("%s: the elements of a head must lie side by side" % name)
+    return Heads(t.data_ptr(), a, b)
+
+
+def _spec(q, kv_heads, left, right, sinks, skip_self, scale, bias, buckets):
+    if q.dtype not in TYPES:
+        raise TypeError("q must be float32, float16 or bfloat16")
+    heads, width = q.shape[1], q.shape[2]
+    s = AttendSpec(TYPES[q.dtype], heads, kv_heads, width, UNBOUNDED if left is None else int(left),
+                   UNBOUNDED if right is None else int(right), int(sinks), 1 if skip_self else 0,
+                   width ** -0.5 if scale is None else float(scale))
+    if bias is not None:
+        if bias.dim() != 2 or bias.shape[0] != heads or bias.device != q.device:
+            raise ValueError("bias must be [heads, buckets]")
+        if buckets is None or buckets.dim() != 1 or buckets.numel() % 2 == 0 or buckets.device != q.device:
+            raise ValueError("buckets must give the bucket of the distances -span..span")
+        s.n_buckets, s.span = bias.shape[1], buckets.numel() // 2
+        s.bias_dev, s.bucket_dev = _dev(bias, torch.float32, "bias"), _dev(buckets, IDX, "buckets")
+    return s
+
+
+def _texts(sent_off, keep, q):
+    if sent_off.device != q.device or (keep is not None and (keep.device != q.device or keep.shape != (q.shape[0],))):
+        raise ValueError("sent_off and keep [tokens] must be on the device of q")
+    return (_dev(sent_off, torch.int64, "sent_off"), max(sent_off.numel() - 1, 0), q.shape[0],
+            _dev(keep, torch.uint8, "keep"))
+
+
+def attend(q, k, v, sent_off, left=None, right=None, sinks=0, skip_self=False, scale=None, keep=None, bias=None,
+           buckets=None, out=None, stream=None):
+    """(out, lse) of w2v_attend: q [tokens, heads, width], k and v [tokens, kv_heads, width], texts as sent_off
+    int64 [n + 1].  left, right: words shown on either side (None: all).  scale: width^-1/2 unless given.  keep:
+    uint8 [tokens], 0 where a word is not to be seen.  bias float32 [heads, buckets] with the map ``buckets`` (relative_buckets)."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise TypeError("q, k and v must be [tokens, heads, width]")
+    T, H, _ = q.shape
+    G = k.shape[1]
+    with _on(stream, q):
+        st = torch.cuda.current_stream(q.device)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+        spec = _spec(q, G, left, right, sinks, skip_self, scale, bias, buckets)
+        off, n, t, kp = _texts(sent_off, keep, q)
+        _check(lib().w2v_attend(ctypes.byref(spec), ctypes.byref(_heads(q, q, T, H, "q")),
+                                ctypes.byref(_heads(k, q, T, G, "k")), ctypes.byref(_heads(v, q, T, G, "v")), off, n, t, kp,
+                                ctypes.byref(_heads(out, q, T, H, "out")), lse.data_ptr(), st.cuda_stream))
+    return out, lse
+
+
+def attend_backward(dout, q, k, v, out, lse, sent_off, left=None, right=None, sinks=0, skip_self=False, scale=None,
+                    keep=None, bias=None, buckets=None, workspace=None, stream=None):
+    """(dq, dk, dv, dbias) of w2v_attend_backward, for the arguments and results of ``attend``; dbias is None without
+    a bias.  ``workspace``: optional uint8 device tensor to reuse."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise TypeError("q, k and v must be [tokens, heads, width]")
+    T, H, _ = q.shape
+    G = k.shape[1]
+    if lse.shape != (H, T) or lse.device != q.device:
+        raise ValueError("lse must be [heads, tokens]")
+    with _on(stream, q):
+        st = torch.cuda.current_stream(q.device)
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        dk, dv = [torch.empty(k.shape, dtype=q.dtype, device=q.device) for _ in range(2)]
+        dbias = None if bias is None else torch.empty(bias.shape, dtype=torch.float32, device=q.device)
+        spec = _spec(q, G, left, right, sinks, skip_self, scale, bias, buckets)
+        if workspace is None:
+            need = int(lib().w2v_attend_backward_workspace(ctypes.byref(spec), T))
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        off, n, t, kp = _texts(sent_off, keep, q)
+        r = ctypes.byref
+        _check(lib().w2v_attend_backward(
+            r(spec), r(_heads(dout, q, T, H, "dout")), r(_heads(q, q, T, H, "q")), r(_heads(k, q, T, G, "k")),
+            r(_heads(v, q, T, G, "v")), r(_heads(out, q, T, H, "out")), _dev(lse, torch.float32, "lse"), off, n, t, kp,
+            r(_heads(dq, q, T, H, "dq")), r(_heads(dk, q, T, G, "dk")), r(_heads(dv, q, T, G, "dv")),
+            _dev(dbias, torch.float32, "dbias"), workspace.data_ptr(), workspace.numel(), st.cuda_stream))
+    return dq, dk, dv, dbias
