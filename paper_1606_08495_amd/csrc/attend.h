@@ -170,10 +170,10 @@ __device__ inline float2 row_gradient(const BackwardArgs& b, uint32_t head, uint
     return make_float2(p, p == 0.f ? 0.f : p * (dp - delta));
 }
 
-// dq_i; bias_sums (optional): the wavefront's own 2 span + 1 sums of dS by distance, in LDS.
+// dq_i.
 template <typename T>
 __device__ void query_row(const BackwardArgs& b, uint32_t head, uint32_t i, const Shown& s, float delta, uint32_t lane,
-                          float (&dq)[2], float* bias_sums) {
+                          float (&dq)[2]) {
     const AttendArgs& a = b.a;
     const uint32_t sunk = s.sunk - s.first, n = sunk + s.hi - s.lo;
     dq[0] = dq[1] = 0.f;
@@ -182,13 +182,6 @@ __device__ void query_row(const BackwardArgs& b, uint32_t head, uint32_t i, cons
         const uint32_t j = at < sunk ? s.first + at : s.lo + at - sunk;
         const bool in = at < n && row_keeps(a, i, j);
         const float ds = in ? row_gradient<T>(b, head, i, j, delta).y : 0.f;
-        if (bias_sums) {
-            const int32_t dist = (int32_t)j - (int32_t)i, span = (int32_t)a.span;
-            const float low = lanes_sum<64>(in && dist <= -span ? ds : 0.f);
-            const float high = lanes_sum<64>(in && dist >= span ? ds : 0.f);
-            if (in && dist > -span && dist < span) bias_sums[dist + span] += ds;      // one lane a distance
-            if (lane == 0) { bias_sums[0] += low; bias_sums[2 * span] += high; }
-        }
         for (uint64_t left = __ballot(in && ds != 0.f); left; left &= left - 1) {
             const int l = __builtin_ctzll(left);
             const uint32_t jl = (uint32_t)__shfl((int)j, l, 64);

@@ -48,7 +48,13 @@ struct BackwardArgs {
     HeadsOut dq, dk, dv; float* dbias;                   // dbias [heads][n_buckets], may be null
     float* delta;                                        // workspace: [heads][T] sums of dout o
     float* by_distance;                                  // workspace: [heads][bias_parts][2 span + 1]
+    // first words that stay visible: queries further than `reach` behind their block are taken in `late` pieces of
+    // late_words queries, whose sums (and those of the text's own block) lie in workspace: [late][kv_heads][sinks][2][width]
+    uint32_t late, late_words, reach;
+    float* late_sums; float* own_sums;
 };
+struct LatePieces { uint32_t count, words, reach; };
+LatePieces attend_late_pieces(uint32_t T, uint32_t left, uint32_t sinks);
 uint32_t attend_bias_parts(uint32_t T);
 void launch_attend_backward(const BackwardArgs& b, uint32_t type, hipStream_t st);
 

@@ -14,111 +14,12 @@
 // leaves them the relative rounding that v has; their sum is taken before the rounding.  Heads of up to 32 columns add
 // what the rounding left in a second product: the gradient's dout . out is then a sum of few terms, which
 // may cancel down to the weights' rounding, and the matrix cores wait for the exponentials there anyway.
-#include "attend.h"
-#include "tiles.h"
+#include "attend_tiles.h"
 
 namespace w2v {
 namespace {
 
-constexpr int BLOCK_WORDS = 128, WAVE_WORDS = 32, KEYS = 64, THREADS = 256;
 constexpr float RISE = 8.f;           // how far (to base two) a maximum may rise before outputs are rescaled
-
-// A word and what it is shown, for the lanes of a wavefront; and over the wavefront's words, in scalar registers.
-struct Words {
-    uint32_t i; Shown s;
-    uint32_t lo_least, lo_most, hi_least, hi_most, i_first, i_last, first_least, sunk_least;
-    __device__ Words(const AttendArgs& a, uint32_t first, uint32_t lane) {
-        const uint32_t last = first + WAVE_WORDS - 1 < a.T ? first + WAVE_WORDS - 1 : a.T - 1;
-        i = first + lane % WAVE_WORDS < last ? first + lane % WAVE_WORDS : last;
-        i_first = first < last ? first : last;
-        i_last = last;
-        const uint32_t s0 = text_of(a.off, a.n_sent, i_first, lane), s1 = text_of(a.off, a.n_sent, i_last, lane);
-        s = shown_to(a, i, text_between(a.off, s0, s1, i, a.T));
-        lo_least = __builtin_amdgcn_readfirstlane(s.lo);
-        hi_least = __builtin_amdgcn_readfirstlane(s.hi);
-        first_least = __builtin_amdgcn_readfirstlane(s.first);
-        sunk_least = __builtin_amdgcn_readfirstlane(s.sunk);
-        lo_most = __builtin_amdgcn_readlane(s.lo, WAVE_WORDS - 1);
-        hi_most = __builtin_amdgcn_readlane(s.hi, WAVE_WORDS - 1);
-    }
-    // Whether any of the words is shown any of the tokens j0 .. j0 + 31.  (First words that stay visible lie before all
-    // windows only for the first word's text: later texts begin at or after the first word.)
-    __device__ bool shown_any(uint32_t j0) const {
-        return j0 < hi_most && (j0 + 32 > lo_least || (j0 < sunk_least && j0 + 32 > first_least));
-    }
-};
-
-// The axis of keys of a block: `sunk` words from `first` on, then those from `lo` to the end.
-struct Axis {
-    uint32_t first, sunk, shift, count;
-    __device__ Axis(const AttendArgs& a, uint32_t word0, uint32_t lane) {
-        const uint32_t last = word0 + BLOCK_WORDS - 1 < a.T ? word0 + BLOCK_WORDS - 1 : a.T - 1;
-        const uint32_t s0 = text_of(a.off, a.n_sent, word0, lane), s1 = text_of(a.off, a.n_sent, last, lane);
-        const Shown from = shown_to(a, word0, text_bounds(a.off, s0, word0, a.T));
-        const Shown to = shown_to(a, last, text_bounds(a.off, s1, last, a.T));
-        first = from.first;
-        sunk = from.sunk - from.first;
-        shift = from.lo - sunk;                       // token of key n >= sunk: n + shift
-        count = sunk + (to.hi > from.lo ? to.hi - from.lo : 0);
-        first = __builtin_amdgcn_readfirstlane(first);
-        sunk = __builtin_amdgcn_readfirstlane(sunk);
-        shift = __builtin_amdgcn_readfirstlane(shift);
-        count = __builtin_amdgcn_readfirstlane(count);
-    }
-    __device__ uint32_t token(uint32_t n) const { return n < sunk ? first + n : shift + n; }
-};
-
-// Bias by distance, times log2 e, with the outermost values repeated on both sides so that every distance within a
-// 32 x 32 piece that is not wholly past the span is in the table.
-constexpr int BIAS_SIDE = 64, BIAS_TABLE = 2 * SPAN_MAX + 1 + 2 * BIAS_SIDE;
-__device__ inline void fill_bias(const AttendArgs& a, uint32_t head, float* table) {
-    const int32_t reach = (int32_t)a.span + BIAS_SIDE;
-    for (int32_t at = threadIdx.x; at <= 2 * reach; at += THREADS) table[at] = scaled_bias(a, head, at - reach);
-}
-
-// Scores of a piece of 32 keys, with bias and mask: s on the way in holds the products.
-template <bool BIAS>
-__device__ inline void piece_scores(const AttendArgs& a, const Words& w, const Axis& x, uint32_t n0, uint64_t kept, bool linear,
-                                    const float* table, uint32_t h, Acc& s) {
-    const uint32_t j0 = n0 + x.shift;                 // of the piece's first key where the axis is linear
-    const uint32_t kept32 = (uint32_t)kept;
-    const bool all = linear && j0 >= w.lo_most && j0 + 32 <= w.hi_least && kept32 == 0xFFFFFFFFu &&
-                     !(a.skip_self && j0 <= w.i_last && j0 + 32 > w.i_first);
-    const int32_t span = (int32_t)a.span;
-    if constexpr (BIAS) {
-        const int32_t reach = span + BIAS_SIDE;
-        if (linear) {
-            const int32_t far = (int32_t)j0 - (int32_t)w.i_first + 31, near = (int32_t)j0 - (int32_t)w.i_last;
-            if (far <= -span || near >= span) {
-                const float b = table[far <= -span ? 0 : 2 * reach];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, b);
-            } else {
-                const float* at = table + ((int32_t)j0 - (int32_t)w.i + reach + 4 * (int32_t)h);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, at[acc_row(r, 0)]);
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int32_t dist = (int32_t)x.token(n0 + acc_row(r, h)) - (int32_t)w.i;
-                s[r] = fmaf(s[r], a.scale2, table[(dist < -reach ? -reach : dist > reach ? reach : dist) + reach]);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= a.scale2;
-    }
-    if (all) return;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const uint32_t row = acc_row(r, h), j = linear ? j0 + row : x.token(n0 + row);
-        bool in = (j - w.s.lo < w.s.hi - w.s.lo) | (j - w.s.first < w.s.sunk - w.s.first);
-        in &= (kept32 >> row & 1) != 0;
-        in &= !(a.skip_self && j == w.i);
-        s[r] = in ? s[r] : -__builtin_inff();
-    }
-}
 
 template <typename T, int DB, bool BIAS>
 __global__ __launch_bounds__(THREADS) void attend_kernel(const AttendArgs a) {

@@ -1,93 +1,511 @@
-// Attention over texts, backward: one wavefront at a time per word and head, and per word and key head.
-#include "attend.h"
+// Attention over texts, backward.
+//
+//   dS = p (dP - delta),  dP = dout v^T,  delta = rowsum(dout out)
+//   dq = scale dS k,  dk = scale dS^T q,  dv = p^T dout,  dbias[b] = sum of dS over the pairs of bucket b
+// Weights are formed anew from q, k and the rows' logarithms.  No sum is shared between blocks, so no atomics and the
+// same bits every time: one kernel holds 128 words as queries and walks over their keys (dq, and the bias' sums; three
+// products a pair), another holds 128 words as keys and walks over the queries they are shown to (dk, dv; four products a
+// pair).  That is seven products instead of the five of a kernel that adds dq up in memory.  In both a
+// wavefront's own 32 words are the lanes, their rows feed the B operands from registers, and p and dS feed the last
+// products from the registers they are formed in; p and dS are rounded to the rows' type there, all sums are fp32.
+//
+// A text's first words that stay visible are seen by every later word.  The keys' kernel takes the queries up to a
+// border behind its block; those behind go in pieces to blocks of their own (late), whose sums are joined in
+// order at the end.
+#include "attend_tiles.h"
 
 namespace w2v {
 namespace {
 
-constexpr int BLOCK_WORDS = 128, THREADS = 256, WAVES = THREADS / WAVE;
-
-template <typename T> __global__ __launch_bounds__(THREADS) void query_rows_kernel(const BackwardArgs b) {
-    const AttendArgs& a = b.a;
-    __shared__ float sums[WAVES][2 * SPAN_MAX + 1];
-    const uint32_t lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, head = blockIdx.x % a.heads;
-    const uint32_t part = blockIdx.x / a.heads, distances = 2 * a.span + 1;
-    if (b.dbias) for (uint32_t c = lane; c < distances; c += WAVE) sums[wave][c] = 0.f;
-    for (uint32_t n = wave; n < BLOCK_WORDS; n += WAVES) {
-        const uint32_t i = part * BLOCK_WORDS + n;
-        if (i >= a.T) break;
-        const Shown s = shown_to(a, i, text_bounds(a.off, text_of(a.off, a.n_sent, i, lane), i, a.T));
-        const T *o = (const T*)head_row<T>(a.o, i, head), *g = head_row<T>(b.dout, i, head);
-        float delta = 0.f;
-        for (uint32_t c = lane; c < a.width; c += WAVE) delta = fmaf((float)o[c], (float)g[c], delta);
-        delta = lanes_sum<64>(delta);
-        if (lane == 0) b.delta[(size_t)head * a.T + i] = delta;
-        float row[2];
-        query_row<T>(b, head, i, s, delta, lane, row, b.dbias ? sums[wave] : nullptr);
-        T* dq = head_row<T>(b.dq, i, head);
-        for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) dq[lane + c * WAVE] = (T)row[c];
-    }
-    if (!b.dbias) return;
-    __syncthreads();
-    float* to = b.by_distance + ((size_t)head * gridDim.x / a.heads + part) * distances;
-    for (uint32_t c = threadIdx.x; c < distances; c += THREADS)
-        to[c] = (sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c]);
-}
-
-template <typename T> __global__ __launch_bounds__(THREADS) void key_rows_kernel(const BackwardArgs b) {
-    const AttendArgs& a = b.a;
-    const uint32_t lane = threadIdx.x % WAVE;
-    const uint64_t at = (uint64_t)blockIdx.x * WAVES + threadIdx.x / WAVE;
-    const uint32_t j = (uint32_t)(at / a.kv_heads), kv_head = (uint32_t)(at % a.kv_heads);
-    if (j >= a.T) return;
-    const Shown s = sees(a, j, text_bounds(a.off, text_of(a.off, a.n_sent, j, lane), j, a.T));
-    float dk[2] = {0.f, 0.f}, dv[2] = {0.f, 0.f};
-    key_row<T>(b, kv_head, j, s.lo, s.sunk, lane, dk, dv);
-    T *to_k = head_row<T>(b.dk, j, kv_head), *to_v = head_row<T>(b.dv, j, kv_head);
-    for (int c = 0; c < 2; ++c)
-        if (lane + c * WAVE < a.width) {
-            to_k[lane + c * WAVE] = (T)(dk[c] * a.scale);
-            to_v[lane + c * WAVE] = (T)dv[c];
+// What is stored of a lane's column of results: row `to` of `width` elements, c[b] rows 32 b + acc_row.
+template <typename T, int DB> __device__ inline void store_column(T* to, uint32_t width, const Acc (&c)[DB], float factor, uint32_t h) {
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const uint32_t at = 32 * b + acc_row(r, h);
+            typename Pack<T, 4>::vec four;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) four[e] = (T)(c[b][r + e] * factor);
+            if (at + 4 <= width) *(typename Pack<T, 4>::mem*)(to + at) = four;
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (at + e < width) to[at + e] = four[e];
         }
 }
+// Whether a lane's column, both halves of it, holds a value that is not finite.
+template <int DB> __device__ inline bool not_finite(const Acc (&c)[DB]) {
+    float worst = 0.f;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) worst = fmaf(c[b][r], 0.f, worst);
+    return halves_sum(worst) != 0.f;
+}
 
-// dbias of one head: the parts' sums by distance, then the distances of each bucket, both in order.
-__global__ __launch_bounds__(1024) void bias_buckets_kernel(const BackwardArgs b, uint32_t parts) {
+// ---- queries: dq, delta, the bias' sums -----------------------------------------------------------------
+// Sums of dS by distance: an array in LDS for each half of each wavefront, in which the 32 lanes of one register's row
+// lie side by side, so that no two lanes add to one place at a time; outermost distances by registers.
+template <typename T, int DB, bool BIAS>
+__global__ __launch_bounds__(THREADS) void query_kernel(const BackwardArgs b) {
+    const AttendArgs& a = b.a;
+    typedef Tile<T, DB, KEYS> Tl;
+    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 64 * 1024 ? 2 : 1;
+    __shared__ __align__(16) char tiles[BUFFERS][2][Tl::BYTES];
+    extern __shared__ float dynamic[];
+    const int32_t span = (int32_t)a.span, reach = span + BIAS_SIDE;
+    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE;
+    const uint32_t head = blockIdx.x % a.heads, kv_head = head / a.group;
+    const uint32_t words = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS;
+    const uint32_t part = words - 1 - blockIdx.x / a.heads, word0 = part * BLOCK_WORDS;
+    float* const table = dynamic;
+    float* const sums = dynamic + (2 * wave + 1 + h) * (2 * reach + 1);
+    const Axis x(a, word0, lane);
+    const uint32_t first = word0 + wave * WAVE_WORDS;
+    const Words w(a, first < a.T ? first : a.T - 1, lane);
+    const bool some = first < a.T, real = first + lane % WAVE_WORDS < a.T;
+    if (BIAS) {
+        fill_bias(a, head, table);
+        if (b.dbias) for (int32_t c = lane % 32; c <= 2 * reach; c += 32) sums[c] = 0.f;
+    }
+
+    typename Frag<T>::vec q[2 * DB], g[2 * DB];
+    float delta = 0.f;
+#pragma unroll
+    for (int s = 0; s < 2 * DB; ++s) {
+        q[s] = load_operand(head_row<T>(a.q, w.i, head), s, h, a.width);
+        g[s] = load_operand(head_row<T>(b.dout, w.i, head), s, h, a.width);
+        const auto o = load_operand((const T*)head_row<T>(a.o, w.i, head), s, h, a.width);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            delta = fmaf((float)g[s][t], (float)o[t], delta);
+            if (!real) g[s][t] = (T)0.f;              // lanes past the last word repeat it, without weight
+        }
+    }
+    delta = real ? halves_sum(delta) : 0.f;
+    float lse2 = a.lse[(size_t)head * a.T + w.i];
+    if (real && h == 0) b.delta[(size_t)head * a.T + w.i] = delta;
+    lse2 = lse2 == -__builtin_inff() ? 0.f : lse2 * LOG2E;      // of a word that is shown nothing: every score is masked
+    Acc dq[DB];
+#pragma unroll
+    for (int n = 0; n < DB; ++n) dq[n] = Acc{};
+    float low = 0.f, high = 0.f;
+
+    Transit<T, DB, KEYS, THREADS> tk, tv;
+    uint8_t keep = 1;
+    const uint32_t count = (x.count + KEYS - 1) / KEYS;
+    const auto fetch = [&](uint32_t t) {
+        const auto row = [&](const Heads& p, uint32_t r) -> const T* {
+            const uint32_t n = t * KEYS + r;
+            if (n >= x.count) return nullptr;
+            const uint32_t j = x.token(n);
+            return a.keep && !a.keep[j] ? nullptr : head_row<T>(p, j, kv_head);
+        };
+        tk.load([&](uint32_t r) { return row(a.k, r); }, a.width);
+        tv.load([&](uint32_t r) { return row(a.v, r); }, a.width);
+        if (a.keep) keep = t * KEYS + lane < x.count ? a.keep[x.token(t * KEYS + lane)] : 0;
+    };
+    uint64_t kept = ~0ull;
+    if (count) {
+        fetch(0);
+        tk.store(tiles[0][0]);
+        tv.store(tiles[0][1]);
+        kept = __ballot(keep != 0);
+    }
+    __syncthreads();
+    for (uint32_t t = 0; t < count; ++t) {
+        if (t + 1 < count) fetch(t + 1);
+        const char *kt = tiles[t % BUFFERS][0], *vt = tiles[t % BUFFERS][1];
+#pragma unroll
+        for (uint32_t piece = 0; piece < KEYS / 32; ++piece) {
+            const uint32_t n0 = t * KEYS + piece * 32, j0 = n0 + x.shift;
+            const bool linear = n0 >= x.sunk;
+            if (!some || n0 >= x.count || (linear && !w.shown_any(j0))) continue;
+            Acc s = {}, dp = {};
+#pragma unroll
+            for (int k = 0; k < 2 * DB; ++k) {
+                mma(Tl::along(kt, piece * 32 + lane % 32, k, h), q[k], s);
+                mma(Tl::along(vt, piece * 32 + lane % 32, k, h), g[k], dp);
+            }
+            piece_scores<BIAS>(a, w, x, n0, kept >> (piece * 32), linear, table, h, s);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = __builtin_amdgcn_exp2f(s[r] - lse2);
+                s[r] = p * (dp[r] - delta);
+                if (BIAS && p == 0.f) s[r] = 0.f;     // the sums by distance are not formed anew
+            }
+            if constexpr (BIAS) {
+                if (b.dbias) {
+                    const int32_t far = (int32_t)j0 - (int32_t)w.i_first + 31, near = (int32_t)j0 - (int32_t)w.i_last;
+                    if (linear && (far <= -span || near >= span)) {
+                        float all = 0.f;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) all += s[r];
+                        if (far <= -span) low += all; else high += all;
+                    } else if (linear) {
+                        float* at = sums + ((int32_t)j0 - (int32_t)w.i + reach + 4 * (int32_t)h);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            __hip_atomic_fetch_add(at + acc_row(r, 0), s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int32_t dist = (int32_t)x.token(n0 + acc_row(r, h)) - (int32_t)w.i;
+                            if (dist <= -span) low += s[r];
+                            else if (dist >= span) high += s[r];
+                            else __hip_atomic_fetch_add(sums + dist + reach, s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const auto ds = acc_operand<T>(s, k);
+#pragma unroll
+                for (int n = 0; n < DB; ++n) mma(Tl::across(kt, piece * 32, k, n, lane), ds, dq[n]);
+            }
+        }
+        if (t + 1 < count) {
+            if (BUFFERS == 1) __syncthreads();
+            tk.store(tiles[(t + 1) % BUFFERS][0]);
+            tv.store(tiles[(t + 1) % BUFFERS][1]);
+            kept = __ballot(keep != 0);
+            __syncthreads();
+        }
+    }
+    if (some) {
+        const bool redo = not_finite(dq);
+        if (real && !redo) store_column<T>(head_row<T>(b.dq, w.i, head), a.width, dq, a.scale, h);
+        for (uint64_t rows = __ballot(redo && real && h == 0); rows; rows &= rows - 1) {
+            const int l = __builtin_ctzll(rows);
+            Shown s;
+            s.lo = __shfl(w.s.lo, l, 64); s.hi = __shfl(w.s.hi, l, 64);
+            s.first = __shfl(w.s.first, l, 64); s.sunk = __shfl(w.s.sunk, l, 64);
+            const uint32_t i = __shfl(w.i, l, 64);
+            float row[2];
+            query_row<T>(b, head, i, s, __shfl(delta, l, 64), lane, row);
+            T* to = head_row<T>(b.dq, i, head);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) to[lane + c * WAVE] = (T)row[c];
+        }
+    }
+    if constexpr (BIAS) {
+        if (!b.dbias) return;
+        // the outermost distances: what lies past the span in the array, then what went by registers
+        __syncthreads();
+        const int32_t d = lane % 32 + 1;
+        static_assert(BIAS_SIDE == 64, "two places a lane on either side");
+        low = lanes_sum<32>(low + sums[BIAS_SIDE - d] + sums[BIAS_SIDE - 32 - d]);
+        high = lanes_sum<32>(high + sums[2 * reach - BIAS_SIDE + d] + sums[2 * reach - BIAS_SIDE + 32 + d]);
+        if (lane % 32 == 0) { sums[BIAS_SIDE] += low; sums[2 * reach - BIAS_SIDE] += high; }
+        __syncthreads();
+        float* to = b.by_distance + ((size_t)head * words + part) * (2 * span + 1);
+        for (int32_t c = threadIdx.x; c <= 2 * span; c += THREADS) {
+            float all = 0.f;
+#pragma unroll
+            for (int n = 0; n < 2 * THREADS / WAVE; ++n) all += dynamic[(1 + n) * (2 * reach + 1) + BIAS_SIDE + c];
+            to[c] = all;
+        }
+    }
+}
+
+// ---- keys: dk, dv ---------------------------------------------------------------------------------------
+// The border behind which queries of the block's first words that stay visible are late.
+__device__ inline uint32_t late_border(const BackwardArgs& b, uint32_t j) {
+    return j / BLOCK_WORDS * BLOCK_WORDS + BLOCK_WORDS + b.reach;
+}
+
+template <typename T, int DB, bool BIAS>
+__global__ __launch_bounds__(THREADS) void key_kernel(const BackwardArgs b) {
+    const AttendArgs& a = b.a;
+    typedef Tile<T, DB, KEYS> Tl;
+    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 64 * 1024 ? 2 : 1;
+    __shared__ __align__(16) char tiles[BUFFERS][2][Tl::BYTES];
+    __shared__ float rows[BUFFERS][2][KEYS];          // the queries' logarithms to base two, and delta
+    extern __shared__ float table[];
+    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE;
+    const uint32_t kv_head = blockIdx.x % a.kv_heads, block = blockIdx.x / a.kv_heads;
+    const bool late = block < b.late;
+    const int32_t reach = (int32_t)a.span + BIAS_SIDE;
+
+    // the block's keys k0 .. k1, the queries q0 .. q1 that any of them is shown to, and a lane's own [lo, hi) of them
+    uint32_t k0, k1, q0, q1;
+    if (late) {
+        q0 = block * b.late_words;
+        const Text t = text_bounds(a.off, text_of(a.off, a.n_sent, q0, lane), q0, a.T);
+        k0 = t.first;
+        k1 = t.end - t.first < a.sinks ? t.end : t.first + a.sinks;
+        q1 = t.end < q0 + b.late_words ? t.end : q0 + b.late_words;
+        if (late_border(b, k0) >= q1) return;         // none of this piece's queries are late
+    } else {
+        k0 = (block - b.late) * BLOCK_WORDS;
+        k1 = k0 + BLOCK_WORDS < a.T ? k0 + BLOCK_WORDS : a.T;
+        const uint32_t s0 = text_of(a.off, a.n_sent, k0, lane), s1 = text_of(a.off, a.n_sent, k1 - 1, lane);
+        q0 = sees(a, k0, text_bounds(a.off, s0, k0, a.T)).lo;
+        const Text t = text_bounds(a.off, s1, k1 - 1, a.T);
+        q1 = sees(a, k1 - 1, t).hi;
+        if (a.sinks && t.first + a.sinks > k0) {
+            const uint32_t border = late_border(b, k0), to = t.end < border ? t.end : border;
+            q1 = q1 < to ? to : q1;
+        }
+    }
+    k0 = __builtin_amdgcn_readfirstlane(k0);
+    k1 = __builtin_amdgcn_readfirstlane(k1);
+    q0 = __builtin_amdgcn_readfirstlane(q0);
+    q1 = __builtin_amdgcn_readfirstlane(q1);
+    const uint32_t wave0 = k0 + wave * WAVE_WORDS;
+    const bool some = wave0 < k1, real = wave0 + lane % WAVE_WORDS < k1;
+    const uint32_t j = real ? wave0 + lane % WAVE_WORDS : k1 - 1;
+    uint32_t lo = 0, hi = 0, text_first, text_end;
+    {
+        const uint32_t j0 = some ? wave0 : k1 - 1, j1 = wave0 + WAVE_WORDS - 1 < k1 ? wave0 + WAVE_WORDS - 1 : k1 - 1;
+        const Text t = text_between(a.off, text_of(a.off, a.n_sent, j0, lane), text_of(a.off, a.n_sent, j1, lane), j, a.T);
+        text_first = t.first;
+        text_end = t.end;
+        const uint32_t border = late_border(b, j);
+        if (real && !(a.keep && !a.keep[j])) {
+            if (late) {
+                lo = border > q0 ? border : q0;
+                hi = q1;
+            } else {
+                const Shown s = sees(a, j, t);
+                lo = s.lo;
+                hi = s.sunk < border ? s.sunk : border;
+                hi = hi < s.hi ? s.hi : hi;
+            }
+            if (lo >= hi) lo = hi = 0;
+        }
+    }
+    uint32_t lo_least = lo < hi ? lo : ~0u, lo_most = lo_least, hi_most = hi, hi_least = hi;
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) {
+        lo_least = min(lo_least, (uint32_t)__shfl_xor((int)lo_least, m, 64));
+        lo_most = max(lo_most, (uint32_t)__shfl_xor((int)lo_most, m, 64));
+        hi_least = min(hi_least, (uint32_t)__shfl_xor((int)hi_least, m, 64));
+        hi_most = max(hi_most, (uint32_t)__shfl_xor((int)hi_most, m, 64));
+    }
+    lo_least = __builtin_amdgcn_readfirstlane(lo_least);
+    lo_most = __builtin_amdgcn_readfirstlane(lo_most);
+    hi_least = __builtin_amdgcn_readfirstlane(hi_least);
+    hi_most = __builtin_amdgcn_readfirstlane(hi_most);
+    const uint32_t j_first = some ? wave0 : k1 - 1, j_last = wave0 + WAVE_WORDS - 1 < k1 ? wave0 + WAVE_WORDS - 1 : k1 - 1;
+
+    typename Frag<T>::vec kf[2 * DB], vf[2 * DB];
+#pragma unroll
+    for (int s = 0; s < 2 * DB; ++s) {
+        kf[s] = load_operand(head_row<T>(a.k, j, kv_head), s, h, a.width);
+        vf[s] = load_operand(head_row<T>(a.v, j, kv_head), s, h, a.width);
+    }
+    Acc dk[DB], dv[DB];
+#pragma unroll
+    for (int n = 0; n < DB; ++n) dk[n] = dv[n] = Acc{};
+
+    Transit<T, DB, KEYS, THREADS> tq, tg;
+    float lse2 = 0.f, delta = 0.f;
+    const uint32_t per_head = q1 > q0 ? (q1 - q0 + KEYS - 1) / KEYS : 0, count = per_head * a.group;
+    const auto fetch = [&](uint32_t t) {
+        const uint32_t head = kv_head * a.group + t / per_head, i0 = q0 + t % per_head * KEYS;
+        tq.load([&](uint32_t r) -> const T* { return i0 + r < q1 ? head_row<T>(a.q, i0 + r, head) : nullptr; }, a.width);
+        tg.load([&](uint32_t r) -> const T* { return i0 + r < q1 ? head_row<T>(b.dout, i0 + r, head) : nullptr; }, a.width);
+        if (threadIdx.x < KEYS && i0 + threadIdx.x < q1) {
+            const float l = a.lse[(size_t)head * a.T + i0 + threadIdx.x];
+            lse2 = l == -__builtin_inff() ? 0.f : l * LOG2E;
+            delta = b.delta[(size_t)head * a.T + i0 + threadIdx.x];
+        }
+    };
+    const auto put = [&](uint32_t t) {
+        tq.store(tiles[t % BUFFERS][0]);
+        tg.store(tiles[t % BUFFERS][1]);
+        if (threadIdx.x < KEYS) {
+            rows[t % BUFFERS][0][threadIdx.x] = lse2;
+            rows[t % BUFFERS][1][threadIdx.x] = delta;
+        }
+    };
+    if (count) {
+        fetch(0);
+        put(0);
+    }
+    for (uint32_t t = 0; t < count; ++t) {
+        if (BIAS && t % per_head == 0) {
+            __syncthreads();
+            fill_bias(a, kv_head * a.group + t / per_head, table);
+        }
+        if (BUFFERS == 1 || t == 0 || (BIAS && t % per_head == 0)) __syncthreads();
+        if (t + 1 < count) fetch(t + 1);
+        const char *qt = tiles[t % BUFFERS][0], *gt = tiles[t % BUFFERS][1];
+#pragma unroll
+        for (uint32_t piece = 0; piece < KEYS / 32; ++piece) {
+            const uint32_t i0 = q0 + t % per_head * KEYS + piece * 32;
+            if (!some || i0 >= hi_most || i0 + 32 <= lo_least) continue;
+            Acc s = {}, dp = {};
+#pragma unroll
+            for (int k = 0; k < 2 * DB; ++k) {
+                mma(Tl::along(qt, piece * 32 + lane % 32, k, h), kf[k], s);
+                mma(Tl::along(gt, piece * 32 + lane % 32, k, h), vf[k], dp);
+            }
+            const float *l2 = &rows[t % BUFFERS][0][piece * 32 + 4 * h], *dl = &rows[t % BUFFERS][1][piece * 32 + 4 * h];
+            if constexpr (BIAS) {
+                const int32_t far = (int32_t)j_last - (int32_t)i0, near = (int32_t)j_first - (int32_t)i0 - 31;
+                if (far <= -(int32_t)a.span || near >= (int32_t)a.span) {
+                    const float c = table[far <= -(int32_t)a.span ? 0 : 2 * reach];
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, c - l2[acc_row(r, 0)]);
+                } else {
+                    const float* at = table + ((int32_t)j - (int32_t)i0 + reach - 4 * (int32_t)h);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, at[-acc_row(r, 0)]) - l2[acc_row(r, 0)];
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, -l2[acc_row(r, 0)]);
+            }
+            if (!(i0 >= lo_most && i0 + 32 <= hi_least && !(a.skip_self && i0 <= j_last && i0 + 32 > j_first))) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const uint32_t i = i0 + acc_row(r, h);
+                    const bool in = (i - lo < hi - lo) & !(a.skip_self && i == j);
+                    s[r] = in ? s[r] : -__builtin_inff();
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(s[r]);
+                dp[r] = s[r] * (dp[r] - dl[acc_row(r, 0)]);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const auto p = acc_operand<T>(s, k), ds = acc_operand<T>(dp, k);
+#pragma unroll
+                for (int n = 0; n < DB; ++n) {
+                    mma(Tl::across(gt, piece * 32, k, n, lane), p, dv[n]);
+                    mma(Tl::across(qt, piece * 32, k, n, lane), ds, dk[n]);
+                }
+            }
+        }
+        if (t + 1 < count) {
+            if (BUFFERS == 1) __syncthreads();
+            put(t + 1);
+            if (BUFFERS == 2) __syncthreads();
+        }
+    }
+    if (!some) return;
+
+    // rows that later pieces add to are left in fp32, the others are finished
+    const uint32_t place = late ? j - k0 : j - text_first;
+    const uint32_t last = (text_end - 1) / (b.late_words ? b.late_words : 1);
+    const bool joined = b.late && place < a.sinks && text_end > late_border(b, j);
+    const bool redo = not_finite(dk) | not_finite(dv);
+    float* const kept = late || joined
+        ? (late ? b.late_sums + ((size_t)block * a.kv_heads + kv_head) * a.sinks * 2 * a.width
+                : b.own_sums + ((size_t)last * a.kv_heads + kv_head) * a.sinks * 2 * a.width) + (size_t)place * 2 * a.width
+        : nullptr;
+    if (real && !redo) {
+        if (kept) {
+            store_column<float>(kept, a.width, dk, 1.f, h);
+            store_column<float>(kept + a.width, a.width, dv, 1.f, h);
+        } else {
+            store_column<T>(head_row<T>(b.dk, j, kv_head), a.width, dk, a.scale, h);
+            store_column<T>(head_row<T>(b.dv, j, kv_head), a.width, dv, 1.f, h);
+        }
+    }
+    for (uint64_t again = __ballot(redo && real && h == 0); again; again &= again - 1) {
+        const int l = __builtin_ctzll(again);
+        const uint32_t jl = __shfl(j, l, 64);
+        float ck[2] = {0.f, 0.f}, cv[2] = {0.f, 0.f};
+        key_row<T>(b, kv_head, jl, __shfl(lo, l, 64), __shfl(hi, l, 64), lane, ck, cv);
+        float* const at = (float*)__shfl((unsigned long long)kept, l, 64);
+        T *to_k = head_row<T>(b.dk, jl, kv_head), *to_v = head_row<T>(b.dv, jl, kv_head);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const uint32_t col = lane + c * WAVE;
+            if (col >= a.width) continue;
+            if (at) { at[col] = ck[c]; at[a.width + col] = cv[c]; }
+            else { to_k[col] = (T)(ck[c] * a.scale); to_v[col] = (T)cv[c]; }
+        }
+    }
+}
+
+// ---- the end: late pieces joined, the bias' gradient -----------------------------------------------------
+constexpr uint32_t END_THREADS = 1024;
+template <typename T> __global__ __launch_bounds__(END_THREADS) void end_kernel(const BackwardArgs b, uint32_t parts) {
     const AttendArgs& a = b.a;
     __shared__ float by_distance[2 * SPAN_MAX + 1];
     __shared__ uint32_t bucket[2 * SPAN_MAX + 1];
-    const uint32_t head = blockIdx.x, distances = 2 * a.span + 1;
+    const uint32_t lane = threadIdx.x % WAVE;
+    const uint32_t joins = b.late * a.kv_heads;
+    if (blockIdx.x < joins) {
+        // the piece that holds a text's last word joins that text's rows
+        const uint32_t piece = blockIdx.x / a.kv_heads, kv_head = blockIdx.x % a.kv_heads, i0 = piece * b.late_words;
+        const Text t = text_bounds(a.off, text_of(a.off, a.n_sent, i0, lane), i0, a.T);
+        if ((t.end - 1) / b.late_words != piece) return;
+        for (uint32_t at = threadIdx.x; at < a.sinks * 2 * a.width; at += END_THREADS) {
+            const uint32_t place = at / (2 * a.width), j = t.first + place;
+            if (j >= t.end || t.end <= late_border(b, j)) continue;
+            const size_t step = (size_t)a.kv_heads * a.sinks * 2 * a.width;
+            const size_t from = (size_t)kv_head * a.sinks * 2 * a.width + at;
+            float s = b.own_sums[piece * step + from];
+            for (uint32_t p = late_border(b, j) / b.late_words; p <= piece; ++p) s += b.late_sums[p * step + from];
+            const uint32_t c = at % (2 * a.width);
+            if (c < a.width) head_row<T>(b.dk, j, kv_head)[c] = (T)(s * a.scale);
+            else head_row<T>(b.dv, j, kv_head)[c - a.width] = (T)s;
+        }
+        return;
+    }
+    // a head's sums by distance over the blocks, then the distances of each bucket, both in order
+    const uint32_t head = blockIdx.x - joins, distances = 2 * a.span + 1;
     const float* from = b.by_distance + (size_t)head * parts * distances;
-    for (uint32_t c = threadIdx.x; c < distances; c += 1024) {
+    for (uint32_t c = threadIdx.x; c < distances; c += END_THREADS) {
         float s = 0.f;
         for (uint32_t p = 0; p < parts; ++p) s += from[(size_t)p * distances + c];
         by_distance[c] = s;
         bucket[c] = a.buckets[c];
     }
     __syncthreads();
-    for (uint32_t k = threadIdx.x; k < a.n_buckets; k += 1024) {
+    for (uint32_t k = threadIdx.x; k < a.n_buckets; k += END_THREADS) {
         float s = 0.f;
         for (uint32_t c = 0; c < distances; ++c) if (bucket[c] == k) s += by_distance[c];
         b.dbias[(size_t)head * a.n_buckets + k] = s;
     }
 }
 
-template <typename T> void backward_any(const BackwardArgs& b, hipStream_t st) {
+template <typename T, int DB, bool BIAS> void backward_run(const BackwardArgs& b, hipStream_t st) {
     const AttendArgs& a = b.a;
-    query_rows_kernel<T><<<attend_bias_parts(a.T) * a.heads, THREADS, 0, st>>>(b);
-    key_rows_kernel<T><<<(uint32_t)(((uint64_t)a.T * a.kv_heads + WAVES - 1) / WAVES), THREADS, 0, st>>>(b);
+    const uint32_t words = attend_bias_parts(a.T), side = BIAS ? (2 * (a.span + BIAS_SIDE) + 1) * sizeof(float) : 0;
+    query_kernel<T, DB, BIAS><<<words * a.heads, THREADS, side * (b.dbias ? 1 + 2 * THREADS / WAVE : 1), st>>>(b);
+    key_kernel<T, DB, BIAS><<<(b.late + words) * a.kv_heads, THREADS, side, st>>>(b);
+}
+template <typename T, int DB> void backward_bias(const BackwardArgs& b, hipStream_t st) {
+    if (b.a.bias) backward_run<T, DB, true>(b, st);
+    else backward_run<T, DB, false>(b, st);
+}
+template <typename T> void backward_any(const BackwardArgs& b, hipStream_t st) {
+    if (b.a.T)
+        switch ((b.a.width + 31) / 32) {
+            case 1: backward_bias<T, 1>(b, st); break;
+            case 2: backward_bias<T, 2>(b, st); break;
+            case 3: backward_bias<T, 3>(b, st); break;
+            default: backward_bias<T, 4>(b, st);
+        }
+    const uint32_t blocks = b.late * b.a.kv_heads + (b.dbias ? b.a.heads : 0);
+    if (blocks) end_kernel<T><<<blocks, END_THREADS, 0, st>>>(b, attend_bias_parts(b.a.T));
 }
 
 }  // namespace
 
 uint32_t attend_bias_parts(uint32_t T) { return (T + BLOCK_WORDS - 1) / BLOCK_WORDS; }
 
+// Pieces of at least 512 queries, at most 256 of them; none where no word outlives its window.
+LatePieces attend_late_pieces(uint32_t T, uint32_t left, uint32_t sinks) {
+    const uint32_t size = (T + 255) / 256 > 512 ? ((T + 255) / 256 + KEYS - 1) / KEYS * KEYS : 512;
+    const uint32_t reach = left > size ? left : size;
+    if (sinks == 0 || T <= BLOCK_WORDS + reach) return LatePieces{0, size, T};
+    return LatePieces{(T + size - 1) / size, size, reach};
+}
+
 void launch_attend_backward(const BackwardArgs& b, uint32_t type, hipStream_t st) {
-    if (b.a.T) {
-        if (type == ELEM_F32) backward_any<float>(b, st);
-        else if (type == ELEM_F16) backward_any<_Float16>(b, st);
-        else backward_any<__bf16>(b, st);
-    }
-    if (b.dbias) bias_buckets_kernel<<<b.a.heads, 1024, 0, st>>>(b, attend_bias_parts(b.a.T));
+    if (type == ELEM_F32) backward_any<float>(b, st);
+    else if (type == ELEM_F16) backward_any<_Float16>(b, st);
+    else backward_any<__bf16>(b, st);
 }
 
 }  // namespace w2v
