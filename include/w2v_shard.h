@@ -407,6 +407,20 @@ int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads* dout, cons
                         const uint8_t* keep_dev, const w2v_heads* dq, const w2v_heads* dk, const w2v_heads* dv,
                         float* dbias_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/* ---- one new word per text over cached keys and values -------------------------------------------------
+ * Text b has n_dev[b] words so far (at most `room`, more counts as room), whose keys and values lie in caches: element c of
+ * head h of word j of text b at p[b text_stride + j token_stride + h head_stride + c].  q and out hold the newest word's heads,
+ * token_stride leading from text to text.  out is what w2v_attend (right = 0) gives that word: over the words
+ * i - left <= j <= i and the first `sinks` ones, i = n_dev[b] - 1, whose byte keep_dev[b room + j] is not 0 (NULL: all); no
+ * words: zeros.  spec->right is not read.  workspace_dev: 256-byte aligned device memory of
+ * w2v_attend_step_workspace bytes, contents irrelevant before and after.  batch * heads <= 2^24,
+ * room <= 2^31 - 2^12. */
+typedef struct w2v_cache { const void* p; uint64_t text_stride, token_stride, head_stride; } w2v_cache;
+size_t w2v_attend_step_workspace(const w2v_attend_spec* spec, uint32_t batch, uint32_t room);
+int w2v_attend_step(const w2v_attend_spec* spec, const w2v_heads* q, const w2v_cache* k, const w2v_cache* v,
+                    const uint32_t* n_dev, uint32_t batch, uint32_t room, const uint8_t* keep_dev,
+                    const w2v_heads* out, void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* Seed of minibatch number h (the client picks a fresh seed per minibatch), a function of a master seed. */
 uint64_t w2v_minibatch_seed(uint64_t master_seed, uint64_t h);
 

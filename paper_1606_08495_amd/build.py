@@ -15,7 +15,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libw2v_shard.so")
 
 HIP_SOURCES = ["api.hip", "k_gather.hip", "k_sort.hip", "k_adjust.hip", "k_pairs.hip", "k_cbow.hip", "k_topk.hip",
-               "context.hip", "k_norm.hip", "k_attend.hip", "k_attend_back.hip"]
+               "context.hip", "k_norm.hip", "k_attend.hip", "k_attend_back.hip", "k_step.hip"]
 CPP_SOURCES = ["tables.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -83,15 +83,19 @@ __device__ inline Shown sees(const AttendArgs& a, uint32_t j, Text t) {
 // ---- bias --------------------------------------------------------------------------------------------
 // The bias of a distance, times log2 e.  Values that would leave fp32 with that factor are held at the last that do
 // not, infinities are kept; a bucket past the last adds nothing.
-__device__ inline float scaled_bias(const AttendArgs& a, uint32_t head, int32_t dist) {
-    const int32_t span = (int32_t)a.span;
+__device__ inline float scaled_bias(const float* bias, const uint32_t* buckets, uint32_t n_buckets, uint32_t reach, uint32_t head,
+                                    int32_t dist) {
+    const int32_t span = (int32_t)reach;
     const int32_t at = (dist < -span ? -span : dist > span ? span : dist) + span;
-    const uint32_t b = a.buckets[at];
-    if (b >= a.n_buckets) return 0.f;
-    const float x = a.bias[(size_t)head * a.n_buckets + b];
+    const uint32_t b = buckets[at];
+    if (b >= n_buckets) return 0.f;
+    const float x = bias[(size_t)head * n_buckets + b];
     if (!(fabsf(x) < __builtin_inff())) return x;
     const float most = 1.7e38f;
     return fminf(fmaxf(x, -most), most) * LOG2E;
+}
+__device__ inline float scaled_bias(const AttendArgs& a, uint32_t head, int32_t dist) {
+    return scaled_bias(a.bias, a.buckets, a.n_buckets, a.span, head, dist);
 }
 
 // ---- a row at a time ---------------------------------------------------------------------------------

@@ -58,4 +58,19 @@ LatePieces attend_late_pieces(uint32_t T, uint32_t left, uint32_t sinks);
 uint32_t attend_bias_parts(uint32_t T);
 void launch_attend_backward(const BackwardArgs& b, uint32_t type, hipStream_t st);
 
+// ---- one new word per text over a cache --------------------------------------------------------------
+struct Cache { const void* p; uint64_t text, token, head; };
+struct StepArgs {
+    Heads q; Cache k, v; HeadsOut o;                     // q, o: token = text
+    const uint32_t* n; uint32_t batch, room;             // words of each text, the new one last
+    uint32_t heads, kv_heads, group, width, left, sinks; bool skip_self;
+    float scale2;
+    const uint8_t* keep;                                 // [batch][room] or null
+    const float* bias; const uint32_t* buckets; uint32_t n_buckets, span;
+    uint32_t splits, per_split; float* parts;            // workspace: [batch][heads][splits][width + 2]
+};
+struct StepSplits { uint32_t splits, per_split; };
+StepSplits step_splits(uint32_t batch, uint32_t kv_heads, uint32_t room, uint32_t left, uint32_t sinks);
+void launch_step(const StepArgs& a, uint32_t type, hipStream_t st);
+
 }  // namespace w2v

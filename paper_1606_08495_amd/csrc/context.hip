@@ -266,3 +266,67 @@ extern "C" int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads*
     launch_attend_backward(b, (uint32_t)spec->type, (hipStream_t)stream);
     return launched();
 }
+
+namespace {
+
+int check_step(const w2v_attend_spec* s, uint32_t batch, uint32_t room) {
+    if (int rc = check_spec(s)) return rc;
+    if (room == 0 || room > 0x7FFFFFFFu - 4095u) return fail(W2V_ERR_ARG, "room = %u outside 1..2^31 - 2^12", room);
+    if ((uint64_t)batch * s->heads > 1u << 24) return fail(W2V_ERR_ARG, "too many texts at once");
+    return W2V_OK;
+}
+
+int check_cache(const w2v_cache* x, const w2v_attend_spec* s, uint32_t batch, uint32_t room, const char* name) {
+    if (!x || !x->p) return fail(W2V_ERR_NULL, "%s is NULL", name);
+    if (!aligned(x->p, elem_bytes(s->type))) return fail(W2V_ERR_ARG, "%s is not aligned to its elements", name);
+    if (x->text_stride >= STRIDE_MAX || x->token_stride >= STRIDE_MAX || x->head_stride >= STRIDE_MAX ||
+        x->token_stride > (1ull << 59) / room || x->text_stride > (1ull << 59) / batch)
+        return fail(W2V_ERR_ARG, "%s reaches too far", name);
+    return W2V_OK;
+}
+
+// The workspace: partial results where a cache is read by several blocks.
+size_t step_bytes(const w2v_attend_spec* s, uint32_t batch, const StepSplits& p) {
+    return p.splits > 1 ? (size_t)batch * s->heads * p.splits * (s->width + 2) * sizeof(float) : 0;
+}
+
+}  // namespace
+
+extern "C" size_t w2v_attend_step_workspace(const w2v_attend_spec* spec, uint32_t batch, uint32_t room) {
+    if (batch == 0 || check_step(spec, batch, room)) return 0;
+    return step_bytes(spec, batch, step_splits(batch, spec->kv_heads, room, spec->left, spec->sinks));
+}
+
+extern "C" int w2v_attend_step(const w2v_attend_spec* spec, const w2v_heads* q, const w2v_cache* k, const w2v_cache* v,
+                               const uint32_t* n, uint32_t batch, uint32_t room, const uint8_t* keep, const w2v_heads* out,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_spec(spec)) return rc;
+    if (batch == 0) return W2V_OK;
+    if (int rc = check_step(spec, batch, room)) return rc;
+    if (int rc = check_heads(q, spec, spec->heads, batch, false, "q")) return rc;
+    if (int rc = check_cache(k, spec, batch, room, "k")) return rc;
+    if (int rc = check_cache(v, spec, batch, room, "v")) return rc;
+    if (int rc = check_heads(out, spec, spec->heads, batch, true, "out")) return rc;
+    if (!n) return fail(W2V_ERR_NULL, "n_dev is NULL");
+    const StepSplits p = step_splits(batch, spec->kv_heads, room, spec->left, spec->sinks);
+    const size_t need = step_bytes(spec, batch, p);
+    if (need) {
+        if (!workspace) return fail(W2V_ERR_NULL, "workspace is NULL");
+        if (!aligned(workspace, 256)) return fail(W2V_ERR_ARG, "workspace must be 256-byte aligned");
+        if (workspace_bytes < need)
+            return fail(W2V_ERR_ARG, "workspace of %zu bytes is too small: %zu are needed", workspace_bytes, need);
+    }
+    StepArgs a;
+    a.q = heads_of(q); a.o = heads_out(out);
+    a.k = Cache{k->p, k->text_stride, k->token_stride, k->head_stride};
+    a.v = Cache{v->p, v->text_stride, v->token_stride, v->head_stride};
+    a.n = n; a.batch = batch; a.room = room;
+    a.heads = spec->heads; a.kv_heads = spec->kv_heads; a.group = spec->heads / spec->kv_heads; a.width = spec->width;
+    a.left = spec->left; a.sinks = spec->sinks; a.skip_self = spec->skip_self != 0;
+    a.scale2 = spec->scale * 1.4426950408889634f;
+    a.keep = keep;
+    a.bias = spec->bias_dev; a.buckets = spec->bucket_dev; a.n_buckets = spec->n_buckets; a.span = spec->span;
+    a.splits = p.splits; a.per_split = p.per_split; a.parts = (float*)workspace;
+    launch_step(a, (uint32_t)spec->type, (hipStream_t)stream);
+    return launched();
+}

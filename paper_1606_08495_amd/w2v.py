@@ -77,6 +77,9 @@ _SIGNATURES = {
     "w2v_attend_backward_workspace": (ctypes.c_size_t, [c_vp, c_u32]),
     "w2v_attend_backward": (ctypes.c_int, [c_vp] * 6 + [c_vp, c_vp, c_u32, c_u32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
                                                         ctypes.c_size_t, c_vp]),
+    "w2v_attend_step_workspace": (ctypes.c_size_t, [c_vp, c_u32, c_u32]),
+    "w2v_attend_step": (ctypes.c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_u32, c_u32, c_vp, c_vp, c_vp, ctypes.c_size_t,
+                                       c_vp]),
     "w2v_minibatch_seed": (c_u64, [c_u64, c_u64]),
     "w2v_shard_timing_enable": (ctypes.c_int, [c_vp, ctypes.c_int]),
     "w2v_shard_timing_read": (ctypes.c_int, [c_vp, c_vp, c_vp]),
@@ -471,6 +474,11 @@ class Heads(ctypes.Structure):
     _fields_ = [("p", c_vp), ("token_stride", c_u64), ("head_stride", c_u64)]
 
 
+class Cache(ctypes.Structure):
+    """w2v_cache: element c of head h of word j of text b at p[b text_stride + j token_stride + h head_stride + c]."""
+    _fields_ = [("p", c_vp), ("text_stride", c_u64), ("token_stride", c_u64), ("head_stride", c_u64)]
+
+
 class AttendSpec(ctypes.Structure):
     """w2v_attend_spec."""
     _fields_ = [("type", ctypes.c_int32), ("heads", c_u32), ("kv_heads", c_u32), ("width", c_u32), ("left", c_u32),
@@ -569,3 +577,41 @@ def attend_backward(dout, q, k, v, out, lse, sent_off, left=None, right=None, si
             r(_heads(dq, q, T, H, "dq")), r(_heads(dk, q, T, G, "dk")), r(_heads(dv, q, T, G, "dv")),
             _dev(dbias, torch.float32, "dbias"), workspace.data_ptr(), workspace.numel(), st.cuda_stream))
     return dq, dk, dv, dbias
+
+
+def _cache(t, like, shape, name):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == like.dtype and t.device == like.device and
+            t.shape == shape):
+        raise TypeError("%s must be a CUDA tensor %s of %s" % (name, list(shape), like.dtype))
+    s = t.stride()
+    if (s[3] != 1 and shape[3] > 1) or min(s) < 0:
+        raise ValueError("%s: the elements of a head must lie side by side" % name)
+    return Cache(t.data_ptr(), s[0], s[1], s[2])
+
+
+def attend_step(q, k, v, n, left=None, sinks=0, skip_self=False, scale=None, keep=None, bias=None, buckets=None, out=None,
+                workspace=None, stream=None):
+    """out [texts, heads, width] of w2v_attend_step: the newest word's q [texts, heads, width] over the caches k and
+    v [texts, room, kv_heads, width], of which text b has filled n[b] (int32, the newest word's among them).  keep: uint8
+    [texts, room].  ``workspace``: optional uint8 device tensor to reuse.  Other arguments as for ``attend``."""
+    if q.dim() != 3 or k.dim() != 4:
+        raise TypeError("q must be [texts, heads, width], k and v [texts, room, heads, width]")
+    B, H, d = q.shape
+    room, G = k.shape[1], k.shape[2]
+    if n.shape != (B,) or n.device != q.device or (keep is not None and (keep.shape != (B, room) or keep.device != q.device)):
+        raise ValueError("n must be [texts] and keep [texts, room] on the device of q")
+    with _on(stream, q):
+        st = torch.cuda.current_stream(q.device)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        spec = _spec(q, G, left, 0, sinks, skip_self, scale, bias, buckets)
+        r = ctypes.byref
+        if workspace is None:
+            need = int(lib().w2v_attend_step_workspace(r(spec), B, room))
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        shape = torch.Size((B, room, G, d))
+        _check(lib().w2v_attend_step(r(spec), r(_heads(q, q, B, H, "q")), r(_cache(k, q, shape, "k")),
+                                     r(_cache(v, q, shape, "v")), _dev(n, IDX, "n"), B, room, _dev(keep, torch.uint8, "keep"),
+                                     r(_heads(out, q, B, H, "out")), workspace.data_ptr(), workspace.numel(),
+                                     st.cuda_stream))
+    return out
