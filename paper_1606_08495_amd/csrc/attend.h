@@ -23,19 +23,27 @@ template <typename T> __device__ inline T* head_row(const HeadsOut& x, uint32_t 
 }
 
 // ---- texts ------------------------------------------------------------------------------------------
-// The last text that starts at or before token i, found by the whole wavefront: 64 offsets at a time.  Whatever the
-// offsets hold, the result is below n_sent and the search ends.
-__device__ inline uint32_t text_of(const uint64_t* off, uint32_t n_sent, uint32_t i, uint32_t lane) {
+// The last text that starts at or before a token, for four tokens at a time: lanes 16 g .. 16 g + 15 look for their token i
+// together, 64 offsets a round, and all end with its text.  Whatever the offsets hold, the result is below n_sent and the search
+// ends.
+__device__ inline uint32_t texts_of(const uint64_t* off, uint32_t n_sent, uint32_t i, uint32_t lane) {
     uint32_t lo = 0, hi = n_sent;
-    while (hi - lo > 1) {
-        const uint32_t step = (hi - lo + WAVE - 1) / WAVE;
-        const uint32_t at = lo + (lane + 1) * step;              // n_sent < 2^31: no overflow
-        const uint64_t before = __ballot(at < hi && off[at < hi ? at : lo] <= (uint64_t)i);
-        const uint32_t c = ~before ? (uint32_t)__builtin_ctzll(~before) : WAVE;
+    while (__any(hi - lo > 1)) {
+        const uint32_t step = (hi - lo + 63) / 64;
+        uint32_t c = 0;
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t at = lo + (lane % 16 * 4 + u + 1) * step;       // n_sent < 2^31: no overflow
+            const uint64_t before = __ballot(at < hi && off[at < hi ? at : lo] <= (uint64_t)i);
+            c += __popc((uint32_t)(before >> (lane / 16 * 16)) & 0xFFFFu);
+        }
         lo += c * step;
         hi = hi - lo < step ? hi : lo + step;
     }
     return lo;
+}
+__device__ inline uint32_t text_of(const uint64_t* off, uint32_t n_sent, uint32_t i, uint32_t lane) {
+    return __builtin_amdgcn_readfirstlane(texts_of(off, n_sent, i, lane));
 }
 
 // Tokens [first, end) of the text of token i, always first <= i < end <= T.
@@ -48,9 +56,25 @@ __device__ inline Text text_bounds(const uint64_t* off, uint32_t text, uint32_t 
     if (t.end <= i) t.end = i + 1;
     return t;
 }
-// The same for the tokens of a wavefront's lanes, which lie between those of texts s0 and s1.
-__device__ inline Text text_between(const uint64_t* off, uint32_t s0, uint32_t s1, uint32_t i, uint32_t T) {
-    uint32_t lo = s0, hi = s1 + 1;
+// The same for the tokens of a wavefront's lanes, which lie between those of texts s0 and s1 (the same in all lanes).
+__device__ inline Text text_between(const uint64_t* off, uint32_t s0, uint32_t s1, uint32_t i, uint32_t T, uint32_t lane) {
+    Text t;
+    if (s1 - s0 < 63) {                               // their offsets side by side in the lanes
+        const uint64_t mine = off[lane <= s1 - s0 ? s0 + lane : s1 + 1];
+        const uint32_t o = mine < (uint64_t)T ? (uint32_t)mine : T;
+        uint32_t at = 0;
+#pragma unroll
+        for (uint32_t b = 32; b; b /= 2) {
+            const uint32_t there = (uint32_t)__shfl((int)o, (int)((at + b) & 63), 64);
+            if (at + b <= s1 - s0 && there <= i) at += b;
+        }
+        t.first = (uint32_t)__shfl((int)o, (int)at, 64);
+        t.end = (uint32_t)__shfl((int)o, (int)at + 1, 64);
+        t.first = t.first < i ? t.first : i;
+        if (t.end <= i) t.end = i + 1;
+        return t;
+    }
+    uint32_t lo = s0, hi = s1 + 1;                    // many texts without a word
     while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
         if (off[mid] <= (uint64_t)i) lo = mid; else hi = mid;

@@ -7,17 +7,30 @@ namespace w2v {
 
 constexpr int BLOCK_WORDS = 128, WAVE_WORDS = 32, KEYS = 64, THREADS = 256;
 
+// The texts of a block's first and last token and of a wavefront's.
+struct Texts {
+    uint32_t block_first, block_last, wave_first, wave_last;
+    __device__ Texts(const AttendArgs& a, uint32_t b0, uint32_t b1, uint32_t w0, uint32_t w1, uint32_t lane) {
+        const uint32_t s = texts_of(a.off, a.n_sent, lane < 32 ? (lane < 16 ? b0 : b1) : (lane < 48 ? w0 : w1), lane);
+        block_first = __builtin_amdgcn_readlane(s, 0);
+        block_last = __builtin_amdgcn_readlane(s, 16);
+        wave_first = __builtin_amdgcn_readlane(s, 32);
+        wave_last = __builtin_amdgcn_readlane(s, 48);
+    }
+};
+
 // A word and what it is shown, for the lanes of a wavefront; and over the wavefront's words, in scalar registers.
+// (A wavefront past the last token takes that token, without weight.)
 struct Words {
     uint32_t i; Shown s;
     uint32_t lo_least, lo_most, hi_least, hi_most, i_first, i_last, first_least, sunk_least;
     __device__ Words(const AttendArgs& a, uint32_t first, uint32_t lane) {
-        const uint32_t last = first + WAVE_WORDS - 1 < a.T ? first + WAVE_WORDS - 1 : a.T - 1;
-        i = first + lane % WAVE_WORDS < last ? first + lane % WAVE_WORDS : last;
-        i_first = first < last ? first : last;
-        i_last = last;
-        const uint32_t s0 = text_of(a.off, a.n_sent, i_first, lane), s1 = text_of(a.off, a.n_sent, i_last, lane);
-        s = shown_to(a, i, text_between(a.off, s0, s1, i, a.T));
+        i_first = first < a.T ? first : a.T - 1;
+        i_last = first + WAVE_WORDS - 1 < a.T ? first + WAVE_WORDS - 1 : a.T - 1;
+        i = first + lane % WAVE_WORDS < i_last ? first + lane % WAVE_WORDS : i_last;
+    }
+    __device__ void find(const AttendArgs& a, const Texts& t, uint32_t lane) {
+        s = shown_to(a, i, text_between(a.off, t.wave_first, t.wave_last, i, a.T, lane));
         lo_least = __builtin_amdgcn_readfirstlane(s.lo);
         hi_least = __builtin_amdgcn_readfirstlane(s.hi);
         first_least = __builtin_amdgcn_readfirstlane(s.first);
@@ -35,9 +48,8 @@ struct Words {
 // The axis of keys of a block: `sunk` words from `first` on, then those from `lo` to the end.
 struct Axis {
     uint32_t first, sunk, shift, count;
-    __device__ Axis(const AttendArgs& a, uint32_t word0, uint32_t lane) {
-        const uint32_t last = word0 + BLOCK_WORDS - 1 < a.T ? word0 + BLOCK_WORDS - 1 : a.T - 1;
-        const uint32_t s0 = text_of(a.off, a.n_sent, word0, lane), s1 = text_of(a.off, a.n_sent, last, lane);
+    __device__ Axis(const AttendArgs& a, uint32_t word0, uint32_t last, const Texts& t) {
+        const uint32_t s0 = t.block_first, s1 = t.block_last;
         const Shown from = shown_to(a, word0, text_bounds(a.off, s0, word0, a.T));
         const Shown to = shown_to(a, last, text_bounds(a.off, s1, last, a.T));
         first = from.first;

@@ -31,15 +31,17 @@ __global__ __launch_bounds__(THREADS) void attend_kernel(const AttendArgs a) {
     const uint32_t head = blockIdx.x % a.heads, kv_head = head / a.group;
     const uint32_t words = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS;
     const uint32_t word0 = (words - 1 - blockIdx.x / a.heads) * BLOCK_WORDS;      // those that may see most first
-    const Axis x(a, word0, lane);
-    const uint32_t first = word0 + wave * WAVE_WORDS;
-    const Words w(a, first < a.T ? first : a.T - 1, lane);
+    const uint32_t first = word0 + wave * WAVE_WORDS, last = word0 + BLOCK_WORDS - 1 < a.T ? word0 + BLOCK_WORDS - 1 : a.T - 1;
+    Words w(a, first, lane);
     const bool some = first < a.T;                    // the block's last wavefronts may have no word
-    if (BIAS) fill_bias(a, head, table);
 
     typename Frag<T>::vec q[2 * DB];
 #pragma unroll
     for (int s = 0; s < 2 * DB; ++s) q[s] = load_operand(head_row<T>(a.q, w.i, head), s, h, a.width);
+    const Texts texts(a, word0, last, w.i_first, w.i_last, lane);
+    const Axis x(a, word0, last, texts);
+    w.find(a, texts, lane);
+    if (BIAS) fill_bias(a, head, table);
     Acc o[DB];
 #pragma unroll
     for (int b = 0; b < DB; ++b) o[b] = Acc{};
@@ -52,8 +54,7 @@ __global__ __launch_bounds__(THREADS) void attend_kernel(const AttendArgs a) {
         const auto row = [&](const Heads& p, uint32_t r) -> const T* {
             const uint32_t n = t * KEYS + r;
             if (n >= x.count) return nullptr;
-            const uint32_t j = x.token(n);
-            return a.keep && !a.keep[j] ? nullptr : head_row<T>(p, j, kv_head);
+            return head_row<T>(p, x.token(n), kv_head);
         };
         tk.load([&](uint32_t r) { return row(a.k, r); }, a.width);
         tv.load([&](uint32_t r) { return row(a.v, r); }, a.width);

@@ -60,9 +60,8 @@ __global__ __launch_bounds__(THREADS) void query_kernel(const BackwardArgs b) {
     const uint32_t part = words - 1 - blockIdx.x / a.heads, word0 = part * BLOCK_WORDS;
     float* const table = dynamic;
     float* const sums = dynamic + (2 * wave + 1 + h) * (2 * reach + 1);
-    const Axis x(a, word0, lane);
-    const uint32_t first = word0 + wave * WAVE_WORDS;
-    const Words w(a, first < a.T ? first : a.T - 1, lane);
+    const uint32_t first = word0 + wave * WAVE_WORDS, last = word0 + BLOCK_WORDS - 1 < a.T ? word0 + BLOCK_WORDS - 1 : a.T - 1;
+    Words w(a, first, lane);
     const bool some = first < a.T, real = first + lane % WAVE_WORDS < a.T;
     if (BIAS) {
         fill_bias(a, head, table);
@@ -86,6 +85,9 @@ __global__ __launch_bounds__(THREADS) void query_kernel(const BackwardArgs b) {
     float lse2 = a.lse[(size_t)head * a.T + w.i];
     if (real && h == 0) b.delta[(size_t)head * a.T + w.i] = delta;
     lse2 = lse2 == -__builtin_inff() ? 0.f : lse2 * LOG2E;      // of a word that is shown nothing: every score is masked
+    const Texts texts(a, word0, last, w.i_first, w.i_last, lane);
+    const Axis x(a, word0, last, texts);
+    w.find(a, texts, lane);
     Acc dq[DB];
 #pragma unroll
     for (int n = 0; n < DB; ++n) dq[n] = Acc{};
@@ -98,8 +100,7 @@ __global__ __launch_bounds__(THREADS) void query_kernel(const BackwardArgs b) {
         const auto row = [&](const Heads& p, uint32_t r) -> const T* {
             const uint32_t n = t * KEYS + r;
             if (n >= x.count) return nullptr;
-            const uint32_t j = x.token(n);
-            return a.keep && !a.keep[j] ? nullptr : head_row<T>(p, j, kv_head);
+            return head_row<T>(p, x.token(n), kv_head);
         };
         tk.load([&](uint32_t r) { return row(a.k, r); }, a.width);
         tv.load([&](uint32_t r) { return row(a.v, r); }, a.width);
@@ -240,42 +241,43 @@ __global__ __launch_bounds__(THREADS) void key_kernel(const BackwardArgs b) {
     } else {
         k0 = (block - b.late) * BLOCK_WORDS;
         k1 = k0 + BLOCK_WORDS < a.T ? k0 + BLOCK_WORDS : a.T;
-        const uint32_t s0 = text_of(a.off, a.n_sent, k0, lane), s1 = text_of(a.off, a.n_sent, k1 - 1, lane);
-        q0 = sees(a, k0, text_bounds(a.off, s0, k0, a.T)).lo;
-        const Text t = text_bounds(a.off, s1, k1 - 1, a.T);
-        q1 = sees(a, k1 - 1, t).hi;
-        if (a.sinks && t.first + a.sinks > k0) {
-            const uint32_t border = late_border(b, k0), to = t.end < border ? t.end : border;
-            q1 = q1 < to ? to : q1;
-        }
     }
     k0 = __builtin_amdgcn_readfirstlane(k0);
     k1 = __builtin_amdgcn_readfirstlane(k1);
-    q0 = __builtin_amdgcn_readfirstlane(q0);
-    q1 = __builtin_amdgcn_readfirstlane(q1);
     const uint32_t wave0 = k0 + wave * WAVE_WORDS;
     const bool some = wave0 < k1, real = wave0 + lane % WAVE_WORDS < k1;
+    const uint32_t j_first = some ? wave0 : k1 - 1, j_last = wave0 + WAVE_WORDS - 1 < k1 ? wave0 + WAVE_WORDS - 1 : k1 - 1;
     const uint32_t j = real ? wave0 + lane % WAVE_WORDS : k1 - 1;
-    uint32_t lo = 0, hi = 0, text_first, text_end;
-    {
-        const uint32_t j0 = some ? wave0 : k1 - 1, j1 = wave0 + WAVE_WORDS - 1 < k1 ? wave0 + WAVE_WORDS - 1 : k1 - 1;
-        const Text t = text_between(a.off, text_of(a.off, a.n_sent, j0, lane), text_of(a.off, a.n_sent, j1, lane), j, a.T);
-        text_first = t.first;
-        text_end = t.end;
-        const uint32_t border = late_border(b, j);
-        if (real && !(a.keep && !a.keep[j])) {
-            if (late) {
-                lo = border > q0 ? border : q0;
-                hi = q1;
-            } else {
-                const Shown s = sees(a, j, t);
-                lo = s.lo;
-                hi = s.sunk < border ? s.sunk : border;
-                hi = hi < s.hi ? s.hi : hi;
-            }
-            if (lo >= hi) lo = hi = 0;
-        }
+    typename Frag<T>::vec kf[2 * DB], vf[2 * DB];
+#pragma unroll
+    for (int s = 0; s < 2 * DB; ++s) {
+        kf[s] = load_operand(head_row<T>(a.k, j, kv_head), s, h, a.width);
+        vf[s] = load_operand(head_row<T>(a.v, j, kv_head), s, h, a.width);
     }
+    const bool keep = !(a.keep && !a.keep[j]);
+    const Texts texts(a, k0, k1 - 1, j_first, j_last, lane);
+    const Text text = text_between(a.off, texts.wave_first, texts.wave_last, j, a.T, lane);
+    uint32_t lo = 0, hi = 0;
+    const uint32_t border = late_border(b, j);
+    if (late) {
+        lo = border > q0 ? border : q0;
+        hi = q1;
+    } else {
+        q0 = sees(a, k0, text_bounds(a.off, texts.block_first, k0, a.T)).lo;
+        const Text t = text_bounds(a.off, texts.block_last, k1 - 1, a.T);
+        q1 = sees(a, k1 - 1, t).hi;
+        if (a.sinks && t.first + a.sinks > k0) {
+            const uint32_t last = late_border(b, k0), to = t.end < last ? t.end : last;
+            q1 = q1 < to ? to : q1;
+        }
+        const Shown s = sees(a, j, text);
+        lo = s.lo;
+        hi = s.sunk < border ? s.sunk : border;
+        hi = hi < s.hi ? s.hi : hi;
+    }
+    q0 = __builtin_amdgcn_readfirstlane(q0);
+    q1 = __builtin_amdgcn_readfirstlane(q1);
+    if (!real || !keep || lo >= hi) lo = hi = 0;
     uint32_t lo_least = lo < hi ? lo : ~0u, lo_most = lo_least, hi_most = hi, hi_least = hi;
 #pragma unroll
     for (int m = 1; m < 32; m *= 2) {
@@ -288,14 +290,6 @@ __global__ __launch_bounds__(THREADS) void key_kernel(const BackwardArgs b) {
     lo_most = __builtin_amdgcn_readfirstlane(lo_most);
     hi_least = __builtin_amdgcn_readfirstlane(hi_least);
     hi_most = __builtin_amdgcn_readfirstlane(hi_most);
-    const uint32_t j_first = some ? wave0 : k1 - 1, j_last = wave0 + WAVE_WORDS - 1 < k1 ? wave0 + WAVE_WORDS - 1 : k1 - 1;
-
-    typename Frag<T>::vec kf[2 * DB], vf[2 * DB];
-#pragma unroll
-    for (int s = 0; s < 2 * DB; ++s) {
-        kf[s] = load_operand(head_row<T>(a.k, j, kv_head), s, h, a.width);
-        vf[s] = load_operand(head_row<T>(a.v, j, kv_head), s, h, a.width);
-    }
     Acc dk[DB], dv[DB];
 #pragma unroll
     for (int n = 0; n < DB; ++n) dk[n] = dv[n] = Acc{};
@@ -391,9 +385,9 @@ __global__ __launch_bounds__(THREADS) void key_kernel(const BackwardArgs b) {
     if (!some) return;
 
     // rows that later pieces add to are left in fp32, the others are finished
-    const uint32_t place = late ? j - k0 : j - text_first;
-    const uint32_t last = (text_end - 1) / (b.late_words ? b.late_words : 1);
-    const bool joined = b.late && place < a.sinks && text_end > late_border(b, j);
+    const uint32_t place = late ? j - k0 : j - text.first;
+    const uint32_t last = (text.end - 1) / (b.late_words ? b.late_words : 1);
+    const bool joined = b.late && place < a.sinks && text.end > border;
     const bool redo = not_finite(dk) | not_finite(dv);
     float* const kept = late || joined
         ? (late ? b.late_sums + ((size_t)block * a.kv_heads + kv_head) * a.sinks * 2 * a.width

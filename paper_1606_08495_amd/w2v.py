@@ -4,6 +4,7 @@ Argument marshalling only: every step of the shard path runs in the library's HI
 PyTorch supplies device memory (``tensor.data_ptr()``) and the stream.  There is no fallback: if
 the library has not been built, or a call fails, an exception is raised.
 """
+import contextlib
 import ctypes
 import os
 
@@ -410,19 +411,26 @@ def topk_cosine(queries, cands, K, tau=-2.0, round_candidates=32768, workspace=N
 TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
+_AS_IT_IS = contextlib.nullcontext()
+
+
 def _on(stream, t):
     """What is allocated for a call belongs to the stream the call runs on, and to the tensor's device."""
-    return torch.cuda.stream(torch.cuda.current_stream(t.device) if stream is None else stream)
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    return _AS_IT_IS if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
 
 
 def _rows(t, like, name):
     """A matrix of rows that lie anywhere, their elements side by side: (pointer, elements from row to row)."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in TYPES and t.dim() == 2 and
-            (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= 0)):
-        raise TypeError("%s must be a CUDA matrix of float32, float16 or bfloat16 with dense rows" % name)
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in TYPES and t.dim() == 2):
+        raise TypeError("%s must be a CUDA matrix of float32, float16 or bfloat16" % name)
     if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
         raise ValueError("%s differs in shape, type or device" % name)
-    return t.data_ptr(), max(t.stride(0), 0) if t.shape[0] > 1 else t.shape[1]
+    (m, d), (a, b) = t.shape, t.stride()
+    if b != 1 and d > 1 and m > 0:
+        raise ValueError("%s: the elements of a row must lie side by side" % name)
+    return t.data_ptr(), a if m > 1 else d
 
 
 def _vec(t, n, device, name):
@@ -437,8 +445,8 @@ def layer_norm(x, gain=None, offset=None, eps=1e-5, out=None, stream=None):
     """(y, mean, rstd) of w2v_layer_norm for the rows of x [m, d]; gain and offset are float32 [d]."""
     xp, xs = _rows(x, None, "x")
     m, d = x.shape
-    with _on(stream, x) as _:
-        st = torch.cuda.current_stream(x.device)
+    with _on(stream, x):
+        st = torch.cuda.current_stream()
         y = torch.empty((m, d), dtype=x.dtype, device=x.device) if out is None else out
         stats = torch.empty((2, m), dtype=torch.float32, device=x.device)
         yp, ys = _rows(y, x, "out")
@@ -454,8 +462,8 @@ def layer_norm_backward(dy, x, gain, mean, rstd, out=None, workspace=None, strea
     xp, xs = _rows(x, None, "x")
     gp, gs = _rows(dy, x, "dy")
     m, d = x.shape
-    with _on(stream, x) as _:
-        st = torch.cuda.current_stream(x.device)
+    with _on(stream, x):
+        st = torch.cuda.current_stream()
         dx = torch.empty((m, d), dtype=x.dtype, device=x.device) if out is None else out
         columns = torch.empty((2, d), dtype=torch.float32, device=x.device)
         if workspace is None:
@@ -538,7 +546,7 @@ def attend(q, k, v, sent_off, left=None, right=None, sinks=0, skip_self=False, s
     T, H, _ = q.shape
     G = k.shape[1]
     with _on(stream, q):
-        st = torch.cuda.current_stream(q.device)
+        st = torch.cuda.current_stream()
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
@@ -561,7 +569,7 @@ def attend_backward(dout, q, k, v, out, lse, sent_off, left=None, right=None, si
     if lse.shape != (H, T) or lse.device != q.device:
         raise ValueError("lse must be [heads, tokens]")
     with _on(stream, q):
-        st = torch.cuda.current_stream(q.device)
+        st = torch.cuda.current_stream()
         dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         dk, dv = [torch.empty(k.shape, dtype=q.dtype, device=q.device) for _ in range(2)]
         dbias = None if bias is None else torch.empty(bias.shape, dtype=torch.float32, device=q.device)
@@ -601,7 +609,7 @@ def attend_step(q, k, v, n, left=None, sinks=0, skip_self=False, scale=None, kee
     if n.shape != (B,) or n.device != q.device or (keep is not None and (keep.shape != (B, room) or keep.device != q.device)):
         raise ValueError("n must be [texts] and keep [texts, room] on the device of q")
     with _on(stream, q):
-        st = torch.cuda.current_stream(q.device)
+        st = torch.cuda.current_stream()
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         spec = _spec(q, G, left, 0, sinks, skip_self, scale, bias, buckets)
