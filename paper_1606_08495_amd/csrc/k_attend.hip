@@ -22,7 +22,7 @@ namespace {
 constexpr float RISE = 8.f;           // how far (to base two) a maximum may rise before outputs are rescaled
 
 template <typename T, int DB, bool BIAS>
-__global__ __launch_bounds__(THREADS) void attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) {
     typedef Tile<T, DB, KEYS> Tl;
     constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 128 * 1024 ? 2 : 1;
     __shared__ __align__(16) char tiles[BUFFERS][2][Tl::BYTES];

@@ -47,7 +47,7 @@ template <int DB> __device__ inline bool not_finite(const Acc (&c)[DB]) {
 // Sums of dS by distance: an array in LDS for each half of each wavefront, in which the 32 lanes of one register's row
 // lie side by side, so that no two lanes add to one place at a time; outermost distances by registers.
 template <typename T, int DB, bool BIAS>
-__global__ __launch_bounds__(THREADS) void query_kernel(const BackwardArgs b) {
+__global__ __launch_bounds__(THREADS, 2) void query_kernel(const BackwardArgs b) {
     const AttendArgs& a = b.a;
     typedef Tile<T, DB, KEYS> Tl;
     constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 64 * 1024 ? 2 : 1;
@@ -217,7 +217,7 @@ __device__ inline uint32_t late_border(const BackwardArgs& b, uint32_t j) {
 }
 
 template <typename T, int DB, bool BIAS>
-__global__ __launch_bounds__(THREADS) void key_kernel(const BackwardArgs b) {
+__global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const BackwardArgs b) {
     const AttendArgs& a = b.a;
     typedef Tile<T, DB, KEYS> Tl;
     constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 64 * 1024 ? 2 : 1;
