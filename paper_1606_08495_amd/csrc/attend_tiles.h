@@ -10,7 +10,7 @@ constexpr int BLOCK_WORDS = 128, WAVE_WORDS = 32, KEYS = 64, THREADS = 256;
 // The texts of a block's first and last token and of a wavefront's.
 struct Texts {
     uint32_t block_first, block_last, wave_first, wave_last;
-    __device__ Texts(const AttendArgs& a, uint32_t b0, uint32_t b1, uint32_t w0, uint32_t w1, uint32_t lane) {
+    __device__ __forceinline__ Texts(const AttendArgs& a, uint32_t b0, uint32_t b1, uint32_t w0, uint32_t w1, uint32_t lane) {
         const uint32_t s = texts_of(a.off, a.n_sent, lane < 32 ? (lane < 16 ? b0 : b1) : (lane < 48 ? w0 : w1), lane);
         block_first = __builtin_amdgcn_readlane(s, 0);
         block_last = __builtin_amdgcn_readlane(s, 16);
@@ -24,12 +24,12 @@ struct Texts {
 struct Words {
     uint32_t i; Shown s;
     uint32_t lo_least, lo_most, hi_least, hi_most, i_first, i_last, first_least, sunk_least;
-    __device__ Words(const AttendArgs& a, uint32_t first, uint32_t lane) {
+    __device__ __forceinline__ Words(const AttendArgs& a, uint32_t first, uint32_t lane) {
         i_first = first < a.T ? first : a.T - 1;
         i_last = first + WAVE_WORDS - 1 < a.T ? first + WAVE_WORDS - 1 : a.T - 1;
         i = first + lane % WAVE_WORDS < i_last ? first + lane % WAVE_WORDS : i_last;
     }
-    __device__ void find(const AttendArgs& a, const Texts& t, uint32_t lane) {
+    __device__ __forceinline__ void find(const AttendArgs& a, const Texts& t, uint32_t lane) {
         s = shown_to(a, i, text_between(a.off, t.wave_first, t.wave_last, i, a.T, lane));
         lo_least = __builtin_amdgcn_readfirstlane(s.lo);
         hi_least = __builtin_amdgcn_readfirstlane(s.hi);
@@ -40,7 +40,7 @@ struct Words {
     }
     // Whether any of the words is shown any of the tokens j0 .. j0 + 31.  (First words that stay visible lie before all
     // windows only for the first word's text: later texts begin at or after the first word.)
-    __device__ bool shown_any(uint32_t j0) const {
+    __device__ __forceinline__ bool shown_any(uint32_t j0) const {
         return j0 < hi_most && (j0 + 32 > lo_least || (j0 < sunk_least && j0 + 32 > first_least));
     }
 };
@@ -48,7 +48,7 @@ struct Words {
 // The axis of keys of a block: `sunk` words from `first` on, then those from `lo` to the end.
 struct Axis {
     uint32_t first, sunk, shift, count;
-    __device__ Axis(const AttendArgs& a, uint32_t word0, uint32_t last, const Texts& t) {
+    __device__ __forceinline__ Axis(const AttendArgs& a, uint32_t word0, uint32_t last, const Texts& t) {
         const uint32_t s0 = t.block_first, s1 = t.block_last;
         const Shown from = shown_to(a, word0, text_bounds(a.off, s0, word0, a.T));
         const Shown to = shown_to(a, last, text_bounds(a.off, s1, last, a.T));
@@ -61,20 +61,21 @@ struct Axis {
         shift = __builtin_amdgcn_readfirstlane(shift);
         count = __builtin_amdgcn_readfirstlane(count);
     }
-    __device__ uint32_t token(uint32_t n) const { return n < sunk ? first + n : shift + n; }
+    __device__ __forceinline__ uint32_t token(uint32_t n) const { return n < sunk ? first + n : shift + n; }
 };
 
 // Bias by distance, times log2 e, with the outermost values repeated on both sides so that every distance within a
 // 32 x 32 piece that is not wholly past the span is in the table.
 constexpr int BIAS_SIDE = 64, BIAS_TABLE = 2 * SPAN_MAX + 1 + 2 * BIAS_SIDE;
-__device__ inline void fill_bias(const AttendArgs& a, uint32_t head, float* table) {
+__device__ __forceinline__ void fill_bias(const AttendArgs& a, uint32_t head, float* table) {
     const int32_t reach = (int32_t)a.span + BIAS_SIDE;
     for (int32_t at = threadIdx.x; at <= 2 * reach; at += THREADS) table[at] = scaled_bias(a, head, at - reach);
 }
 
-// Scores of a piece of 32 keys, with bias and mask: s on the way in holds the products.
+// Scores of a piece of 32 keys, masked: s on the way in holds the products.  With a bias they are to base two, without one
+// they still lack the scale, which is positive.
 template <bool BIAS>
-__device__ inline void piece_scores(const AttendArgs& a, const Words& w, const Axis& x, uint32_t n0, uint64_t kept, bool linear,
+__device__ __forceinline__ void piece_scores(const AttendArgs& a, const Words& w, const Axis& x, uint32_t n0, uint64_t kept, bool linear,
                                     const float* table, uint32_t h, Acc& s) {
     const uint32_t j0 = n0 + x.shift;                 // of the piece's first key where the axis is linear
     const uint32_t kept32 = (uint32_t)kept;
@@ -101,9 +102,6 @@ __device__ inline void piece_scores(const AttendArgs& a, const Words& w, const A
                 s[r] = fmaf(s[r], a.scale2, table[(dist < -reach ? -reach : dist > reach ? reach : dist) + reach]);
             }
         }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= a.scale2;
     }
     if (all) return;
 #pragma unroll
@@ -115,5 +113,27 @@ __device__ inline void piece_scores(const AttendArgs& a, const Words& w, const A
         s[r] = in ? s[r] : -__builtin_inff();
     }
 }
+
+// Keys and values of a block, tile by tile from memory to LDS, and which of the next tile's words are kept.
+template <typename T, int DB> struct KeyTiles {
+    Transit<T, DB, KEYS, THREADS> k, v;
+    uint8_t keep;
+    __device__ __forceinline__ void start(const AttendArgs& a, uint32_t kv_head, const Axis& x) {
+        k.start(a.k, kv_head, (int64_t)(int32_t)x.shift, a.width);
+        v.start(a.v, kv_head, (int64_t)(int32_t)x.shift, a.width);
+        keep = 1;
+    }
+    __device__ __forceinline__ void fetch(const AttendArgs& a, uint32_t kv_head, const Axis& x, uint32_t t, uint32_t lane) {
+        const uint32_t rows = x.count - t * KEYS;
+        if (t * KEYS >= x.sunk) {
+            k.load(rows, a.width);
+            v.load(rows, a.width);
+        } else {
+            k.load_rows([&](uint32_t r) { return head_row<T>(a.k, x.token(t * KEYS + r), kv_head); }, rows, a.width);
+            v.load_rows([&](uint32_t r) { return head_row<T>(a.v, x.token(t * KEYS + r), kv_head); }, rows, a.width);
+        }
+        if (a.keep) keep = lane < rows ? a.keep[x.token(t * KEYS + lane)] : 0;
+    }
+};
 
 }  // namespace w2v

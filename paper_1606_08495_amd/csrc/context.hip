@@ -199,7 +199,7 @@ extern "C" int w2v_attend(const w2v_attend_spec* spec, const w2v_heads* q, const
 namespace {
 // The parts of the backward pass's workspace, each from a 256-byte border on.
 struct BackwardSpace {
-    size_t delta, by_distance, late_sums, own_sums, bytes;
+    size_t delta, by_distance, distance_sums, late_sums, own_sums, bytes;
     BackwardSpace(const w2v_attend_spec* s, uint32_t T) {
         size_t at = 0;
         const auto part = [&](size_t count) {
@@ -209,6 +209,7 @@ struct BackwardSpace {
         };
         delta = part((size_t)s->heads * T);
         by_distance = part(s->bias_dev ? (size_t)s->heads * attend_bias_parts(T) * (2 * s->span + 1) : 0);
+        distance_sums = part(s->bias_dev ? (size_t)s->heads * (2 * s->span + 1) : 0);
         const size_t late = (size_t)attend_late_pieces(T, s->left < T ? s->left : T, s->sinks).count * s->kv_heads * s->sinks * 2 * s->width;
         late_sums = part(late);
         own_sums = part(late);
@@ -253,6 +254,7 @@ extern "C" int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads*
         b.dq = heads_out(dq); b.dk = heads_out(dk); b.dv = heads_out(dv);
         b.delta = (float*)((char*)workspace + space.delta);
         b.by_distance = (float*)((char*)workspace + space.by_distance);
+        b.distance_sums = (float*)((char*)workspace + space.distance_sums);
         const LatePieces late = attend_late_pieces(n_tokens, b.a.left, b.a.sinks);
         b.late = late.count; b.late_words = late.words; b.reach = late.reach;
         b.late_sums = (float*)((char*)workspace + space.late_sums);

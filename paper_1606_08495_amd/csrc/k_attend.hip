@@ -37,7 +37,7 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
 
     typename Frag<T>::vec q[2 * DB];
 #pragma unroll
-    for (int s = 0; s < 2 * DB; ++s) q[s] = load_operand(head_row<T>(a.q, w.i, head), s, h, a.width);
+    for (int s = 0; s < 2 * DB; ++s) q[s] = load_operand<T, DB>(head_row<T>(a.q, w.i, head), s, h, a.width);
     const Texts texts(a, word0, last, w.i_first, w.i_last, lane);
     const Axis x(a, word0, last, texts);
     w.find(a, texts, lane);
@@ -46,30 +46,21 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
 #pragma unroll
     for (int b = 0; b < DB; ++b) o[b] = Acc{};
     float m = -__builtin_inff(), total = 0.f;
+    const float unit = BIAS ? 1.f : a.scale2;         // of the scores as piece_scores leaves them
 
-    Transit<T, DB, KEYS, THREADS> tk, tv;
-    uint8_t keep = 1;
+    KeyTiles<T, DB> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
-    const auto fetch = [&](uint32_t t) {
-        const auto row = [&](const Heads& p, uint32_t r) -> const T* {
-            const uint32_t n = t * KEYS + r;
-            if (n >= x.count) return nullptr;
-            return head_row<T>(p, x.token(n), kv_head);
-        };
-        tk.load([&](uint32_t r) { return row(a.k, r); }, a.width);
-        tv.load([&](uint32_t r) { return row(a.v, r); }, a.width);
-        if (a.keep) keep = t * KEYS + lane < x.count ? a.keep[x.token(t * KEYS + lane)] : 0;
-    };
+    next.start(a, kv_head, x);
     uint64_t kept = ~0ull;
     if (count) {
-        fetch(0);
-        tk.store(tiles[0][0]);
-        tv.store(tiles[0][1]);
-        kept = __ballot(keep != 0);
+        next.fetch(a, kv_head, x, 0, lane);
+        next.k.store(tiles[0][0], a.width);
+        next.v.store(tiles[0][1], a.width);
+        kept = __ballot(next.keep != 0);
     }
     __syncthreads();
     for (uint32_t t = 0; t < count; ++t) {
-        if (t + 1 < count) fetch(t + 1);
+        if (t + 1 < count) next.fetch(a, kv_head, x, t + 1, lane);
         const char *kt = tiles[t % BUFFERS][0], *vt = tiles[t % BUFFERS][1];
 #pragma unroll
         for (uint32_t piece = 0; piece < KEYS / 32; ++piece) {
@@ -83,7 +74,7 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
             float most = s[0];
 #pragma unroll
             for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
-            most = halves_max(most);
+            most = halves_max(most) * unit;
             if (__any(most > m + RISE)) {
                 const float to = fmaxf(m, most);
                 const float factor = to == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - to);
@@ -95,7 +86,7 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
             const float base = m == -__builtin_inff() ? 0.f : m;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(s[r] - base);
+                s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -base));
                 total += s[r];
             }
 #pragma unroll
@@ -117,9 +108,9 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
         }
         if (t + 1 < count) {
             if (BUFFERS == 1) __syncthreads();
-            tk.store(tiles[(t + 1) % BUFFERS][0]);
-            tv.store(tiles[(t + 1) % BUFFERS][1]);
-            kept = __ballot(keep != 0);
+            next.k.store(tiles[(t + 1) % BUFFERS][0], a.width);
+            next.v.store(tiles[(t + 1) % BUFFERS][1], a.width);
+            kept = __ballot(next.keep != 0);
             __syncthreads();
         }
     }

@@ -72,9 +72,9 @@ __global__ __launch_bounds__(THREADS, 2) void query_kernel(const BackwardArgs b)
     float delta = 0.f;
 #pragma unroll
     for (int s = 0; s < 2 * DB; ++s) {
-        q[s] = load_operand(head_row<T>(a.q, w.i, head), s, h, a.width);
-        g[s] = load_operand(head_row<T>(b.dout, w.i, head), s, h, a.width);
-        const auto o = load_operand((const T*)head_row<T>(a.o, w.i, head), s, h, a.width);
+        q[s] = load_operand<T, DB>(head_row<T>(a.q, w.i, head), s, h, a.width);
+        g[s] = load_operand<T, DB>(head_row<T>(b.dout, w.i, head), s, h, a.width);
+        const auto o = load_operand<T, DB>((const T*)head_row<T>(a.o, w.i, head), s, h, a.width);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             delta = fmaf((float)g[s][t], (float)o[t], delta);
@@ -92,30 +92,21 @@ __global__ __launch_bounds__(THREADS, 2) void query_kernel(const BackwardArgs b)
 #pragma unroll
     for (int n = 0; n < DB; ++n) dq[n] = Acc{};
     float low = 0.f, high = 0.f;
+    const float unit = BIAS ? 1.f : a.scale2;
 
-    Transit<T, DB, KEYS, THREADS> tk, tv;
-    uint8_t keep = 1;
+    KeyTiles<T, DB> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
-    const auto fetch = [&](uint32_t t) {
-        const auto row = [&](const Heads& p, uint32_t r) -> const T* {
-            const uint32_t n = t * KEYS + r;
-            if (n >= x.count) return nullptr;
-            return head_row<T>(p, x.token(n), kv_head);
-        };
-        tk.load([&](uint32_t r) { return row(a.k, r); }, a.width);
-        tv.load([&](uint32_t r) { return row(a.v, r); }, a.width);
-        if (a.keep) keep = t * KEYS + lane < x.count ? a.keep[x.token(t * KEYS + lane)] : 0;
-    };
+    next.start(a, kv_head, x);
     uint64_t kept = ~0ull;
     if (count) {
-        fetch(0);
-        tk.store(tiles[0][0]);
-        tv.store(tiles[0][1]);
-        kept = __ballot(keep != 0);
+        next.fetch(a, kv_head, x, 0, lane);
+        next.k.store(tiles[0][0], a.width);
+        next.v.store(tiles[0][1], a.width);
+        kept = __ballot(next.keep != 0);
     }
     __syncthreads();
     for (uint32_t t = 0; t < count; ++t) {
-        if (t + 1 < count) fetch(t + 1);
+        if (t + 1 < count) next.fetch(a, kv_head, x, t + 1, lane);
         const char *kt = tiles[t % BUFFERS][0], *vt = tiles[t % BUFFERS][1];
 #pragma unroll
         for (uint32_t piece = 0; piece < KEYS / 32; ++piece) {
@@ -131,7 +122,7 @@ __global__ __launch_bounds__(THREADS, 2) void query_kernel(const BackwardArgs b)
             piece_scores<BIAS>(a, w, x, n0, kept >> (piece * 32), linear, table, h, s);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(s[r] - lse2);
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -lse2));
                 s[r] = p * (dp[r] - delta);
                 if (BIAS && p == 0.f) s[r] = 0.f;     // the sums by distance are not formed anew
             }
@@ -168,9 +159,9 @@ __global__ __launch_bounds__(THREADS, 2) void query_kernel(const BackwardArgs b)
         }
         if (t + 1 < count) {
             if (BUFFERS == 1) __syncthreads();
-            tk.store(tiles[(t + 1) % BUFFERS][0]);
-            tv.store(tiles[(t + 1) % BUFFERS][1]);
-            kept = __ballot(keep != 0);
+            next.k.store(tiles[(t + 1) % BUFFERS][0], a.width);
+            next.v.store(tiles[(t + 1) % BUFFERS][1], a.width);
+            kept = __ballot(next.keep != 0);
             __syncthreads();
         }
     }
@@ -251,8 +242,8 @@ __global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const Bac
     typename Frag<T>::vec kf[2 * DB], vf[2 * DB];
 #pragma unroll
     for (int s = 0; s < 2 * DB; ++s) {
-        kf[s] = load_operand(head_row<T>(a.k, j, kv_head), s, h, a.width);
-        vf[s] = load_operand(head_row<T>(a.v, j, kv_head), s, h, a.width);
+        kf[s] = load_operand<T, DB>(head_row<T>(a.k, j, kv_head), s, h, a.width);
+        vf[s] = load_operand<T, DB>(head_row<T>(a.v, j, kv_head), s, h, a.width);
     }
     const bool keep = !(a.keep && !a.keep[j]);
     const Texts texts(a, k0, k1 - 1, j_first, j_last, lane);
@@ -299,8 +290,12 @@ __global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const Bac
     const uint32_t per_head = q1 > q0 ? (q1 - q0 + KEYS - 1) / KEYS : 0, count = per_head * a.group;
     const auto fetch = [&](uint32_t t) {
         const uint32_t head = kv_head * a.group + t / per_head, i0 = q0 + t % per_head * KEYS;
-        tq.load([&](uint32_t r) -> const T* { return i0 + r < q1 ? head_row<T>(a.q, i0 + r, head) : nullptr; }, a.width);
-        tg.load([&](uint32_t r) -> const T* { return i0 + r < q1 ? head_row<T>(b.dout, i0 + r, head) : nullptr; }, a.width);
+        if (t % per_head == 0) {
+            tq.start(a.q, head, q0, a.width);
+            tg.start(b.dout, head, q0, a.width);
+        }
+        tq.load(q1 - i0, a.width);
+        tg.load(q1 - i0, a.width);
         if (threadIdx.x < KEYS && i0 + threadIdx.x < q1) {
             const float l = a.lse[(size_t)head * a.T + i0 + threadIdx.x];
             lse2 = l == -__builtin_inff() ? 0.f : l * LOG2E;
@@ -308,8 +303,8 @@ __global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const Bac
         }
     };
     const auto put = [&](uint32_t t) {
-        tq.store(tiles[t % BUFFERS][0]);
-        tg.store(tiles[t % BUFFERS][1]);
+        tq.store(tiles[t % BUFFERS][0], a.width);
+        tg.store(tiles[t % BUFFERS][1], a.width);
         if (threadIdx.x < KEYS) {
             rows[t % BUFFERS][0][threadIdx.x] = lse2;
             rows[t % BUFFERS][1][threadIdx.x] = delta;
@@ -423,8 +418,6 @@ __global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const Bac
 constexpr uint32_t END_THREADS = 1024;
 template <typename T> __global__ __launch_bounds__(END_THREADS) void end_kernel(const BackwardArgs b, uint32_t parts) {
     const AttendArgs& a = b.a;
-    __shared__ float by_distance[2 * SPAN_MAX + 1];
-    __shared__ uint32_t bucket[2 * SPAN_MAX + 1];
     const uint32_t lane = threadIdx.x % WAVE;
     const uint32_t joins = b.late * a.kv_heads;
     if (blockIdx.x < joins) {
@@ -445,19 +438,37 @@ template <typename T> __global__ __launch_bounds__(END_THREADS) void end_kernel(
         }
         return;
     }
-    // a head's sums by distance over the blocks, then the distances of each bucket, both in order
-    const uint32_t head = blockIdx.x - joins, distances = 2 * a.span + 1;
+    // 32 distances of a head: 32 shares of the blocks' sums, joined in order
+    const uint32_t distances = 2 * a.span + 1, groups = (distances + 31) / 32;
+    const uint32_t head = (blockIdx.x - joins) / groups, c = (blockIdx.x - joins) % groups * 32 + threadIdx.x % 32;
+    __shared__ float shares[END_THREADS / 32][32];
     const float* from = b.by_distance + (size_t)head * parts * distances;
-    for (uint32_t c = threadIdx.x; c < distances; c += END_THREADS) {
-        float s = 0.f;
-        for (uint32_t p = 0; p < parts; ++p) s += from[(size_t)p * distances + c];
-        by_distance[c] = s;
+    float s = 0.f;
+    if (c < distances) {
+#pragma unroll 4
+        for (uint32_t p = threadIdx.x / 32; p < parts; p += END_THREADS / 32) s += from[(size_t)p * distances + c];
+    }
+    shares[threadIdx.x / 32][threadIdx.x % 32] = s;
+    __syncthreads();
+    if (threadIdx.x >= 32 || c >= distances) return;
+    for (uint32_t n = 1; n < END_THREADS / 32; ++n) s += shares[n][threadIdx.x];
+    b.distance_sums[(size_t)head * distances + c] = s;
+}
+
+// dbias of a head: the distances of each bucket, in order.
+__global__ __launch_bounds__(THREADS) void buckets_kernel(const BackwardArgs b, bool none) {
+    const AttendArgs& a = b.a;
+    __shared__ float sums[2 * SPAN_MAX + 1];
+    __shared__ uint32_t bucket[2 * SPAN_MAX + 1];
+    const uint32_t head = blockIdx.x, distances = 2 * a.span + 1;
+    for (uint32_t c = threadIdx.x; c < distances; c += THREADS) {
+        sums[c] = none ? 0.f : b.distance_sums[(size_t)head * distances + c];
         bucket[c] = a.buckets[c];
     }
     __syncthreads();
-    for (uint32_t k = threadIdx.x; k < a.n_buckets; k += END_THREADS) {
+    for (uint32_t k = threadIdx.x; k < a.n_buckets; k += THREADS) {
         float s = 0.f;
-        for (uint32_t c = 0; c < distances; ++c) if (bucket[c] == k) s += by_distance[c];
+        for (uint32_t c = 0; c < distances; ++c) s += bucket[c] == k ? sums[c] : 0.f;
         b.dbias[(size_t)head * a.n_buckets + k] = s;
     }
 }
@@ -480,8 +491,9 @@ template <typename T> void backward_any(const BackwardArgs& b, hipStream_t st) {
             case 3: backward_bias<T, 3>(b, st); break;
             default: backward_bias<T, 4>(b, st);
         }
-    const uint32_t blocks = b.late * b.a.kv_heads + (b.dbias ? b.a.heads : 0);
+    const uint32_t blocks = b.late * b.a.kv_heads + (b.dbias && b.a.T ? b.a.heads * ((2 * b.a.span + 32) / 32) : 0);
     if (blocks) end_kernel<T><<<blocks, END_THREADS, 0, st>>>(b, attend_bias_parts(b.a.T));
+    if (b.dbias) buckets_kernel<<<b.a.heads, THREADS, 0, st>>>(b, b.a.T == 0);
 }
 
 }  // namespace

@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "context.h"
 #include "elem.h"
 
 namespace w2v {
@@ -19,22 +20,22 @@ typedef float Acc __attribute__((ext_vector_type(16)));      // a 32 x 32 result
 
 template <typename T> struct Frag { typedef typename Pack<T, 8>::vec vec; };      // a lane's eight values of an operand
 
-__device__ inline void mma(const Frag<_Float16>::vec& a, const Frag<_Float16>::vec& b, Acc& c) {
+__device__ __forceinline__ void mma(const Frag<_Float16>::vec& a, const Frag<_Float16>::vec& b, Acc& c) {
     c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
-__device__ inline void mma(const Frag<__bf16>::vec& a, const Frag<__bf16>::vec& b, Acc& c) {
+__device__ __forceinline__ void mma(const Frag<__bf16>::vec& a, const Frag<__bf16>::vec& b, Acc& c) {
     c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-__device__ inline void mma(const Frag<float>::vec& a, const Frag<float>::vec& b, Acc& c) {
+__device__ __forceinline__ void mma(const Frag<float>::vec& a, const Frag<float>::vec& b, Acc& c) {
 #pragma unroll
     for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], b[t], c, 0, 0, 0);
 }
 
 // Row of a result's register r in lane half h.
-__device__ inline constexpr int acc_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
+__device__ __forceinline__ constexpr int acc_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
 
 // Registers 8 s .. 8 s + 7 of a result as the operand of the next product.
-template <typename T> __device__ inline typename Frag<T>::vec acc_operand(const Acc& c, int s) {
+template <typename T> __device__ __forceinline__ typename Frag<T>::vec acc_operand(const Acc& c, int s) {
     typename Frag<T>::vec f;
 #pragma unroll
     for (int t = 0; t < 8; ++t) f[t] = (T)c[8 * s + t];
@@ -42,35 +43,57 @@ template <typename T> __device__ inline typename Frag<T>::vec acc_operand(const 
 }
 
 // Sum, and largest, over a lane and its partner in the other half of the wavefront.
-__device__ inline float halves_max(float x) {
+__device__ __forceinline__ float halves_max(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ inline float halves_sum(float x) {
+__device__ __forceinline__ float halves_sum(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// 16 bytes of a row of `width` elements, from element c0 on; zeros past the row's end.
-template <typename T> __device__ inline typename Pack<T, pack16<T>>::vec load_chunk(const T* row, uint32_t c0, uint32_t width) {
-    constexpr int N = pack16<T>;
-    typename Pack<T, N>::vec x;
-    if (c0 + N <= width) {
-        x = *(const typename Pack<T, N>::mem*)(row + c0);
-    } else {
+// Chunks: 16 bytes of a row of `width` elements, from element c0 on, zeros past the row's end.  The chunk that the end cuts is
+// read as the row's last 16 bytes and moved down afterwards (chunk_fit), so that no access leaves the row and none waits for
+// another; rows shorter than a chunk are read by elements.
+template <typename T, bool NARROW> __device__ __forceinline__ typename Pack<T, pack16<T>>::vec chunk_read(const T* row, uint32_t c0, uint32_t width) {
+    constexpr uint32_t N = pack16<T>;
+    typename Pack<T, N>::vec x = {};
+    if (!NARROW || width >= N) {
+        if (c0 < width) x = *(const typename Pack<T, N>::mem*)(row + (c0 < width - N ? c0 : width - N));
+    } else if (c0 == 0) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = c0 + e < width ? row[c0 + e] : (T)0.f;
+        for (uint32_t e = 0; e < N; ++e) if (e < width) x[e] = row[e];
+    }
+    return x;
+}
+template <typename T>
+__device__ __forceinline__ typename Pack<T, pack16<T>>::vec chunk_fit(typename Pack<T, pack16<T>>::vec x, uint32_t c0, uint32_t width) {
+    constexpr uint32_t N = pack16<T>;
+    if (width >= N && width % N) {
+        const bool cut = c0 < width && c0 + N > width;
+        const uint32_t by = cut ? (c0 + N - width) * (uint32_t)sizeof(T) : 0;      // bytes to move down by
+        typedef uint32_t Words __attribute__((ext_vector_type(4)));
+        Words w = __builtin_bit_cast(Words, x);
+        const bool two = by & 8, one = by & 4, half = by & 2;
+        w = Words{two ? w[2] : w[0], two ? w[3] : w[1], two ? 0u : w[2], two ? 0u : w[3]};
+        w = Words{one ? w[1] : w[0], one ? w[2] : w[1], one ? w[3] : w[2], one ? 0u : w[3]};
+        if constexpr (sizeof(T) == 2) {
+            const Words u = {w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+            w = Words{half ? u[0] : w[0], half ? u[1] : w[1], half ? u[2] : w[2], half ? u[3] : w[3]};
+        }
+        x = __builtin_bit_cast(typename Pack<T, N>::vec, w);
     }
     return x;
 }
 
 // A lane's operand for step s straight from its row in memory.
-template <typename T> __device__ inline typename Frag<T>::vec load_operand(const T* row, int s, uint32_t h, uint32_t width) {
+template <typename T, int DB> __device__ __forceinline__ typename Frag<T>::vec load_operand(const T* row, int s, uint32_t h, uint32_t width) {
     constexpr int N = pack16<T>;
     typename Frag<T>::vec f;
 #pragma unroll
     for (int p = 0; p < 8 / N; ++p) {
-        const auto x = load_chunk(row, 16 * s + 8 * h + p * N, width);
+        const uint32_t c0 = 16 * s + 8 * h + p * N;
+        const auto x = chunk_fit<T>(chunk_read<T, DB == 1>(row, c0, width), c0, width);
 #pragma unroll
         for (int e = 0; e < N; ++e) f[p * N + e] = x[e];
     }
@@ -82,14 +105,14 @@ template <typename T> __device__ inline typename Frag<T>::vec load_operand(const
 template <typename T, int DB, int ROWS> struct Tile {
     static constexpr int N = pack16<T>, ROW = DB * 32 * (int)sizeof(T), CHUNKS = ROW / 16, BYTES = ROWS * ROW;
     typedef typename Pack<T, N>::vec Chunk;
-    __device__ static inline uint32_t turn(uint32_t r) {
+    __device__ static __forceinline__ uint32_t turn(uint32_t r) {
         if constexpr (CHUNKS % 16 == 0) return ((r & 3) << 2) | ((r >> 2) & 3);
         else if constexpr (CHUNKS % 8 == 0) return ((r & 2) << 1) | ((r >> 1) & 2) | ((r >> 3) & 1);
         else return (r >> 2) & 3;
     }
-    __device__ static inline uint32_t place(uint32_t r, uint32_t c) { return r * ROW + ((c ^ turn(r)) << 4); }
+    __device__ static __forceinline__ uint32_t place(uint32_t r, uint32_t c) { return r * ROW + ((c ^ turn(r)) << 4); }
     // rows as they are: lane's row of A, step s
-    __device__ static inline typename Frag<T>::vec along(const char* tile, uint32_t r, int s, uint32_t h) {
+    __device__ static __forceinline__ typename Frag<T>::vec along(const char* tile, uint32_t r, int s, uint32_t h) {
         typename Frag<T>::vec f;
 #pragma unroll
         for (int p = 0; p < 8 / N; ++p) {
@@ -100,7 +123,7 @@ template <typename T, int DB, int ROWS> struct Tile {
         return f;
     }
     // columns as rows of A: element 32 b + lane % 32 of rows r0 + 16 s + 8 (t / 4) + 4 h + t % 4
-    __device__ static inline typename Frag<T>::vec across(const char* tile, uint32_t r0, int s, int b, uint32_t lane) {
+    __device__ static __forceinline__ typename Frag<T>::vec across(const char* tile, uint32_t r0, int s, int b, uint32_t lane) {
         typename Frag<T>::vec f;
         const uint32_t h = lane / 32;
         if constexpr (sizeof(T) == 2) {
@@ -124,31 +147,57 @@ template <typename T, int DB, int ROWS> struct Tile {
     }
 };
 
-// A tile's rows on their way from memory to LDS, in the registers of THREADS threads.
+// A tile's rows on their way from memory to LDS, in the registers of THREADS threads: a thread keeps one chunk's column and
+// every RS-th row.  Rows past the last are not read and keep what was there: they are masked.
 template <typename T, int DB, int ROWS, int THREADS> struct Transit {
     typedef Tile<T, DB, ROWS> Tl;
-    static constexpr int PER = (ROWS * Tl::CHUNKS + THREADS - 1) / THREADS;
+    static constexpr uint32_t LANES = Tl::CHUNKS <= 4 ? 4 : Tl::CHUNKS <= 8 ? 8 : Tl::CHUNKS <= 16 ? 16 : 32;
+    static constexpr uint32_t RS = THREADS / LANES, PER = ROWS / RS;
     typename Tl::Chunk x[PER];
-    // row(r): the row's first element in memory, or null where the tile has none
-    template <typename F> __device__ inline void load(F row, uint32_t width) {
+    const T* at;                                      // the chunk of the thread's first row in the tile to be read next
+    uint64_t stride;
+    uint32_t r0, c0;
+    bool mine;
+    // row 0 of the first tile is token `token` (which may lie before the first, where no such row is read)
+    __device__ __forceinline__ void start(const Heads& p, uint32_t head, int64_t token, uint32_t width) {
+        r0 = threadIdx.x / LANES;
+        c0 = threadIdx.x % LANES * Tl::N;
+        mine = c0 < width;
+        stride = p.token;
+        at = (const T*)p.p + (uint64_t)head * p.head + (token + r0) * (int64_t)p.token;
 #pragma unroll
-        for (int n = 0; n < PER; ++n) {
-            const uint32_t at = threadIdx.x + n * THREADS;
-            typename Tl::Chunk z = {};
-            x[n] = z;
-            if (ROWS * Tl::CHUNKS % THREADS == 0 || at < ROWS * Tl::CHUNKS) {
-                const T* p = row(at / Tl::CHUNKS);
-                if (p) x[n] = load_chunk(p, (at % Tl::CHUNKS) * Tl::N, width);
-            }
-        }
+        for (uint32_t n = 0; n < PER; ++n) x[n] = typename Tl::Chunk{};
     }
-    __device__ inline void store(char* tile) const {
+    __device__ __forceinline__ void read(uint32_t n, const T* row, uint32_t width) {
+        constexpr uint32_t N = Tl::N;
+        if (DB == 1 && width < N) x[n] = chunk_read<T, true>(row, c0, width);
+        else x[n] = *(const typename Pack<T, N>::mem*)(row + (c0 < width - N ? c0 : width - N));
+    }
+    // the tile's first `rows` rows, then on to the next tile
+    __device__ __forceinline__ void load(uint32_t rows, uint32_t width) {
+        if (rows >= (uint32_t)ROWS) {
+            if (mine)
 #pragma unroll
-        for (int n = 0; n < PER; ++n) {
-            const uint32_t at = threadIdx.x + n * THREADS;
-            if (ROWS * Tl::CHUNKS % THREADS == 0 || at < ROWS * Tl::CHUNKS)
-                *(typename Tl::Chunk*)(tile + Tl::place(at / Tl::CHUNKS, at % Tl::CHUNKS)) = x[n];
+                for (uint32_t n = 0; n < PER; ++n) read(n, at + n * RS * stride, width);
+        } else {
+#pragma unroll
+            for (uint32_t n = 0; n < PER; ++n) if (mine && r0 + n * RS < rows) read(n, at + n * RS * stride, width);
         }
+        at += ROWS * stride;
+    }
+    // the same where row r lies at row(r)
+    template <typename F> __device__ __forceinline__ void load_rows(const F& row, uint32_t rows, uint32_t width) {
+#pragma unroll
+        for (uint32_t n = 0; n < PER; ++n) if (mine && r0 + n * RS < rows) read(n, row(r0 + n * RS), width);
+        at += ROWS * stride;
+    }
+    __device__ __forceinline__ void store(char* tile, uint32_t width) {
+        if (c0 >= (uint32_t)Tl::CHUNKS * Tl::N) return;
+        if (width % Tl::N)
+#pragma unroll
+            for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_fit<T>(x[n], c0, width);
+#pragma unroll
+        for (uint32_t n = 0; n < PER; ++n) *(typename Tl::Chunk*)(tile + Tl::place(r0 + n * RS, c0 / Tl::N)) = x[n];
     }
 };
 
