@@ -5,7 +5,11 @@
 
 namespace w2v {
 
-constexpr int BLOCK_WORDS = 128, WAVE_WORDS = 32, KEYS = 64, THREADS = 256;
+constexpr int BLOCK_WORDS = 128, WAVE_WORDS = 32, KEYS = 64, THREADS = 256, GROUPS = BLOCK_WORDS / WAVE_WORDS;
+
+// Where there are fewer blocks than this, a block has twice the wavefronts, and each takes one of a tile's two pieces.
+constexpr uint32_t SPLIT_BELOW = 512;
+constexpr size_t LDS_BYTES = 160 * 1024;              // a block's most
 
 // The texts of a block's first and last token and of a wavefront's.
 struct Texts {
@@ -66,10 +70,11 @@ struct Axis {
 
 // Bias by distance, times log2 e, with the outermost values repeated on both sides so that every distance within a
 // 32 x 32 piece that is not wholly past the span is in the table.
-constexpr int BIAS_SIDE = 64, BIAS_TABLE = 2 * SPAN_MAX + 1 + 2 * BIAS_SIDE;
+constexpr int BIAS_SIDE = 64;
+__host__ __device__ inline uint32_t bias_table(uint32_t span) { return (2 * (span + BIAS_SIDE) + 1 + 3) / 4 * 4; }
 __device__ __forceinline__ void fill_bias(const AttendArgs& a, uint32_t head, float* table) {
     const int32_t reach = (int32_t)a.span + BIAS_SIDE;
-    for (int32_t at = threadIdx.x; at <= 2 * reach; at += THREADS) table[at] = scaled_bias(a, head, at - reach);
+    for (int32_t at = threadIdx.x; at <= 2 * reach; at += (int32_t)blockDim.x) table[at] = scaled_bias(a, head, at - reach);
 }
 
 // Scores of a piece of 32 keys, masked: s on the way in holds the products.  With a bias they are to base two, without one
@@ -115,8 +120,8 @@ __device__ __forceinline__ void piece_scores(const AttendArgs& a, const Words& w
 }
 
 // Keys and values of a block, tile by tile from memory to LDS, and which of the next tile's words are kept.
-template <typename T, int DB> struct KeyTiles {
-    Transit<T, DB, KEYS, THREADS> k, v;
+template <typename T, int DB, int SPLIT> struct KeyTiles {
+    Transit<T, DB, KEYS, SPLIT * THREADS> k, v;
     uint8_t keep;
     __device__ __forceinline__ void start(const AttendArgs& a, uint32_t kv_head, const Axis& x) {
         k.start(a.k, kv_head, (int64_t)(int32_t)x.shift, a.width);

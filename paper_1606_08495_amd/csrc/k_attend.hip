@@ -14,6 +14,8 @@
 // leaves them the relative rounding that v has; their sum is taken before the rounding.  Heads of up to 32 columns add
 // what the rounding left in a second product: the gradient's dout . out is then a sum of few terms, which
 // may cancel down to the weights' rounding, and the matrix cores wait for the exponentials there anyway.
+#include <type_traits>
+
 #include "attend_tiles.h"
 
 namespace w2v {
@@ -21,13 +23,15 @@ namespace {
 
 constexpr float RISE = 8.f;           // how far (to base two) a maximum may rise before outputs are rescaled
 
-template <typename T, int DB, bool BIAS>
-__global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) {
+template <typename T, int DB, bool BIAS, int SPLIT>
+__global__ __launch_bounds__(SPLIT * THREADS, 2) void attend_kernel(const AttendArgs a) {
     typedef Tile<T, DB, KEYS> Tl;
-    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 128 * 1024 ? 2 : 1;
+    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 72 * 1024 ? 2 : 1, KEEP = DB * 16 + 2;
+    constexpr bool JOINT = sizeof(T) == 2 || DB <= 2;      // both pieces of a tile at a time, where registers allow
     __shared__ __align__(16) char tiles[BUFFERS][2][Tl::BYTES];
-    __shared__ float table[BIAS ? BIAS_TABLE : 1];
-    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE;
+    static_assert(SPLIT == 1 || GROUPS * KEEP * WAVE * 4 <= (int)sizeof(tiles), "room to join the halves");
+    extern __shared__ float table[];
+    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE % GROUPS, half = threadIdx.x / THREADS;
     const uint32_t head = blockIdx.x % a.heads, kv_head = head / a.group;
     const uint32_t words = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS;
     const uint32_t word0 = (words - 1 - blockIdx.x / a.heads) * BLOCK_WORDS;      // those that may see most first
@@ -47,8 +51,9 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
     for (int b = 0; b < DB; ++b) o[b] = Acc{};
     float m = -__builtin_inff(), total = 0.f;
     const float unit = BIAS ? 1.f : a.scale2;         // of the scores as piece_scores leaves them
+    const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
 
-    KeyTiles<T, DB> next;
+    KeyTiles<T, DB, SPLIT> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
     next.start(a, kv_head, x);
     uint64_t kept = ~0ull;
@@ -62,18 +67,23 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
     for (uint32_t t = 0; t < count; ++t) {
         if (t + 1 < count) next.fetch(a, kv_head, x, t + 1, lane);
         const char *kt = tiles[t % BUFFERS][0], *vt = tiles[t % BUFFERS][1];
+        // P pieces of 32 keys from piece p0 on
+        const auto pieces = [&](auto P, int p0) __attribute__((always_inline)) {
+            Acc s[P.value];
 #pragma unroll
-        for (uint32_t piece = 0; piece < KEYS / 32; ++piece) {
-            const uint32_t n0 = t * KEYS + piece * 32;
-            const bool linear = n0 >= x.sunk;
-            if (!some || n0 >= x.count || (linear && !w.shown_any(n0 + x.shift))) continue;
-            Acc s = {};
+            for (int p = 0; p < P.value; ++p) s[p] = Acc{};
 #pragma unroll
-            for (int k = 0; k < 2 * DB; ++k) mma(Tl::along(kt, piece * 32 + lane % 32, k, h), q[k], s);
-            piece_scores<BIAS>(a, w, x, n0, kept >> (piece * 32), linear, table, h, s);
-            float most = s[0];
+            for (int k = 0; k < 2 * DB; ++k)
 #pragma unroll
-            for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
+                for (int p = 0; p < P.value; ++p) mma(Tl::along(kt, at_along, (p0 + p) * 32, k), q[k], s[p]);
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int p = 0; p < P.value; ++p) {
+                const uint32_t n0 = t * KEYS + (p0 + p) * 32;
+                piece_scores<BIAS>(a, w, x, n0, kept >> ((p0 + p) * 32), n0 >= x.sunk, table, h, s[p]);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, s[p][r]);
+            }
             most = halves_max(most) * unit;
             if (__any(most > m + RISE)) {
                 const float to = fmaxf(m, most);
@@ -85,25 +95,43 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
             }
             const float base = m == -__builtin_inff() ? 0.f : m;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -base));
-                total += s[r];
+            for (int p = 0; p < P.value; ++p) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[p][r] = __builtin_amdgcn_exp2f(fmaf(s[p][r], unit, -base));
+                    total += s[p][r];
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const auto e = acc_operand<T>(s[p], k);
+                    typename Frag<T>::vec v[DB];
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) {
+                        v[b] = Tl::across(vt, at_across, (p0 + p) * 32, k, b);
+                        mma(v[b], e, o[b]);
+                    }
+                    if constexpr (sizeof(T) == 2 && DB == 1) {      // what the rounding left of the weights
+                        typename Frag<T>::vec rest;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) rest[c] = (T)(s[p][8 * k + c] - (float)e[c]);
+                        mma(v[0], rest, o[0]);
+                    }
+                }
             }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const auto p = acc_operand<T>(s, k);
-                typename Frag<T>::vec v[DB];
-#pragma unroll
-                for (int b = 0; b < DB; ++b) {
-                    v[b] = Tl::across(vt, piece * 32, k, b, lane);
-                    mma(v[b], p, o[b]);
-                }
-                if constexpr (sizeof(T) == 2 && DB == 1) {      // what the rounding left of the weights
-                    typename Frag<T>::vec rest;
-#pragma unroll
-                    for (int t = 0; t < 8; ++t) rest[t] = (T)(s[8 * k + t] - (float)p[t]);
-                    mma(v[0], rest, o[0]);
-                }
+        };
+        const auto needs = [&](uint32_t piece) __attribute__((always_inline)) {
+            const uint32_t n0 = t * KEYS + piece * 32;
+            return some && n0 < x.count && (n0 < x.sunk || w.shown_any(n0 + x.shift));
+        };
+        if constexpr (SPLIT == 2) {
+            if (half == 0) { if (needs(0)) pieces(std::integral_constant<int, 1>{}, 0); }
+            else if (needs(1)) pieces(std::integral_constant<int, 1>{}, 1);
+        } else {
+            const bool n0 = needs(0), n1 = needs(1);
+            if (JOINT && n0 && n1) pieces(std::integral_constant<int, JOINT ? 2 : 1>{}, 0);
+            else {
+                if (n0) pieces(std::integral_constant<int, 1>{}, 0);
+                if (n1) pieces(std::integral_constant<int, 1>{}, 1);
             }
         }
         if (t + 1 < count) {
@@ -113,6 +141,30 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
             kept = __ballot(next.keep != 0);
             __syncthreads();
         }
+    }
+    if constexpr (SPLIT == 2) {                       // the second half's sums through LDS to the first
+        float* const other = (float*)&tiles[0][0][0] + wave * KEEP * WAVE + lane;
+        __syncthreads();
+        if (half) {
+            other[0] = m;
+            other[WAVE] = total;
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) other[(2 + b * 16 + r) * WAVE] = o[b][r];
+        }
+        __syncthreads();
+        if (half) return;
+        const float m1 = other[0], to = fmaxf(m, m1);
+        const float f0 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - to);
+        const float f1 = m1 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m1 - to);
+        // (a maximum is -infinity where a half has seen nothing: its sums are zero; not a number stays where it is)
+        total = total * (total == 0.f ? 1.f : f0) + other[WAVE] * (other[WAVE] == 0.f ? 1.f : f1);
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[b][r] = o[b][r] * f0 + other[(2 + b * 16 + r) * WAVE] * f1;
+        m = to;
     }
     if (!some) return;
 
@@ -163,10 +215,14 @@ __global__ __launch_bounds__(THREADS, 2) void attend_kernel(const AttendArgs a) 
     }
 }
 
+template <typename T, int DB, bool BIAS> void attend_bias(const AttendArgs& a, hipStream_t st) {
+    const uint32_t blocks = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS * a.heads, table = BIAS ? bias_table(a.span) * sizeof(float) : 0;
+    if (blocks < SPLIT_BELOW) attend_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(a);
+    else attend_kernel<T, DB, BIAS, 1><<<blocks, THREADS, table, st>>>(a);
+}
 template <typename T, int DB> void attend_run(const AttendArgs& a, hipStream_t st) {
-    const uint32_t blocks = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS * a.heads;
-    if (a.bias) attend_kernel<T, DB, true><<<blocks, THREADS, 0, st>>>(a);
-    else attend_kernel<T, DB, false><<<blocks, THREADS, 0, st>>>(a);
+    if (a.bias) attend_bias<T, DB, true>(a, st);
+    else attend_bias<T, DB, false>(a, st);
 }
 template <typename T> void attend_any(const AttendArgs& a, hipStream_t st) {
     switch ((a.width + 31) / 32) {

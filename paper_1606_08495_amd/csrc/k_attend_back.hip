@@ -12,6 +12,8 @@
 // A text's first words that stay visible are seen by every later word.  The keys' kernel takes the queries up to a
 // border behind its block; those behind go in pieces to blocks of their own (late), whose sums are joined in
 // order at the end.
+#include <type_traits>
+
 #include "attend_tiles.h"
 
 namespace w2v {
@@ -43,30 +45,53 @@ template <int DB> __device__ inline bool not_finite(const Acc (&c)[DB]) {
     return halves_sum(worst) != 0.f;
 }
 
+// Joins what two halves of a block have summed for the same words: the second's through LDS to the first.  True for the half
+// that goes on with the sums.  A place for each of the block's four groups of words.
+template <int N> __device__ __forceinline__ bool join_halves(float* room, Acc (&c)[N], uint32_t wave, uint32_t half, uint32_t lane) {
+    float* const other = room + wave * N * 16 * WAVE + lane;
+    __syncthreads();
+    if (half)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) other[(n * 16 + r) * WAVE] = c[n][r];
+    __syncthreads();
+    if (half) return false;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) c[n][r] += other[(n * 16 + r) * WAVE];
+    return true;
+}
+
 // ---- queries: dq, delta, the bias' sums -----------------------------------------------------------------
-// Sums of dS by distance: an array in LDS for each half of each wavefront, in which the 32 lanes of one register's row
-// lie side by side, so that no two lanes add to one place at a time; outermost distances by registers.
-template <typename T, int DB, bool BIAS>
-__global__ __launch_bounds__(THREADS, 2) void query_kernel(const BackwardArgs b) {
+// delta is taken from out as it was rounded, or, where that would show, formed from the scores in a pass of its own before the
+// others (sum of p dP, which needs neither out nor its rounding): for the bias' gradient, an fp32 sum over all pairs, and for
+// words that are shown few others, whose out is large.  EXACT_KEYS is from where on the rounding of dS hides that of out.
+constexpr uint32_t EXACT_KEYS = 512;
+
+// Sums of dS by distance.  A piece's 32 x 32 values have 63 distances.  They go through LDS, each row moved by its number so that a
+// distance is a column (SKEW floats a row; what a row does not fill stays zero), and a lane adds up one column.
+// (Atomic adds in LDS take a cycle a lane: sixteen times that.)
+constexpr int SKEW = 64, SKEW_FLOATS = 32 * SKEW;
+
+template <typename T, int DB, bool BIAS, int SPLIT>
+__global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) void query_kernel(const BackwardArgs b) {
     const AttendArgs& a = b.a;
     typedef Tile<T, DB, KEYS> Tl;
-    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 64 * 1024 ? 2 : 1;
-    __shared__ __align__(16) char tiles[BUFFERS][2][Tl::BYTES];
+    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= (BIAS ? 40 : 72) * 1024 ? 2 : 1;
+    constexpr int ROOM = SPLIT == 2 ? GROUPS * DB * 16 * WAVE * 4 : 0;
+    __shared__ __align__(16) char tiles[BUFFERS * 2 * Tl::BYTES > ROOM ? BUFFERS * 2 * Tl::BYTES : ROOM];
+    __shared__ float deltas[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS];
     extern __shared__ float dynamic[];
     const int32_t span = (int32_t)a.span, reach = span + BIAS_SIDE;
-    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE;
+    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE % GROUPS, half = threadIdx.x / THREADS;
     const uint32_t head = blockIdx.x % a.heads, kv_head = head / a.group;
     const uint32_t words = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS;
     const uint32_t part = words - 1 - blockIdx.x / a.heads, word0 = part * BLOCK_WORDS;
-    float* const table = dynamic;
-    float* const sums = dynamic + (2 * wave + 1 + h) * (2 * reach + 1);
     const uint32_t first = word0 + wave * WAVE_WORDS, last = word0 + BLOCK_WORDS - 1 < a.T ? word0 + BLOCK_WORDS - 1 : a.T - 1;
     Words w(a, first, lane);
     const bool some = first < a.T, real = first + lane % WAVE_WORDS < a.T;
-    if (BIAS) {
-        fill_bias(a, head, table);
-        if (b.dbias) for (int32_t c = lane % 32; c <= 2 * reach; c += 32) sums[c] = 0.f;
-    }
 
     typename Frag<T>::vec q[2 * DB], g[2 * DB];
     float delta = 0.f;
@@ -83,89 +108,138 @@ __global__ __launch_bounds__(THREADS, 2) void query_kernel(const BackwardArgs b)
     }
     delta = real ? halves_sum(delta) : 0.f;
     float lse2 = a.lse[(size_t)head * a.T + w.i];
-    if (real && h == 0) b.delta[(size_t)head * a.T + w.i] = delta;
     lse2 = lse2 == -__builtin_inff() ? 0.f : lse2 * LOG2E;      // of a word that is shown nothing: every score is masked
     const Texts texts(a, word0, last, w.i_first, w.i_last, lane);
     const Axis x(a, word0, last, texts);
     w.find(a, texts, lane);
+    float* const table = dynamic;
+    float* const skew = dynamic + bias_table(a.span) + threadIdx.x / WAVE * (SKEW_FLOATS + bias_table(a.span));
+    float* const sums = skew + SKEW_FLOATS;
+    if (BIAS) {
+        fill_bias(a, head, table);
+        if (b.dbias) for (int32_t c = lane; c < SKEW_FLOATS + (int32_t)bias_table(a.span); c += WAVE) skew[c] = 0.f;
+    }
     Acc dq[DB];
 #pragma unroll
     for (int n = 0; n < DB; ++n) dq[n] = Acc{};
     float low = 0.f, high = 0.f;
     const float unit = BIAS ? 1.f : a.scale2;
+    const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
 
-    KeyTiles<T, DB> next;
+    KeyTiles<T, DB, SPLIT> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
-    next.start(a, kv_head, x);
-    uint64_t kept = ~0ull;
-    if (count) {
-        next.fetch(a, kv_head, x, 0, lane);
-        next.k.store(tiles[0][0], a.width);
-        next.v.store(tiles[0][1], a.width);
-        kept = __ballot(next.keep != 0);
-    }
-    __syncthreads();
-    for (uint32_t t = 0; t < count; ++t) {
-        if (t + 1 < count) next.fetch(a, kv_head, x, t + 1, lane);
-        const char *kt = tiles[t % BUFFERS][0], *vt = tiles[t % BUFFERS][1];
+    const bool exact = sizeof(T) == 2 && ((BIAS && b.dbias) || x.count <= EXACT_KEYS);
+    float formed = 0.f;
+    const auto walk = [&](auto PASS) __attribute__((always_inline)) {
+        constexpr int pass = PASS.value;
+        next.start(a, kv_head, x);
+        uint64_t kept = ~0ull;
+        if (count) {
+            next.fetch(a, kv_head, x, 0, lane);
+            if (pass == 1 && exact) __syncthreads();  // the last tiles of the pass before
+            next.k.store(tiles, a.width);
+            next.v.store(tiles + Tl::BYTES, a.width);
+            kept = __ballot(next.keep != 0);
+        }
+        __syncthreads();
+        for (uint32_t t = 0; t < count; ++t) {
+            if (t + 1 < count) next.fetch(a, kv_head, x, t + 1, lane);
+            const char *kt = tiles + t % BUFFERS * 2 * Tl::BYTES, *vt = kt + Tl::BYTES;
+            const auto one = [&](auto P) __attribute__((always_inline)) {
+                constexpr int piece = P.value;
+                const uint32_t n0 = t * KEYS + piece * 32, j0 = n0 + x.shift;
+                const bool linear = n0 >= x.sunk;
+                if (!some || n0 >= x.count || (linear && !w.shown_any(j0))) return;
+                Acc s = {}, dp = {};
 #pragma unroll
-        for (uint32_t piece = 0; piece < KEYS / 32; ++piece) {
-            const uint32_t n0 = t * KEYS + piece * 32, j0 = n0 + x.shift;
-            const bool linear = n0 >= x.sunk;
-            if (!some || n0 >= x.count || (linear && !w.shown_any(j0))) continue;
-            Acc s = {}, dp = {};
+                for (int k = 0; k < 2 * DB; ++k) {
+                    mma(Tl::along(kt, at_along, piece * 32, k), q[k], s);
+                    mma(Tl::along(vt, at_along, piece * 32, k), g[k], dp);
+                }
+                piece_scores<BIAS>(a, w, x, n0, kept >> (piece * 32), linear, table, h, s);
+                if constexpr (pass == 0) {
 #pragma unroll
-            for (int k = 0; k < 2 * DB; ++k) {
-                mma(Tl::along(kt, piece * 32 + lane % 32, k, h), q[k], s);
-                mma(Tl::along(vt, piece * 32 + lane % 32, k, h), g[k], dp);
-            }
-            piece_scores<BIAS>(a, w, x, n0, kept >> (piece * 32), linear, table, h, s);
+                    for (int r = 0; r < 16; ++r) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -lse2));
+                        formed = fmaf(p, p == 0.f ? 0.f : dp[r], formed);
+                    }
+                    return;
+                }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -lse2));
-                s[r] = p * (dp[r] - delta);
-                if (BIAS && p == 0.f) s[r] = 0.f;     // the sums by distance are not formed anew
-            }
-            if constexpr (BIAS) {
-                if (b.dbias) {
-                    const int32_t far = (int32_t)j0 - (int32_t)w.i_first + 31, near = (int32_t)j0 - (int32_t)w.i_last;
-                    if (linear && (far <= -span || near >= span)) {
-                        float all = 0.f;
+                for (int r = 0; r < 16; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -lse2));
+                    s[r] = p * (dp[r] - delta);
+                    if (BIAS && p == 0.f) s[r] = 0.f;     // the sums by distance are not formed anew
+                }
+                if constexpr (BIAS) {
+                    if (b.dbias) {
+                        const int32_t far = (int32_t)j0 - (int32_t)w.i_first + 31, near = (int32_t)j0 - (int32_t)w.i_last;
+                        if (linear && (far <= -span || near >= span)) {
+                            float all = 0.f;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) all += s[r];
-                        if (far <= -span) low += all; else high += all;
-                    } else if (linear) {
-                        float* at = sums + ((int32_t)j0 - (int32_t)w.i + reach + 4 * (int32_t)h);
+                            for (int r = 0; r < 16; ++r) all += s[r];
+                            if (far <= -span) low += all; else high += all;
+                        } else if (linear) {
+                            float* const to = skew + 4 * h * (SKEW + 1) + 31 - lane % 32;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            __hip_atomic_fetch_add(at + acc_row(r, 0), s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-                    } else {
+                            for (int r = 0; r < 16; ++r) to[acc_row(r, 0) * (SKEW + 1)] = s[r];
+                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                            float all = 0.f;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int32_t dist = (int32_t)x.token(n0 + acc_row(r, h)) - (int32_t)w.i;
-                            if (dist <= -span) low += s[r];
-                            else if (dist >= span) high += s[r];
-                            else __hip_atomic_fetch_add(sums + dist + reach, s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                            for (int n = 0; n < 32; ++n) all += skew[n * SKEW + lane];
+                            // column c: distance j0 - i_first - 31 + c
+                            if (lane < 63) sums[(int32_t)j0 - (int32_t)w.i_first - 31 + (int32_t)lane + reach] += all;
+                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        } else {
+// the piece where the first words and the window meet: one half after the other, no place twice at a time
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) {
+                                const int32_t dist = (int32_t)x.token(n0 + acc_row(r, h)) - (int32_t)w.i;
+                                const bool inside = dist > -span && dist < span;
+                                low += dist <= -span ? s[r] : 0.f;
+                                high += dist >= span ? s[r] : 0.f;
+                                float* const to = sums + (inside ? dist + reach : 0);
+                                if (inside && h == 0) __hip_atomic_fetch_add(to, s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                                if (inside && h == 1) __hip_atomic_fetch_add(to, s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                            }
                         }
                     }
                 }
-            }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const auto ds = acc_operand<T>(s, k);
+                for (int k = 0; k < 2; ++k) {
+                    const auto ds = acc_operand<T>(s, k);
 #pragma unroll
-                for (int n = 0; n < DB; ++n) mma(Tl::across(kt, piece * 32, k, n, lane), ds, dq[n]);
+                    for (int n = 0; n < DB; ++n) mma(Tl::across(kt, at_across, piece * 32, k, n), ds, dq[n]);
+                }
+            };
+            if (SPLIT == 1 || half == 0) one(std::integral_constant<int, 0>{});
+            if (SPLIT == 1 || half == 1) one(std::integral_constant<int, 1>{});
+            if (t + 1 < count) {
+                if (BUFFERS == 1) __syncthreads();
+                char* const to = tiles + (t + 1) % BUFFERS * 2 * Tl::BYTES;
+                next.k.store(to, a.width);
+                next.v.store(to + Tl::BYTES, a.width);
+                kept = __ballot(next.keep != 0);
+                __syncthreads();
             }
         }
-        if (t + 1 < count) {
-            if (BUFFERS == 1) __syncthreads();
-            next.k.store(tiles[(t + 1) % BUFFERS][0], a.width);
-            next.v.store(tiles[(t + 1) % BUFFERS][1], a.width);
-            kept = __ballot(next.keep != 0);
-            __syncthreads();
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (exact) {
+            walk(std::integral_constant<int, 0>{});
+            delta = halves_sum(formed);
+            if constexpr (SPLIT == 2) {
+                if (h == 0) deltas[half][wave][lane] = delta;
+                __syncthreads();
+                delta = deltas[0][wave][lane % 32] + deltas[1][wave][lane % 32];
+            }
         }
     }
-    if (some) {
+    walk(std::integral_constant<int, 1>{});
+    if (real && h == 0 && half == 0) b.delta[(size_t)head * a.T + w.i] = delta;
+    bool mine = true;
+    if constexpr (SPLIT == 2) mine = join_halves(( float*)tiles, dq, wave, half, lane);
+    if (some && mine) {
         const bool redo = not_finite(dq);
         if (real && !redo) store_column<T>(head_row<T>(b.dq, w.i, head), a.width, dq, a.scale, h);
         for (uint64_t rows = __ballot(redo && real && h == 0); rows; rows &= rows - 1) {
@@ -183,19 +257,19 @@ __global__ __launch_bounds__(THREADS, 2) void query_kernel(const BackwardArgs b)
     }
     if constexpr (BIAS) {
         if (!b.dbias) return;
-        // the outermost distances: what lies past the span in the array, then what went by registers
+        // the outermost distances: what lies past the span in the array, and what went by registers
         __syncthreads();
-        const int32_t d = lane % 32 + 1;
-        static_assert(BIAS_SIDE == 64, "two places a lane on either side");
-        low = lanes_sum<32>(low + sums[BIAS_SIDE - d] + sums[BIAS_SIDE - 32 - d]);
-        high = lanes_sum<32>(high + sums[2 * reach - BIAS_SIDE + d] + sums[2 * reach - BIAS_SIDE + 32 + d]);
-        if (lane % 32 == 0) { sums[BIAS_SIDE] += low; sums[2 * reach - BIAS_SIDE] += high; }
+        static_assert(BIAS_SIDE == 64, "one place a lane on either side");
+        low = lanes_sum<64>(low + sums[lane]);
+        high = lanes_sum<64>(high + sums[2 * reach - lane]);
+        if (lane == 0) { sums[BIAS_SIDE] += low; sums[2 * reach - BIAS_SIDE] += high; }
         __syncthreads();
         float* to = b.by_distance + ((size_t)head * words + part) * (2 * span + 1);
-        for (int32_t c = threadIdx.x; c <= 2 * span; c += THREADS) {
+        for (int32_t c = threadIdx.x; c <= 2 * span; c += SPLIT * THREADS) {
             float all = 0.f;
 #pragma unroll
-            for (int n = 0; n < 2 * THREADS / WAVE; ++n) all += dynamic[(1 + n) * (2 * reach + 1) + BIAS_SIDE + c];
+            for (int n = 0; n < SPLIT * GROUPS; ++n)
+                all += dynamic[bias_table(a.span) + n * (SKEW_FLOATS + bias_table(a.span)) + SKEW_FLOATS + BIAS_SIDE + c];
             to[c] = all;
         }
     }
@@ -207,15 +281,16 @@ __device__ inline uint32_t late_border(const BackwardArgs& b, uint32_t j) {
     return j / BLOCK_WORDS * BLOCK_WORDS + BLOCK_WORDS + b.reach;
 }
 
-template <typename T, int DB, bool BIAS>
-__global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const BackwardArgs b) {
+template <typename T, int DB, bool BIAS, int SPLIT>
+__global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 ? 2 : 1) void key_kernel(const BackwardArgs b) {
     const AttendArgs& a = b.a;
     typedef Tile<T, DB, KEYS> Tl;
-    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 64 * 1024 ? 2 : 1;
-    __shared__ __align__(16) char tiles[BUFFERS][2][Tl::BYTES];
+    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 72 * 1024 ? 2 : 1;
+    constexpr int ROOM = SPLIT == 2 ? GROUPS * DB * 16 * WAVE * 4 : 0;
+    __shared__ __align__(16) char tiles[BUFFERS * 2 * Tl::BYTES > ROOM ? BUFFERS * 2 * Tl::BYTES : ROOM];
     __shared__ float rows[BUFFERS][2][KEYS];          // the queries' logarithms to base two, and delta
     extern __shared__ float table[];
-    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE;
+    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE % GROUPS, half = threadIdx.x / THREADS;
     const uint32_t kv_head = blockIdx.x % a.kv_heads, block = blockIdx.x / a.kv_heads;
     const bool late = block < b.late;
     const int32_t reach = (int32_t)a.span + BIAS_SIDE;
@@ -285,10 +360,11 @@ __global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const Bac
 #pragma unroll
     for (int n = 0; n < DB; ++n) dk[n] = dv[n] = Acc{};
 
-    Transit<T, DB, KEYS, THREADS> tq, tg;
+    Transit<T, DB, KEYS, SPLIT * THREADS> tq, tg;
+    const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
     float lse2 = 0.f, delta = 0.f;
     const uint32_t per_head = q1 > q0 ? (q1 - q0 + KEYS - 1) / KEYS : 0, count = per_head * a.group;
-    const auto fetch = [&](uint32_t t) {
+    const auto fetch = [&](uint32_t t) __attribute__((always_inline)) {
         const uint32_t head = kv_head * a.group + t / per_head, i0 = q0 + t % per_head * KEYS;
         if (t % per_head == 0) {
             tq.start(a.q, head, q0, a.width);
@@ -302,9 +378,9 @@ __global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const Bac
             delta = b.delta[(size_t)head * a.T + i0 + threadIdx.x];
         }
     };
-    const auto put = [&](uint32_t t) {
-        tq.store(tiles[t % BUFFERS][0], a.width);
-        tg.store(tiles[t % BUFFERS][1], a.width);
+    const auto put = [&](uint32_t t) __attribute__((always_inline)) {
+        tq.store(tiles + t % BUFFERS * 2 * Tl::BYTES, a.width);
+        tg.store(tiles + t % BUFFERS * 2 * Tl::BYTES + Tl::BYTES, a.width);
         if (threadIdx.x < KEYS) {
             rows[t % BUFFERS][0][threadIdx.x] = lse2;
             rows[t % BUFFERS][1][threadIdx.x] = delta;
@@ -321,16 +397,16 @@ __global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const Bac
         }
         if (BUFFERS == 1 || t == 0 || (BIAS && t % per_head == 0)) __syncthreads();
         if (t + 1 < count) fetch(t + 1);
-        const char *qt = tiles[t % BUFFERS][0], *gt = tiles[t % BUFFERS][1];
-#pragma unroll
-        for (uint32_t piece = 0; piece < KEYS / 32; ++piece) {
+        const char *qt = tiles + t % BUFFERS * 2 * Tl::BYTES, *gt = qt + Tl::BYTES;
+        const auto one = [&](auto P) __attribute__((always_inline)) {
+            constexpr int piece = P.value;
             const uint32_t i0 = q0 + t % per_head * KEYS + piece * 32;
-            if (!some || i0 >= hi_most || i0 + 32 <= lo_least) continue;
+            if (!some || i0 >= hi_most || i0 + 32 <= lo_least) return;
             Acc s = {}, dp = {};
 #pragma unroll
             for (int k = 0; k < 2 * DB; ++k) {
-                mma(Tl::along(qt, piece * 32 + lane % 32, k, h), kf[k], s);
-                mma(Tl::along(gt, piece * 32 + lane % 32, k, h), vf[k], dp);
+                mma(Tl::along(qt, at_along, piece * 32, k), kf[k], s);
+                mma(Tl::along(gt, at_along, piece * 32, k), vf[k], dp);
             }
             const float *l2 = &rows[t % BUFFERS][0][piece * 32 + 4 * h], *dl = &rows[t % BUFFERS][1][piece * 32 + 4 * h];
             if constexpr (BIAS) {
@@ -366,16 +442,23 @@ __global__ __launch_bounds__(THREADS, DB <= 2 ? 2 : 1) void key_kernel(const Bac
                 const auto p = acc_operand<T>(s, k), ds = acc_operand<T>(dp, k);
 #pragma unroll
                 for (int n = 0; n < DB; ++n) {
-                    mma(Tl::across(gt, piece * 32, k, n, lane), p, dv[n]);
-                    mma(Tl::across(qt, piece * 32, k, n, lane), ds, dk[n]);
+                    mma(Tl::across(gt, at_across, piece * 32, k, n), p, dv[n]);
+                    mma(Tl::across(qt, at_across, piece * 32, k, n), ds, dk[n]);
                 }
             }
-        }
+        };
+        if (SPLIT == 1 || half == 0) one(std::integral_constant<int, 0>{});
+        if (SPLIT == 1 || half == 1) one(std::integral_constant<int, 1>{});
         if (t + 1 < count) {
             if (BUFFERS == 1) __syncthreads();
             put(t + 1);
             if (BUFFERS == 2) __syncthreads();
         }
+    }
+    if constexpr (SPLIT == 2) {
+        const bool mine = join_halves((float*)tiles, dk, wave, half, lane);
+        join_halves((float*)tiles, dv, wave, half, lane);
+        if (!mine) return;
     }
     if (!some) return;
 
@@ -473,11 +556,24 @@ __global__ __launch_bounds__(THREADS) void buckets_kernel(const BackwardArgs b, 
     }
 }
 
+// LDS of a block of the queries' kernel beside its tiles: the bias' table and, where its gradient is wanted, room for it.
+template <bool BIAS, int SPLIT> size_t query_room(const BackwardArgs& b) {
+    const uint32_t table = BIAS ? bias_table(b.a.span) : 0;
+    return (table + (BIAS && b.dbias ? SPLIT * GROUPS * (SKEW_FLOATS + table) : 0)) * sizeof(float);
+}
+template <typename T, int DB, bool BIAS> bool query_split(const BackwardArgs& b, uint32_t blocks) {
+    constexpr size_t tiles = 4 * Tile<T, DB, KEYS>::BYTES, joined = GROUPS * DB * 16 * WAVE * 4;      // at most
+    return blocks < SPLIT_BELOW && query_room<BIAS, 2>(b) + (tiles > joined ? tiles : joined) + 2 * BLOCK_WORDS * 4 <= LDS_BYTES;
+}
 template <typename T, int DB, bool BIAS> void backward_run(const BackwardArgs& b, hipStream_t st) {
     const AttendArgs& a = b.a;
-    const uint32_t words = attend_bias_parts(a.T), side = BIAS ? (2 * (a.span + BIAS_SIDE) + 1) * sizeof(float) : 0;
-    query_kernel<T, DB, BIAS><<<words * a.heads, THREADS, side * (b.dbias ? 1 + 2 * THREADS / WAVE : 1), st>>>(b);
-    key_kernel<T, DB, BIAS><<<(b.late + words) * a.kv_heads, THREADS, side, st>>>(b);
+    const uint32_t words = attend_bias_parts(a.T), table = BIAS ? bias_table(a.span) * sizeof(float) : 0;
+    uint32_t blocks = words * a.heads;
+    if (query_split<T, DB, BIAS>(b, blocks)) query_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, query_room<BIAS, 2>(b), st>>>(b);
+    else query_kernel<T, DB, BIAS, 1><<<blocks, THREADS, query_room<BIAS, 1>(b), st>>>(b);
+    blocks = (b.late + words) * a.kv_heads;
+    if (blocks < SPLIT_BELOW) key_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(b);
+    else key_kernel<T, DB, BIAS, 1><<<blocks, THREADS, table, st>>>(b);
 }
 template <typename T, int DB> void backward_bias(const BackwardArgs& b, hipStream_t st) {
     if (b.a.bias) backward_run<T, DB, true>(b, st);

@@ -100,50 +100,54 @@ template <typename T, int DB> __device__ __forceinline__ typename Frag<T>::vec l
     return f;
 }
 
-// ROWS rows of 32 DB elements in LDS, in chunks of 16 bytes.  Chunk c of row r lies at place c ^ turn(r) of its row: then
-// neither 16 rows' chunks c nor four rows' 64 bytes side by side -- what the two reads below ask for at a time -- meet in a bank.
+// ROWS rows of 32 DB elements in LDS.  Rows r, r + 4, r + 8 .. lie together, 16 bytes apart from each other, and the four such
+// groups 64 bytes apart: what one access takes at a time -- a chunk of 16 rows, or 64 bytes of four rows side by side -- then
+// meets in no bank, and every place is a lane's own base plus a constant.
 template <typename T, int DB, int ROWS> struct Tile {
-    static constexpr int N = pack16<T>, ROW = DB * 32 * (int)sizeof(T), CHUNKS = ROW / 16, BYTES = ROWS * ROW;
+    static constexpr int N = pack16<T>, ROW = DB * 32 * (int)sizeof(T), CHUNKS = ROW / 16;
+    static constexpr int STRIDE = ROW + 16, GROUP = ROWS / 4 * STRIDE + 64, BYTES = 4 * GROUP;
+    static_assert(ROWS % 64 == 0, "groups begin 16 banks apart");
     typedef typename Pack<T, N>::vec Chunk;
-    __device__ static __forceinline__ uint32_t turn(uint32_t r) {
-        if constexpr (CHUNKS % 16 == 0) return ((r & 3) << 2) | ((r >> 2) & 3);
-        else if constexpr (CHUNKS % 8 == 0) return ((r & 2) << 1) | ((r >> 1) & 2) | ((r >> 3) & 1);
-        else return (r >> 2) & 3;
+    __device__ static __forceinline__ uint32_t place(uint32_t r, uint32_t c) { return (r & 3) * GROUP + (r >> 2) * STRIDE + c * 16; }
+    // a lane's bases for the two reads
+    __device__ static __forceinline__ uint32_t base_along(uint32_t lane) {
+        return place(lane % 32, 0) + lane / 32 * 8 * (uint32_t)sizeof(T);
     }
-    __device__ static __forceinline__ uint32_t place(uint32_t r, uint32_t c) { return r * ROW + ((c ^ turn(r)) << 4); }
-    // rows as they are: lane's row of A, step s
-    __device__ static __forceinline__ typename Frag<T>::vec along(const char* tile, uint32_t r, int s, uint32_t h) {
+    __device__ static __forceinline__ uint32_t base_across(uint32_t lane) {
+        const uint32_t h = lane / 32;
+        if constexpr (sizeof(T) == 2)      // 16 lanes: 4 rows of 32 bytes
+            return ((lane >> 2) & 3) * GROUP + h * STRIDE + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+        else return h * STRIDE + lane % 32 * 4;
+    }
+    // rows r0 .. r0 + 31 as they are: a lane's row of A, step s
+    __device__ static __forceinline__ typename Frag<T>::vec along(const char* tile, uint32_t base, int r0, int s) {
         typename Frag<T>::vec f;
+        const char* at = tile + base + r0 / 4 * STRIDE + s * 16 * (int)sizeof(T);
 #pragma unroll
         for (int p = 0; p < 8 / N; ++p) {
-            const Chunk x = *(const Chunk*)(tile + place(r, (16 * s + 8 * h) / N + p));
+            const Chunk x = *(const Chunk*)(at + 16 * p);
 #pragma unroll
             for (int e = 0; e < N; ++e) f[p * N + e] = x[e];
         }
         return f;
     }
     // columns as rows of A: element 32 b + lane % 32 of rows r0 + 16 s + 8 (t / 4) + 4 h + t % 4
-    __device__ static __forceinline__ typename Frag<T>::vec across(const char* tile, uint32_t r0, int s, int b, uint32_t lane) {
-        typename Frag<T>::vec f;
-        const uint32_t h = lane / 32;
+    __device__ static __forceinline__ typename Frag<T>::vec across(const char* tile, uint32_t base, int r0, int s, int b) {
+        const char* at = tile + base + (r0 / 4 + 4 * s) * STRIDE + b * 32 * (int)sizeof(T);
         if constexpr (sizeof(T) == 2) {
             typedef short Four __attribute__((ext_vector_type(4)));
             union { Four part[2]; typename Frag<T>::vec f; } u;
-            const uint32_t c = 4 * b + 2 * ((lane / 16) & 1) + ((lane >> 1) & 1);      // 16 lanes: 4 rows of 32 bytes
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const uint32_t r = r0 + 16 * s + 8 * p + 4 * h + ((lane >> 2) & 3);
+            for (int p = 0; p < 2; ++p)
                 u.part[p] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) Four*)(tile + place(r, c) + 8 * (lane & 1)));
-            }
-            f = u.f;
+                    (__attribute__((address_space(3))) Four*)(at + 2 * p * STRIDE));
+            return u.f;
         } else {
-            const uint32_t at = 32 * b + lane % 32;
+            typename Frag<T>::vec f;
 #pragma unroll
-            for (int t = 0; t < 8; ++t)
-                f[t] = *(const T*)(tile + place(r0 + 16 * s + 8 * (t / 4) + 4 * h + t % 4, at / N) + (at % N) * sizeof(T));
+            for (int t = 0; t < 8; ++t) f[t] = *(const T*)(at + 2 * (t / 4) * STRIDE + t % 4 * GROUP);
+            return f;
         }
-        return f;
     }
 };
 
@@ -152,7 +156,7 @@ template <typename T, int DB, int ROWS> struct Tile {
 template <typename T, int DB, int ROWS, int THREADS> struct Transit {
     typedef Tile<T, DB, ROWS> Tl;
     static constexpr uint32_t LANES = Tl::CHUNKS <= 4 ? 4 : Tl::CHUNKS <= 8 ? 8 : Tl::CHUNKS <= 16 ? 16 : 32;
-    static constexpr uint32_t RS = THREADS / LANES, PER = ROWS / RS;
+    static constexpr uint32_t RS = THREADS / LANES < ROWS ? THREADS / LANES : ROWS, PER = ROWS / RS;      // (threads past the rows: idle)
     typename Tl::Chunk x[PER];
     const T* at;                                      // the chunk of the thread's first row in the tile to be read next
     uint64_t stride;
@@ -162,7 +166,7 @@ template <typename T, int DB, int ROWS, int THREADS> struct Transit {
     __device__ __forceinline__ void start(const Heads& p, uint32_t head, int64_t token, uint32_t width) {
         r0 = threadIdx.x / LANES;
         c0 = threadIdx.x % LANES * Tl::N;
-        mine = c0 < width;
+        mine = c0 < width && r0 < (uint32_t)ROWS;
         stride = p.token;
         at = (const T*)p.p + (uint64_t)head * p.head + (token + r0) * (int64_t)p.token;
 #pragma unroll
@@ -192,7 +196,7 @@ template <typename T, int DB, int ROWS, int THREADS> struct Transit {
         at += ROWS * stride;
     }
     __device__ __forceinline__ void store(char* tile, uint32_t width) {
-        if (c0 >= (uint32_t)Tl::CHUNKS * Tl::N) return;
+        if (c0 >= (uint32_t)Tl::CHUNKS * Tl::N || r0 >= (uint32_t)ROWS) return;
         if (width % Tl::N)
 #pragma unroll
             for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_fit<T>(x[n], c0, width);
