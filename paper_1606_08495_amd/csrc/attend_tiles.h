@@ -124,20 +124,23 @@ template <typename T, int DB, int SPLIT> struct KeyTiles {
     Transit<T, DB, KEYS, SPLIT * THREADS> k, v;
     uint8_t keep;
     __device__ __forceinline__ void start(const AttendArgs& a, uint32_t kv_head, const Axis& x) {
-        k.start(a.k, kv_head, (int64_t)(int32_t)x.shift, a.width);
-        v.start(a.v, kv_head, (int64_t)(int32_t)x.shift, a.width);
+        k.start(a.k, kv_head, (int64_t)(int32_t)x.shift);
+        v.start(a.v, kv_head, (int64_t)(int32_t)x.shift);
         keep = 1;
     }
     __device__ __forceinline__ void fetch(const AttendArgs& a, uint32_t kv_head, const Axis& x, uint32_t t, uint32_t lane) {
-        const uint32_t rows = x.count - t * KEYS;
-        if (t * KEYS >= x.sunk) {
-            k.load(rows, a.width);
-            v.load(rows, a.width);
+        const uint32_t n0 = t * KEYS, last = x.count - 1;
+        if (n0 >= x.sunk && n0 + KEYS <= x.count) {
+            k.aim();
+            v.aim();
         } else {
-            k.load_rows([&](uint32_t r) { return head_row<T>(a.k, x.token(t * KEYS + r), kv_head); }, rows, a.width);
-            v.load_rows([&](uint32_t r) { return head_row<T>(a.v, x.token(t * KEYS + r), kv_head); }, rows, a.width);
+            const auto token = [&](uint32_t r) __attribute__((always_inline)) { return x.token(n0 + r < last ? n0 + r : last); };
+            k.aim(token);
+            v.aim(token);
         }
-        if (a.keep) keep = lane < rows ? a.keep[x.token(t * KEYS + lane)] : 0;
+        k.load(a.width);
+        v.load(a.width);
+        if (a.keep) keep = a.keep[x.token(n0 + lane < last ? n0 + lane : last)];
     }
 };
 

@@ -367,22 +367,28 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     const auto fetch = [&](uint32_t t) __attribute__((always_inline)) {
         const uint32_t head = kv_head * a.group + t / per_head, i0 = q0 + t % per_head * KEYS;
         if (t % per_head == 0) {
-            tq.start(a.q, head, q0, a.width);
-            tg.start(b.dout, head, q0, a.width);
+            tq.start(a.q, head, q0);
+            tg.start(b.dout, head, q0);
         }
-        tq.load(q1 - i0, a.width);
-        tg.load(q1 - i0, a.width);
-        if (threadIdx.x < KEYS && i0 + threadIdx.x < q1) {
-            const float l = a.lse[(size_t)head * a.T + i0 + threadIdx.x];
-            lse2 = l == -__builtin_inff() ? 0.f : l * LOG2E;
-            delta = b.delta[(size_t)head * a.T + i0 + threadIdx.x];
+        if (i0 + KEYS <= q1) {
+            tq.aim();
+            tg.aim();
+        } else {
+            const auto token = [&](uint32_t r) __attribute__((always_inline)) { return i0 + r < q1 ? i0 + r : q1 - 1; };
+            tq.aim(token);
+            tg.aim(token);
         }
+        tq.load(a.width);
+        tg.load(a.width);
+        const uint32_t i = i0 + threadIdx.x % KEYS < q1 ? i0 + threadIdx.x % KEYS : q1 - 1;
+        lse2 = a.lse[(size_t)head * a.T + i];
+        delta = b.delta[(size_t)head * a.T + i];
     };
     const auto put = [&](uint32_t t) __attribute__((always_inline)) {
         tq.store(tiles + t % BUFFERS * 2 * Tl::BYTES, a.width);
         tg.store(tiles + t % BUFFERS * 2 * Tl::BYTES + Tl::BYTES, a.width);
         if (threadIdx.x < KEYS) {
-            rows[t % BUFFERS][0][threadIdx.x] = lse2;
+            rows[t % BUFFERS][0][threadIdx.x] = lse2 == -__builtin_inff() ? 0.f : lse2 * LOG2E;
             rows[t % BUFFERS][1][threadIdx.x] = delta;
         }
     };

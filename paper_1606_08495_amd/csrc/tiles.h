@@ -52,37 +52,38 @@ __device__ __forceinline__ float halves_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Chunks: 16 bytes of a row of `width` elements, from element c0 on, zeros past the row's end.  The chunk that the end cuts is
-// read as the row's last 16 bytes and moved down afterwards (chunk_fit), so that no access leaves the row and none waits for
-// another; rows shorter than a chunk are read by elements.
+// Chunks: 16 bytes of a row of `width` elements, from element c0 on.  What lies past the row's end is not read: the chunk that
+// the end cuts is read as the row's last 16 bytes and moved down afterwards (chunk_fit), and so are chunks wholly past it.
+// No access depends on a condition, so that none waits for another.  Rows shorter than a chunk (where NARROW allows
+// them) are read by elements.
 template <typename T, bool NARROW> __device__ __forceinline__ typename Pack<T, pack16<T>>::vec chunk_read(const T* row, uint32_t c0, uint32_t width) {
     constexpr uint32_t N = pack16<T>;
-    typename Pack<T, N>::vec x = {};
-    if (!NARROW || width >= N) {
-        if (c0 < width) x = *(const typename Pack<T, N>::mem*)(row + (c0 < width - N ? c0 : width - N));
-    } else if (c0 == 0) {
+    if (NARROW && width < N) {
+        typename Pack<T, N>::vec x;
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) if (e < width) x[e] = row[e];
+        for (uint32_t e = 0; e < N; ++e) x[e] = row[e < width ? e : width - 1];
+        return x;
     }
-    return x;
+    return *(const typename Pack<T, N>::mem*)(row + (c0 < width - N ? c0 : width - N));
 }
 template <typename T>
 __device__ __forceinline__ typename Pack<T, pack16<T>>::vec chunk_fit(typename Pack<T, pack16<T>>::vec x, uint32_t c0, uint32_t width) {
     constexpr uint32_t N = pack16<T>;
-    if (width >= N && width % N) {
-        const bool cut = c0 < width && c0 + N > width;
-        const uint32_t by = cut ? (c0 + N - width) * (uint32_t)sizeof(T) : 0;      // bytes to move down by
-        typedef uint32_t Words __attribute__((ext_vector_type(4)));
-        Words w = __builtin_bit_cast(Words, x);
-        const bool two = by & 8, one = by & 4, half = by & 2;
-        w = Words{two ? w[2] : w[0], two ? w[3] : w[1], two ? 0u : w[2], two ? 0u : w[3]};
-        w = Words{one ? w[1] : w[0], one ? w[2] : w[1], one ? w[3] : w[2], one ? 0u : w[3]};
-        if constexpr (sizeof(T) == 2) {
-            const Words u = {w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
-            w = Words{half ? u[0] : w[0], half ? u[1] : w[1], half ? u[2] : w[2], half ? u[3] : w[3]};
-        }
-        x = __builtin_bit_cast(typename Pack<T, N>::vec, w);
+    const uint32_t start = width >= N && c0 > width - N ? width - N : c0;
+    const uint32_t by = (c0 - start) * (uint32_t)sizeof(T);      // bytes to move down by
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    Words w = __builtin_bit_cast(Words, x);
+    const bool two = by & 8, one = by & 4, half = by & 2;
+    w = Words{two ? w[2] : w[0], two ? w[3] : w[1], two ? 0u : w[2], two ? 0u : w[3]};
+    w = Words{one ? w[1] : w[0], one ? w[2] : w[1], one ? w[3] : w[2], one ? 0u : w[3]};
+    if constexpr (sizeof(T) == 2) {
+        const Words u = {w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+        w = Words{half ? u[0] : w[0], half ? u[1] : w[1], half ? u[2] : w[2], half ? u[3] : w[3]};
     }
+    x = __builtin_bit_cast(typename Pack<T, N>::vec, w);
+    if (c0 + N > width)
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) x[e] = c0 + e < width ? x[e] : (T)0.f;
     return x;
 }
 
@@ -152,56 +153,48 @@ template <typename T, int DB, int ROWS> struct Tile {
 };
 
 // A tile's rows on their way from memory to LDS, in the registers of THREADS threads: a thread keeps one chunk's column and
-// every RS-th row.  Rows past the last are not read and keep what was there: they are masked.
+// every RS-th row.  (Rows past the last one are copies of it, columns past the width of the last ones: the former are
+// masked, the latter meet zeros or give columns that nobody reads.)
 template <typename T, int DB, int ROWS, int THREADS> struct Transit {
     typedef Tile<T, DB, ROWS> Tl;
     static constexpr uint32_t LANES = Tl::CHUNKS <= 4 ? 4 : Tl::CHUNKS <= 8 ? 8 : Tl::CHUNKS <= 16 ? 16 : 32;
     static constexpr uint32_t RS = THREADS / LANES < ROWS ? THREADS / LANES : ROWS, PER = ROWS / RS;      // (threads past the rows: idle)
     typename Tl::Chunk x[PER];
-    const T* at;                                      // the chunk of the thread's first row in the tile to be read next
+    const T* at[PER];                                 // what is to be read next
+    const T* base;                                    // the head's row of token 0
+    const T* tile;                                    // this thread's first row of the next tile, if all its rows follow each other
     uint64_t stride;
     uint32_t r0, c0;
-    bool mine;
     // row 0 of the first tile is token `token` (which may lie before the first, where no such row is read)
-    __device__ __forceinline__ void start(const Heads& p, uint32_t head, int64_t token, uint32_t width) {
-        r0 = threadIdx.x / LANES;
+    __device__ __forceinline__ void start(const Heads& p, uint32_t head, int64_t token) {
+        r0 = threadIdx.x / LANES % ROWS;
         c0 = threadIdx.x % LANES * Tl::N;
-        mine = c0 < width && r0 < (uint32_t)ROWS;
         stride = p.token;
-        at = (const T*)p.p + (uint64_t)head * p.head + (token + r0) * (int64_t)p.token;
-#pragma unroll
-        for (uint32_t n = 0; n < PER; ++n) x[n] = typename Tl::Chunk{};
+        base = (const T*)p.p + (uint64_t)head * p.head;
+        tile = base + (token + r0) * (int64_t)stride;
     }
-    __device__ __forceinline__ void read(uint32_t n, const T* row, uint32_t width) {
-        constexpr uint32_t N = Tl::N;
-        if (DB == 1 && width < N) x[n] = chunk_read<T, true>(row, c0, width);
-        else x[n] = *(const typename Pack<T, N>::mem*)(row + (c0 < width - N ? c0 : width - N));
-    }
-    // the tile's first `rows` rows, then on to the next tile
-    __device__ __forceinline__ void load(uint32_t rows, uint32_t width) {
-        if (rows >= (uint32_t)ROWS) {
-            if (mine)
+    // a whole tile whose rows follow each other
+    __device__ __forceinline__ void aim() {
 #pragma unroll
-                for (uint32_t n = 0; n < PER; ++n) read(n, at + n * RS * stride, width);
-        } else {
-#pragma unroll
-            for (uint32_t n = 0; n < PER; ++n) if (mine && r0 + n * RS < rows) read(n, at + n * RS * stride, width);
-        }
-        at += ROWS * stride;
+        for (uint32_t n = 0; n < PER; ++n) at[n] = tile + n * RS * stride;
     }
-    // the same where row r lies at row(r)
-    template <typename F> __device__ __forceinline__ void load_rows(const F& row, uint32_t rows, uint32_t width) {
+    // row r is token(r)
+    template <typename F> __device__ __forceinline__ void aim(const F& token) {
 #pragma unroll
-        for (uint32_t n = 0; n < PER; ++n) if (mine && r0 + n * RS < rows) read(n, row(r0 + n * RS), width);
-        at += ROWS * stride;
+        for (uint32_t n = 0; n < PER; ++n) at[n] = base + (uint64_t)token(r0 + n * RS) * stride;
     }
-    __device__ __forceinline__ void store(char* tile, uint32_t width) {
-        if (c0 >= (uint32_t)Tl::CHUNKS * Tl::N || r0 >= (uint32_t)ROWS) return;
+    __device__ __forceinline__ void load(uint32_t width) {
+#pragma unroll
+        for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_read<T, DB == 1>(at[n], c0, width);
+        tile += ROWS * stride;
+    }
+    __device__ __forceinline__ void store(char* to, uint32_t width) {
+        if (c0 >= (uint32_t)Tl::CHUNKS * Tl::N || threadIdx.x / LANES >= (uint32_t)ROWS) return;
         if (width % Tl::N)
 #pragma unroll
             for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_fit<T>(x[n], c0, width);
 #pragma unroll
-        for (uint32_t n = 0; n < PER; ++n) *(typename Tl::Chunk*)(tile + Tl::place(r0 + n * RS, c0 / Tl::N)) = x[n];
+        for (uint32_t n = 0; n < PER; ++n) *(typename Tl::Chunk*)(to + Tl::place(r0 + n * RS, c0 / Tl::N)) = x[n];
     }
 };
 
