@@ -1,5 +1,7 @@
 // What the tiled attention kernels share: the words of a wavefront, the axis of keys they walk over, scores with bias and mask.
 #pragma once
+#include <type_traits>
+
 #include "attend.h"
 #include "tiles.h"
 
@@ -9,7 +11,21 @@ constexpr int BLOCK_WORDS = 128, WAVE_WORDS = 32, KEYS = 64, THREADS = 256, GROU
 
 // Where there are fewer blocks than this, a block has twice the wavefronts, and each takes one of a tile's two pieces.
 constexpr uint32_t SPLIT_BELOW = 512;
+// (Not for wide heads in 32 bits, whose registers would not hold for the second wavefront on a SIMD.)
+template <typename T, int DB> constexpr bool splits = sizeof(T) == 2 || DB <= 2;
 constexpr size_t LDS_BYTES = 160 * 1024;              // a block's most
+
+// A block's wavefront: which group of 32 words it has, and which half of a tile where it has one.
+struct Place {
+    uint32_t lane, h, wave, half;
+    __device__ __forceinline__ Place() {
+        const uint32_t n = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+        lane = threadIdx.x % WAVE;
+        h = lane / 32;
+        wave = n % GROUPS;
+        half = n / GROUPS;
+    }
+};
 
 // The texts of a block's first and last token and of a wavefront's.
 struct Texts {
@@ -77,6 +93,13 @@ __device__ __forceinline__ void fill_bias(const AttendArgs& a, uint32_t head, fl
     for (int32_t at = threadIdx.x; at <= 2 * reach; at += (int32_t)blockDim.x) table[at] = scaled_bias(a, head, at - reach);
 }
 
+// A value that is computed where it is used, piece by piece: what sixteen rows derive from it is not kept in registers of
+// its own over the whole walk.
+__device__ __forceinline__ uint32_t per_piece(uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // Scores of a piece of 32 keys, masked: s on the way in holds the products.  With a bias they are to base two, without one
 // they still lack the scale, which is positive.
 template <bool BIAS>
@@ -103,20 +126,25 @@ __device__ __forceinline__ void piece_scores(const AttendArgs& a, const Words& w
         } else {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int32_t dist = (int32_t)x.token(n0 + acc_row(r, h)) - (int32_t)w.i;
+                const int32_t dist = (int32_t)x.token(per_piece(n0 + 4 * h) + acc_row(r, 0)) - (int32_t)w.i;
                 s[r] = fmaf(s[r], a.scale2, table[(dist < -reach ? -reach : dist > reach ? reach : dist) + reach]);
             }
         }
     }
     if (all) return;
+    const auto mask = [&](auto LINEAR) __attribute__((always_inline)) {
+        const uint32_t base = per_piece((LINEAR.value ? j0 : n0) + 4 * h);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const uint32_t row = acc_row(r, h), j = linear ? j0 + row : x.token(n0 + row);
-        bool in = (j - w.s.lo < w.s.hi - w.s.lo) | (j - w.s.first < w.s.sunk - w.s.first);
-        in &= (kept32 >> row & 1) != 0;
-        in &= !(a.skip_self && j == w.i);
-        s[r] = in ? s[r] : -__builtin_inff();
-    }
+        for (int r = 0; r < 16; ++r) {
+            const uint32_t j = LINEAR.value ? base + acc_row(r, 0) : x.token(base + acc_row(r, 0));
+            bool in = (j - w.s.lo < w.s.hi - w.s.lo) | (j - w.s.first < w.s.sunk - w.s.first);
+            in &= (kept32 >> acc_row(r, h) & 1) != 0;
+            in &= !(a.skip_self & (j == w.i));
+            s[r] = in ? s[r] : -__builtin_inff();
+        }
+    };
+    if (linear) mask(std::true_type{});
+    else mask(std::false_type{});
 }
 
 // Keys and values of a block, tile by tile from memory to LDS, and which of the next tile's words are kept.

@@ -14,8 +14,6 @@
 // leaves them the relative rounding that v has; their sum is taken before the rounding.  Heads of up to 32 columns add
 // what the rounding left in a second product: the gradient's dout . out is then a sum of few terms, which
 // may cancel down to the weights' rounding, and the matrix cores wait for the exponentials there anyway.
-#include <type_traits>
-
 #include "attend_tiles.h"
 
 namespace w2v {
@@ -24,14 +22,15 @@ namespace {
 constexpr float RISE = 8.f;           // how far (to base two) a maximum may rise before outputs are rescaled
 
 template <typename T, int DB, bool BIAS, int SPLIT>
-__global__ __launch_bounds__(SPLIT * THREADS, 2) void attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void attend_kernel(const AttendArgs a) {
     typedef Tile<T, DB, KEYS> Tl;
     constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 72 * 1024 ? 2 : 1, KEEP = DB * 16 + 2;
-    constexpr bool JOINT = sizeof(T) == 2 || DB <= 2;      // both pieces of a tile at a time, where registers allow
+    constexpr bool JOINT = DB <= 2;      // both pieces of a tile at a time, where registers allow
     __shared__ __align__(16) char tiles[BUFFERS][2][Tl::BYTES];
     static_assert(SPLIT == 1 || GROUPS * KEEP * WAVE * 4 <= (int)sizeof(tiles), "room to join the halves");
     extern __shared__ float table[];
-    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE % GROUPS, half = threadIdx.x / THREADS;
+    const Place place;
+    const uint32_t lane = place.lane, h = place.h, wave = place.wave, half = place.half;
     const uint32_t head = blockIdx.x % a.heads, kv_head = head / a.group;
     const uint32_t words = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS;
     const uint32_t word0 = (words - 1 - blockIdx.x / a.heads) * BLOCK_WORDS;      // those that may see most first
@@ -51,7 +50,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, 2) void attend_kernel(const Attend
     for (int b = 0; b < DB; ++b) o[b] = Acc{};
     float m = -__builtin_inff(), total = 0.f;
     const float unit = BIAS ? 1.f : a.scale2;         // of the scores as piece_scores leaves them
-    const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
+    // a half's piece of every tile is the same one: its rows are part of the lane's bases
+    const uint32_t own_rows = SPLIT == 2 ? half * 32 : 0;
+    const uint32_t at_along = Tl::base_along(lane) + own_rows / 4 * Tl::STRIDE, at_across = Tl::base_across(lane) + own_rows / 4 * Tl::STRIDE;
 
     KeyTiles<T, DB, SPLIT> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
@@ -79,8 +80,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, 2) void attend_kernel(const Attend
             float most = -__builtin_inff();
 #pragma unroll
             for (int p = 0; p < P.value; ++p) {
-                const uint32_t n0 = t * KEYS + (p0 + p) * 32;
-                piece_scores<BIAS>(a, w, x, n0, kept >> ((p0 + p) * 32), n0 >= x.sunk, table, h, s[p]);
+                const uint32_t n0 = t * KEYS + (p0 + p) * 32 + own_rows;
+                piece_scores<BIAS>(a, w, x, n0, kept >> ((p0 + p) * 32 + own_rows), n0 >= x.sunk, table, h, s[p]);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[p][r]);
             }
@@ -95,37 +96,36 @@ __global__ __launch_bounds__(SPLIT * THREADS, 2) void attend_kernel(const Attend
             }
             const float base = m == -__builtin_inff() ? 0.f : m;
 #pragma unroll
-            for (int p = 0; p < P.value; ++p) {
+            for (int g = 0; g < 2 * P.value; ++g) {   // 16 keys
+                const int p = g / 2;
+                typename Frag<T>::vec e;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[p][r] = __builtin_amdgcn_exp2f(fmaf(s[p][r], unit, -base));
-                    total += s[p][r];
+                for (int c = 0; c < 8; ++c) {
+                    const float y = __builtin_amdgcn_exp2f(fmaf(s[p][8 * (g % 2) + c], unit, -base));
+                    total += y;
+                    e[c] = (T)y;
+                    s[p][8 * (g % 2) + c] = y;
                 }
+                typename Frag<T>::vec v[DB];
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const auto e = acc_operand<T>(s[p], k);
-                    typename Frag<T>::vec v[DB];
+                for (int b = 0; b < DB; ++b) {
+                    v[b] = Tl::across(vt, at_across, (p0 + p) * 32, g % 2, b);
+                    mma(v[b], e, o[b]);
+                }
+                if constexpr (sizeof(T) == 2 && DB == 1) {      // what the rounding left of the weights
+                    typename Frag<T>::vec rest;
 #pragma unroll
-                    for (int b = 0; b < DB; ++b) {
-                        v[b] = Tl::across(vt, at_across, (p0 + p) * 32, k, b);
-                        mma(v[b], e, o[b]);
-                    }
-                    if constexpr (sizeof(T) == 2 && DB == 1) {      // what the rounding left of the weights
-                        typename Frag<T>::vec rest;
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) rest[c] = (T)(s[p][8 * k + c] - (float)e[c]);
-                        mma(v[0], rest, o[0]);
-                    }
+                    for (int c = 0; c < 8; ++c) rest[c] = (T)(s[p][8 * (g % 2) + c] - (float)e[c]);
+                    mma(v[0], rest, o[0]);
                 }
             }
         };
         const auto needs = [&](uint32_t piece) __attribute__((always_inline)) {
-            const uint32_t n0 = t * KEYS + piece * 32;
+            const uint32_t n0 = t * KEYS + piece * 32 + own_rows;
             return some && n0 < x.count && (n0 < x.sunk || w.shown_any(n0 + x.shift));
         };
         if constexpr (SPLIT == 2) {
-            if (half == 0) { if (needs(0)) pieces(std::integral_constant<int, 1>{}, 0); }
-            else if (needs(1)) pieces(std::integral_constant<int, 1>{}, 1);
+            if (needs(0)) pieces(std::integral_constant<int, 1>{}, 0);
         } else {
             const bool n0 = needs(0), n1 = needs(1);
             if (JOINT && n0 && n1) pieces(std::integral_constant<int, JOINT ? 2 : 1>{}, 0);
@@ -217,8 +217,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, 2) void attend_kernel(const Attend
 
 template <typename T, int DB, bool BIAS> void attend_bias(const AttendArgs& a, hipStream_t st) {
     const uint32_t blocks = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS * a.heads, table = BIAS ? bias_table(a.span) * sizeof(float) : 0;
-    if (blocks < SPLIT_BELOW) attend_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(a);
-    else attend_kernel<T, DB, BIAS, 1><<<blocks, THREADS, table, st>>>(a);
+    if constexpr (splits<T, DB>)
+        if (blocks < SPLIT_BELOW) return attend_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(a);
+    attend_kernel<T, DB, BIAS, 1><<<blocks, THREADS, table, st>>>(a);
 }
 template <typename T, int DB> void attend_run(const AttendArgs& a, hipStream_t st) {
     if (a.bias) attend_bias<T, DB, true>(a, st);

@@ -12,8 +12,6 @@
 // A text's first words that stay visible are seen by every later word.  The keys' kernel takes the queries up to a
 // border behind its block; those behind go in pieces to blocks of their own (late), whose sums are joined in
 // order at the end.
-#include <type_traits>
-
 #include "attend_tiles.h"
 
 namespace w2v {
@@ -76,7 +74,7 @@ constexpr uint32_t EXACT_KEYS = 512;
 constexpr int SKEW = 64, SKEW_FLOATS = 32 * SKEW;
 
 template <typename T, int DB, bool BIAS, int SPLIT>
-__global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) void query_kernel(const BackwardArgs b) {
+__global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void query_kernel(const BackwardArgs b) {
     const AttendArgs& a = b.a;
     typedef Tile<T, DB, KEYS> Tl;
     constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= (BIAS ? 40 : 72) * 1024 ? 2 : 1;
@@ -85,7 +83,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) 
     __shared__ float deltas[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS];
     extern __shared__ float dynamic[];
     const int32_t span = (int32_t)a.span, reach = span + BIAS_SIDE;
-    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE % GROUPS, half = threadIdx.x / THREADS;
+    const Place place;
+    const uint32_t lane = place.lane, h = place.h, wave = place.wave, half = place.half;
     const uint32_t head = blockIdx.x % a.heads, kv_head = head / a.group;
     const uint32_t words = (a.T + BLOCK_WORDS - 1) / BLOCK_WORDS;
     const uint32_t part = words - 1 - blockIdx.x / a.heads, word0 = part * BLOCK_WORDS;
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) 
     const Axis x(a, word0, last, texts);
     w.find(a, texts, lane);
     float* const table = dynamic;
-    float* const skew = dynamic + bias_table(a.span) + threadIdx.x / WAVE * (SKEW_FLOATS + bias_table(a.span));
+    float* const skew = dynamic + bias_table(a.span) + (half * GROUPS + wave) * (SKEW_FLOATS + bias_table(a.span));
     float* const sums = skew + SKEW_FLOATS;
     if (BIAS) {
         fill_bias(a, head, table);
@@ -124,7 +123,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) 
     for (int n = 0; n < DB; ++n) dq[n] = Acc{};
     float low = 0.f, high = 0.f;
     const float unit = BIAS ? 1.f : a.scale2;
-    const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
+    // a half's piece of every tile is the same one: its rows are part of the lane's bases
+    const uint32_t own_rows = SPLIT == 2 ? half * 32 : 0;
+    const uint32_t at_along = Tl::base_along(lane) + own_rows / 4 * Tl::STRIDE, at_across = Tl::base_across(lane) + own_rows / 4 * Tl::STRIDE;
 
     KeyTiles<T, DB, SPLIT> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) 
             const char *kt = tiles + t % BUFFERS * 2 * Tl::BYTES, *vt = kt + Tl::BYTES;
             const auto one = [&](auto P) __attribute__((always_inline)) {
                 constexpr int piece = P.value;
-                const uint32_t n0 = t * KEYS + piece * 32, j0 = n0 + x.shift;
+                const uint32_t n0 = t * KEYS + piece * 32 + own_rows, j0 = n0 + x.shift;
                 const bool linear = n0 >= x.sunk;
                 if (!some || n0 >= x.count || (linear && !w.shown_any(j0))) return;
                 Acc s = {}, dp = {};
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) 
                     mma(Tl::along(kt, at_along, piece * 32, k), q[k], s);
                     mma(Tl::along(vt, at_along, piece * 32, k), g[k], dp);
                 }
-                piece_scores<BIAS>(a, w, x, n0, kept >> (piece * 32), linear, table, h, s);
+                piece_scores<BIAS>(a, w, x, n0, kept >> (piece * 32 + own_rows), linear, table, h, s);
                 if constexpr (pass == 0) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) 
 // the piece where the first words and the window meet: one half after the other, no place twice at a time
 #pragma unroll
                             for (int r = 0; r < 16; ++r) {
-                                const int32_t dist = (int32_t)x.token(n0 + acc_row(r, h)) - (int32_t)w.i;
+                                const int32_t dist = (int32_t)x.token(per_piece(n0 + 4 * h) + acc_row(r, 0)) - (int32_t)w.i;
                                 const bool inside = dist > -span && dist < span;
                                 low += dist <= -span ? s[r] : 0.f;
                                 high += dist >= span ? s[r] : 0.f;
@@ -212,8 +213,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, sizeof(T) == 4 && DB > 2 ? 1 : 2) 
                     for (int n = 0; n < DB; ++n) mma(Tl::across(kt, at_across, piece * 32, k, n), ds, dq[n]);
                 }
             };
-            if (SPLIT == 1 || half == 0) one(std::integral_constant<int, 0>{});
-            if (SPLIT == 1 || half == 1) one(std::integral_constant<int, 1>{});
+            one(std::integral_constant<int, 0>{});
+            if constexpr (SPLIT == 1) one(std::integral_constant<int, 1>{});
             if (t + 1 < count) {
                 if (BUFFERS == 1) __syncthreads();
                 char* const to = tiles + (t + 1) % BUFFERS * 2 * Tl::BYTES;
@@ -288,9 +289,14 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= 72 * 1024 ? 2 : 1;
     constexpr int ROOM = SPLIT == 2 ? GROUPS * DB * 16 * WAVE * 4 : 0;
     __shared__ __align__(16) char tiles[BUFFERS * 2 * Tl::BYTES > ROOM ? BUFFERS * 2 * Tl::BYTES : ROOM];
+    // wide heads: the block's own keys and values as operands from LDS, registers do not hold them beside the sums
+    constexpr bool OWN = SPLIT == 2 && DB * sizeof(T) >= 6;
+    typedef Tile<T, DB, BLOCK_WORDS> Ow;
+    __shared__ __align__(16) char own[OWN ? 2 * Ow::BYTES : 16];
     __shared__ float rows[BUFFERS][2][KEYS];          // the queries' logarithms to base two, and delta
     extern __shared__ float table[];
-    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = threadIdx.x / WAVE % GROUPS, half = threadIdx.x / THREADS;
+    const Place place;
+    const uint32_t lane = place.lane, h = place.h, wave = place.wave, half = place.half;
     const uint32_t kv_head = blockIdx.x % a.kv_heads, block = blockIdx.x / a.kv_heads;
     const bool late = block < b.late;
     const int32_t reach = (int32_t)a.span + BIAS_SIDE;
@@ -314,12 +320,26 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     const bool some = wave0 < k1, real = wave0 + lane % WAVE_WORDS < k1;
     const uint32_t j_first = some ? wave0 : k1 - 1, j_last = wave0 + WAVE_WORDS - 1 < k1 ? wave0 + WAVE_WORDS - 1 : k1 - 1;
     const uint32_t j = real ? wave0 + lane % WAVE_WORDS : k1 - 1;
-    typename Frag<T>::vec kf[2 * DB], vf[2 * DB];
+    typename Frag<T>::vec kf[OWN ? 1 : 2 * DB], vf[OWN ? 1 : 2 * DB];
+    if constexpr (OWN) {
+        Transit<T, DB, BLOCK_WORDS, SPLIT * THREADS> t;
+        const auto token = [&](uint32_t r) __attribute__((always_inline)) { return k0 + r < k1 ? k0 + r : k1 - 1; };
+        t.start(a.k, kv_head, k0);
+        t.aim(token);
+        t.load(a.width);
+        t.template store<true>(own, a.width);
+        t.start(a.v, kv_head, k0);
+        t.aim(token);
+        t.load(a.width);
+        t.template store<true>(own + Ow::BYTES, a.width);
+    } else {
 #pragma unroll
-    for (int s = 0; s < 2 * DB; ++s) {
-        kf[s] = load_operand<T, DB>(head_row<T>(a.k, j, kv_head), s, h, a.width);
-        vf[s] = load_operand<T, DB>(head_row<T>(a.v, j, kv_head), s, h, a.width);
+        for (int s = 0; s < 2 * DB; ++s) {
+            kf[s] = load_operand<T, DB>(head_row<T>(a.k, j, kv_head), s, h, a.width);
+            vf[s] = load_operand<T, DB>(head_row<T>(a.v, j, kv_head), s, h, a.width);
+        }
     }
+    const uint32_t own_base = Ow::base_along(lane) + wave * (WAVE_WORDS / 4) * Ow::STRIDE;
     const bool keep = !(a.keep && !a.keep[j]);
     const Texts texts(a, k0, k1 - 1, j_first, j_last, lane);
     const Text text = text_between(a.off, texts.wave_first, texts.wave_last, j, a.T, lane);
@@ -361,7 +381,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     for (int n = 0; n < DB; ++n) dk[n] = dv[n] = Acc{};
 
     Transit<T, DB, KEYS, SPLIT * THREADS> tq, tg;
-    const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
+    // a half's piece of every tile is the same one: its rows are part of the lane's bases
+    const uint32_t own_rows = SPLIT == 2 ? half * 32 : 0;
+    const uint32_t at_along = Tl::base_along(lane) + own_rows / 4 * Tl::STRIDE, at_across = Tl::base_across(lane) + own_rows / 4 * Tl::STRIDE;
     float lse2 = 0.f, delta = 0.f;
     const uint32_t per_head = q1 > q0 ? (q1 - q0 + KEYS - 1) / KEYS : 0, count = per_head * a.group;
     const auto fetch = [&](uint32_t t) __attribute__((always_inline)) {
@@ -406,15 +428,22 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
         const char *qt = tiles + t % BUFFERS * 2 * Tl::BYTES, *gt = qt + Tl::BYTES;
         const auto one = [&](auto P) __attribute__((always_inline)) {
             constexpr int piece = P.value;
-            const uint32_t i0 = q0 + t % per_head * KEYS + piece * 32;
+            const uint32_t i0 = q0 + t % per_head * KEYS + piece * 32 + own_rows;
             if (!some || i0 >= hi_most || i0 + 32 <= lo_least) return;
             Acc s = {}, dp = {};
+            const uint32_t at_own = per_piece(own_base);      // (what does not change is not kept in registers)
 #pragma unroll
             for (int k = 0; k < 2 * DB; ++k) {
-                mma(Tl::along(qt, at_along, piece * 32, k), kf[k], s);
-                mma(Tl::along(gt, at_along, piece * 32, k), vf[k], dp);
+                if constexpr (OWN) {
+                    mma(Tl::along(qt, at_along, piece * 32, k), Ow::along(own, at_own, 0, k), s);
+                    mma(Tl::along(gt, at_along, piece * 32, k), Ow::along(own + Ow::BYTES, at_own, 0, k), dp);
+                } else {
+                    mma(Tl::along(qt, at_along, piece * 32, k), kf[k], s);
+                    mma(Tl::along(gt, at_along, piece * 32, k), vf[k], dp);
+                }
             }
-            const float *l2 = &rows[t % BUFFERS][0][piece * 32 + 4 * h], *dl = &rows[t % BUFFERS][1][piece * 32 + 4 * h];
+            __builtin_amdgcn_sched_barrier(0);        // (what the next products read is not asked for before: registers)
+            const float *l2 = &rows[t % BUFFERS][0][piece * 32 + own_rows + 4 * h], *dl = l2 + KEYS;
             if constexpr (BIAS) {
                 const int32_t far = (int32_t)j_last - (int32_t)i0, near = (int32_t)j_first - (int32_t)i0 - 31;
                 if (far <= -(int32_t)a.span || near >= (int32_t)a.span) {
@@ -431,10 +460,11 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
                 for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, -l2[acc_row(r, 0)]);
             }
             if (!(i0 >= lo_most && i0 + 32 <= hi_least && !(a.skip_self && i0 <= j_last && i0 + 32 > j_first))) {
+                const uint32_t base = per_piece(i0 + 4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const uint32_t i = i0 + acc_row(r, h);
-                    const bool in = (i - lo < hi - lo) & !(a.skip_self && i == j);
+                    const uint32_t i = base + acc_row(r, 0);
+                    const bool in = (i - lo < hi - lo) & !(a.skip_self & (i == j));
                     s[r] = in ? s[r] : -__builtin_inff();
                 }
             }
@@ -443,6 +473,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
                 s[r] = __builtin_amdgcn_exp2f(s[r]);
                 dp[r] = s[r] * (dp[r] - dl[acc_row(r, 0)]);
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const auto p = acc_operand<T>(s, k), ds = acc_operand<T>(dp, k);
@@ -453,8 +484,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
                 }
             }
         };
-        if (SPLIT == 1 || half == 0) one(std::integral_constant<int, 0>{});
-        if (SPLIT == 1 || half == 1) one(std::integral_constant<int, 1>{});
+        one(std::integral_constant<int, 0>{});
+        if constexpr (SPLIT == 1) one(std::integral_constant<int, 1>{});
         if (t + 1 < count) {
             if (BUFFERS == 1) __syncthreads();
             put(t + 1);
@@ -469,13 +500,13 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     if (!some) return;
 
     // rows that later pieces add to are left in fp32, the others are finished
-    const uint32_t place = late ? j - k0 : j - text.first;
+    const uint32_t at = late ? j - k0 : j - text.first;      // among the text's first words
     const uint32_t last = (text.end - 1) / (b.late_words ? b.late_words : 1);
-    const bool joined = b.late && place < a.sinks && text.end > border;
+    const bool joined = b.late && at < a.sinks && text.end > border;
     const bool redo = not_finite(dk) | not_finite(dv);
     float* const kept = late || joined
         ? (late ? b.late_sums + ((size_t)block * a.kv_heads + kv_head) * a.sinks * 2 * a.width
-                : b.own_sums + ((size_t)last * a.kv_heads + kv_head) * a.sinks * 2 * a.width) + (size_t)place * 2 * a.width
+                : b.own_sums + ((size_t)last * a.kv_heads + kv_head) * a.sinks * 2 * a.width) + (size_t)at * 2 * a.width
         : nullptr;
     if (real && !redo) {
         if (kept) {
@@ -575,11 +606,14 @@ template <typename T, int DB, bool BIAS> void backward_run(const BackwardArgs& b
     const AttendArgs& a = b.a;
     const uint32_t words = attend_bias_parts(a.T), table = BIAS ? bias_table(a.span) * sizeof(float) : 0;
     uint32_t blocks = words * a.heads;
-    if (query_split<T, DB, BIAS>(b, blocks)) query_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, query_room<BIAS, 2>(b), st>>>(b);
-    else query_kernel<T, DB, BIAS, 1><<<blocks, THREADS, query_room<BIAS, 1>(b), st>>>(b);
+    bool split = splits<T, DB> && query_split<T, DB, BIAS>(b, blocks);
+    if constexpr (splits<T, DB>)
+        if (split) query_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, query_room<BIAS, 2>(b), st>>>(b);
+    if (!split) query_kernel<T, DB, BIAS, 1><<<blocks, THREADS, query_room<BIAS, 1>(b), st>>>(b);
     blocks = (b.late + words) * a.kv_heads;
-    if (blocks < SPLIT_BELOW) key_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(b);
-    else key_kernel<T, DB, BIAS, 1><<<blocks, THREADS, table, st>>>(b);
+    if constexpr (splits<T, DB>)
+        if (blocks < SPLIT_BELOW) return key_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(b);
+    key_kernel<T, DB, BIAS, 1><<<blocks, THREADS, table, st>>>(b);
 }
 template <typename T, int DB> void backward_bias(const BackwardArgs& b, hipStream_t st) {
     if (b.a.bias) backward_run<T, DB, true>(b, st);

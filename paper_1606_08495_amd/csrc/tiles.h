@@ -188,9 +188,10 @@ template <typename T, int DB, int ROWS, int THREADS> struct Transit {
         for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_read<T, DB == 1>(at[n], c0, width);
         tile += ROWS * stride;
     }
-    __device__ __forceinline__ void store(char* to, uint32_t width) {
+    // CLEAN: zeros past the width
+    template <bool CLEAN = false> __device__ __forceinline__ void store(char* to, uint32_t width) {
         if (c0 >= (uint32_t)Tl::CHUNKS * Tl::N || threadIdx.x / LANES >= (uint32_t)ROWS) return;
-        if (width % Tl::N)
+        if (CLEAN || width % Tl::N)
 #pragma unroll
             for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_fit<T>(x[n], c0, width);
 #pragma unroll
