@@ -25,11 +25,29 @@ template <int N> struct Pack<__bf16, N> {
 };
 template <typename T> constexpr int pack16 = 16 / (int)sizeof(T);       // elements of 16 bytes
 
-// The sum over aligned groups of G lanes (a power of two up to 64), in every lane of the group, in a fixed order.
-template <int G> __device__ inline float lanes_sum(float x) {
-#pragma unroll
-    for (int m = 1; m < G; m *= 2) x += __shfl_xor(x, m, 64);
+// The sum (or largest) over aligned groups of G lanes (a power of two up to 64), in every lane of the group, in a fixed order:
+// exchanges inside registers, none through LDS.  (With pairs summed, a lane's mirror in 8 or 16 lanes holds what
+// its partner 4 or 8 lanes on does.)
+template <int CTRL> __device__ __forceinline__ float lane_partner(float x) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+template <int G, typename F> __device__ __forceinline__ float lanes_join(float x, const F& f) {
+    if constexpr (G >= 2) x = f(x, lane_partner<0xB1>(x));        // quad_perm 1 0 3 2
+    if constexpr (G >= 4) x = f(x, lane_partner<0x4E>(x));        // quad_perm 2 3 0 1
+    if constexpr (G >= 8) x = f(x, lane_partner<0x141>(x));       // mirror in 8
+    if constexpr (G >= 16) x = f(x, lane_partner<0x140>(x));      // mirror in 16
+    if constexpr (G >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if constexpr (G >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
     return x;
+}
+template <int G> __device__ __forceinline__ float lanes_sum(float x) {
+    return lanes_join<G>(x, [](float a, float b) __attribute__((always_inline)) { return a + b; });
 }
 
 }  // namespace w2v

@@ -146,18 +146,18 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         for (uint32_t t = 0; t < count; ++t) {
             if (t + 1 < count) next.fetch(a, kv_head, x, t + 1, lane);
             const char *kt = tiles + t % BUFFERS * 2 * Tl::BYTES, *vt = kt + Tl::BYTES;
-            const auto one = [&](auto P) __attribute__((always_inline)) {
-                constexpr int piece = P.value;
-                const uint32_t n0 = t * KEYS + piece * 32 + own_rows, j0 = n0 + x.shift;
+            const auto one = [&](uint32_t piece) __attribute__((always_inline)) {
+                const uint32_t row0 = piece * 32 + own_rows, n0 = t * KEYS + row0, j0 = n0 + x.shift;
+                const char *kp = kt + piece * (32 / 4) * Tl::STRIDE, *vp = vt + piece * (32 / 4) * Tl::STRIDE;
                 const bool linear = n0 >= x.sunk;
                 if (!some || n0 >= x.count || (linear && !w.shown_any(j0))) return;
                 Acc s = {}, dp = {};
 #pragma unroll
                 for (int k = 0; k < 2 * DB; ++k) {
-                    mma(Tl::along(kt, at_along, piece * 32, k), q[k], s);
-                    mma(Tl::along(vt, at_along, piece * 32, k), g[k], dp);
+                    mma(Tl::along(kp, at_along, 0, k), q[k], s);
+                    mma(Tl::along(vp, at_along, 0, k), g[k], dp);
                 }
-                piece_scores<BIAS>(a, w, x, n0, kept >> (piece * 32 + own_rows), linear, table, h, s);
+                piece_scores<BIAS>(a, w, x, n0, kept >> row0, linear, table, h, s);
                 if constexpr (pass == 0) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
@@ -210,11 +210,13 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                 for (int k = 0; k < 2; ++k) {
                     const auto ds = acc_operand<T>(s, k);
 #pragma unroll
-                    for (int n = 0; n < DB; ++n) mma(Tl::across(kt, at_across, piece * 32, k, n), ds, dq[n]);
+                    for (int n = 0; n < DB; ++n) mma(Tl::across(kp, at_across, 0, k, n), ds, dq[n]);
                 }
             };
-            one(std::integral_constant<int, 0>{});
-            if constexpr (SPLIT == 1) one(std::integral_constant<int, 1>{});
+            if constexpr (SPLIT == 2) one(0);
+            else
+#pragma unroll 1
+                for (uint32_t piece = 0; piece < KEYS / 32; ++piece) one(piece);
             if (t + 1 < count) {
                 if (BUFFERS == 1) __syncthreads();
                 char* const to = tiles + (t + 1) % BUFFERS * 2 * Tl::BYTES;
@@ -426,24 +428,24 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
         if (BUFFERS == 1 || t == 0 || (BIAS && t % per_head == 0)) __syncthreads();
         if (t + 1 < count) fetch(t + 1);
         const char *qt = tiles + t % BUFFERS * 2 * Tl::BYTES, *gt = qt + Tl::BYTES;
-        const auto one = [&](auto P) __attribute__((always_inline)) {
-            constexpr int piece = P.value;
-            const uint32_t i0 = q0 + t % per_head * KEYS + piece * 32 + own_rows;
+        const auto one = [&](uint32_t piece) __attribute__((always_inline)) {
+            const uint32_t row0 = piece * 32 + own_rows, i0 = q0 + t % per_head * KEYS + row0;
+            const char *qp = qt + piece * (32 / 4) * Tl::STRIDE, *gp = gt + piece * (32 / 4) * Tl::STRIDE;
             if (!some || i0 >= hi_most || i0 + 32 <= lo_least) return;
             Acc s = {}, dp = {};
             const uint32_t at_own = per_piece(own_base);      // (what does not change is not kept in registers)
 #pragma unroll
             for (int k = 0; k < 2 * DB; ++k) {
                 if constexpr (OWN) {
-                    mma(Tl::along(qt, at_along, piece * 32, k), Ow::along(own, at_own, 0, k), s);
-                    mma(Tl::along(gt, at_along, piece * 32, k), Ow::along(own + Ow::BYTES, at_own, 0, k), dp);
+                    mma(Tl::along(qp, at_along, 0, k), Ow::along(own, at_own, 0, k), s);
+                    mma(Tl::along(gp, at_along, 0, k), Ow::along(own + Ow::BYTES, at_own, 0, k), dp);
                 } else {
-                    mma(Tl::along(qt, at_along, piece * 32, k), kf[k], s);
-                    mma(Tl::along(gt, at_along, piece * 32, k), vf[k], dp);
+                    mma(Tl::along(qp, at_along, 0, k), kf[k], s);
+                    mma(Tl::along(gp, at_along, 0, k), vf[k], dp);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);        // (what the next products read is not asked for before: registers)
-            const float *l2 = &rows[t % BUFFERS][0][piece * 32 + own_rows + 4 * h], *dl = l2 + KEYS;
+            const float *l2 = &rows[t % BUFFERS][0][row0 + 4 * h], *dl = l2 + KEYS;
             if constexpr (BIAS) {
                 const int32_t far = (int32_t)j_last - (int32_t)i0, near = (int32_t)j_first - (int32_t)i0 - 31;
                 if (far <= -(int32_t)a.span || near >= (int32_t)a.span) {
@@ -479,13 +481,15 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
                 const auto p = acc_operand<T>(s, k), ds = acc_operand<T>(dp, k);
 #pragma unroll
                 for (int n = 0; n < DB; ++n) {
-                    mma(Tl::across(gt, at_across, piece * 32, k, n), p, dv[n]);
-                    mma(Tl::across(qt, at_across, piece * 32, k, n), ds, dk[n]);
+                    mma(Tl::across(gp, at_across, 0, k, n), p, dv[n]);
+                    mma(Tl::across(qp, at_across, 0, k, n), ds, dk[n]);
                 }
             }
         };
-        one(std::integral_constant<int, 0>{});
-        if constexpr (SPLIT == 1) one(std::integral_constant<int, 1>{});
+        if constexpr (SPLIT == 2) one(0);
+        else
+#pragma unroll 1
+            for (uint32_t piece = 0; piece < KEYS / 32; ++piece) one(piece);
         if (t + 1 < count) {
             if (BUFFERS == 1) __syncthreads();
             put(t + 1);
