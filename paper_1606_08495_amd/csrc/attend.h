@@ -143,9 +143,7 @@ __device__ inline bool row_keeps(const AttendArgs& a, uint32_t i, uint32_t j) {
 }
 
 __device__ inline float wave_max(float x) {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) x = fmaxf(x, __shfl_xor(x, m, 64));
-    return x;
+    return lanes_join<64>(x, [](float a, float b) __attribute__((always_inline)) { return fmaxf(a, b); });
 }
 
 // o_i and lse_i (lane l holds columns l and l + 64 of o).

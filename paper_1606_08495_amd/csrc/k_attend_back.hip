@@ -539,7 +539,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
 }
 
 // ---- the end: late pieces joined, the bias' gradient -----------------------------------------------------
-constexpr uint32_t END_THREADS = 1024;
+constexpr uint32_t END_THREADS = 1024, FEW_PARTS = 16;      // blocks whose sums the last kernel joins by itself: a launch less
 template <typename T> __global__ __launch_bounds__(END_THREADS) void end_kernel(const BackwardArgs b, uint32_t parts) {
     const AttendArgs& a = b.a;
     const uint32_t lane = threadIdx.x % WAVE;
@@ -579,21 +579,25 @@ template <typename T> __global__ __launch_bounds__(END_THREADS) void end_kernel(
     b.distance_sums[(size_t)head * distances + c] = s;
 }
 
-// dbias of a head: the distances of each bucket, in order.
-__global__ __launch_bounds__(THREADS) void buckets_kernel(const BackwardArgs b, bool none) {
+// dbias of a head: its sums by distance -- joined already, or here from a few blocks' -- then the distances of each bucket, both
+// in order: a wavefront for a bucket, its lanes' shares of the distances joined.
+__global__ __launch_bounds__(END_THREADS) void buckets_kernel(const BackwardArgs b, const float* by_distance, uint32_t parts) {
     const AttendArgs& a = b.a;
     __shared__ float sums[2 * SPAN_MAX + 1];
     __shared__ uint32_t bucket[2 * SPAN_MAX + 1];
     const uint32_t head = blockIdx.x, distances = 2 * a.span + 1;
-    for (uint32_t c = threadIdx.x; c < distances; c += THREADS) {
-        sums[c] = none ? 0.f : b.distance_sums[(size_t)head * distances + c];
+    for (uint32_t c = threadIdx.x; c < distances; c += END_THREADS) {
+        float s = 0.f;
+        for (uint32_t p = 0; p < parts; ++p) s += by_distance[((size_t)head * parts + p) * distances + c];
+        sums[c] = s;
         bucket[c] = a.buckets[c];
     }
     __syncthreads();
-    for (uint32_t k = threadIdx.x; k < a.n_buckets; k += THREADS) {
+    for (uint32_t k = threadIdx.x / WAVE; k < a.n_buckets; k += END_THREADS / WAVE) {
         float s = 0.f;
-        for (uint32_t c = 0; c < distances; ++c) s += bucket[c] == k ? sums[c] : 0.f;
-        b.dbias[(size_t)head * a.n_buckets + k] = s;
+        for (uint32_t c = threadIdx.x % WAVE; c < distances; c += WAVE) s += bucket[c] == k ? sums[c] : 0.f;
+        s = lanes_sum<64>(s);
+        if (threadIdx.x % WAVE == 0) b.dbias[(size_t)head * a.n_buckets + k] = s;
     }
 }
 
@@ -631,9 +635,11 @@ template <typename T> void backward_any(const BackwardArgs& b, hipStream_t st) {
             case 3: backward_bias<T, 3>(b, st); break;
             default: backward_bias<T, 4>(b, st);
         }
-    const uint32_t blocks = b.late * b.a.kv_heads + (b.dbias && b.a.T ? b.a.heads * ((2 * b.a.span + 32) / 32) : 0);
-    if (blocks) end_kernel<T><<<blocks, END_THREADS, 0, st>>>(b, attend_bias_parts(b.a.T));
-    if (b.dbias) buckets_kernel<<<b.a.heads, THREADS, 0, st>>>(b, b.a.T == 0);
+    const uint32_t parts = attend_bias_parts(b.a.T);
+    const bool joined = b.dbias && parts > FEW_PARTS;
+    const uint32_t blocks = b.late * b.a.kv_heads + (joined ? b.a.heads * ((2 * b.a.span + 32) / 32) : 0);
+    if (blocks) end_kernel<T><<<blocks, END_THREADS, 0, st>>>(b, parts);
+    if (b.dbias) buckets_kernel<<<b.a.heads, END_THREADS, 0, st>>>(b, joined ? b.distance_sums : b.by_distance, joined ? 1 : parts);
 }
 
 }  // namespace

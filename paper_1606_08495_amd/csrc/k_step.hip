@@ -6,6 +6,7 @@
 // groups, wavefronts and, for long caches, blocks are joined at the end in a fixed order.  Rows that are
 // not shown are not read.  All arithmetic is fp32.
 #include "attend.h"
+#include "tiles.h"
 
 namespace w2v {
 namespace {
@@ -48,6 +49,8 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
             dynamic[c] = scaled_bias(a.bias, a.buckets, a.n_buckets, a.span, head0 + c % heads, -(int32_t)(c / heads));
         __syncthreads();
     }
+    // a lane's columns: start .. start + N, of which those before c0 are its neighbour's (the row's last 16 bytes are read whole)
+    const uint32_t c0 = part * N, start = a.width < N ? 0 : c0 < a.width - N ? c0 : a.width - N;
     float q[HEADS][N], acc[HEADS][N], m[HEADS], total[HEADS];
 #pragma unroll
     for (int g = 0; g < HEADS; ++g) {
@@ -55,41 +58,44 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
         total[g] = 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const uint32_t c = part * N + e;
-            q[g][e] = g < (int)heads && c < a.width ? (float)head_row<T>(a.q, text, head0 + g)[c] * a.scale2 : 0.f;
+            const uint32_t c = start + e;
+            q[g][e] = g < (int)heads && c >= c0 && c < a.width ? (float)head_row<T>(a.q, text, head0 + g)[c] * a.scale2 : 0.f;
             acc[g][e] = 0.f;
         }
     }
     const T* const k0 = (const T*)a.k.p + (uint64_t)text * a.k.text + (uint64_t)kv_head * a.k.head;
     const T* const v0 = (const T*)a.v.p + (uint64_t)text * a.v.text + (uint64_t)kv_head * a.v.head;
 
-    const auto load = [&](const T* base, uint64_t stride, uint32_t j) {
-        vec x = {};
-        const uint32_t c0 = part * N;
-        const T* p = base + (uint64_t)j * stride;
-        if (c0 + N <= a.width) x = *(const typename Pack<T, N>::mem*)(p + c0);
-        else
-#pragma unroll
-            for (int e = 0; e < N; ++e) if (c0 + e < a.width) x[e] = p[c0 + e];
-        return x;
-    };
     constexpr uint32_t STEP = GROUPS * AHEAD;         // keys of a wavefront's step
-    for (uint32_t n0 = from + wave * STEP; n0 < to; n0 += WAVES * STEP) {
-        vec kx[AHEAD], vx[AHEAD];
-        bool in[AHEAD];
-        uint32_t j[AHEAD];
+    const bool masked = a.keep || a.skip_self;
+    vec kx[AHEAD], vx[AHEAD];
+    uint32_t j[AHEAD];
+    uint8_t keep[AHEAD];
+    const auto fetch = [&](uint32_t n0) __attribute__((always_inline)) {      // (past the end: the last key again, without weight)
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const uint32_t n = n0 + u * GROUPS + group;
-            j[u] = n < keys.sunk ? n : keys.lo + n - keys.sunk;
-            in[u] = n < to && !(a.skip_self && j[u] == keys.last);
-            if (a.keep && in[u]) in[u] = a.keep[(uint64_t)text * a.room + j[u]] != 0;
-            kx[u] = vx[u] = vec{};
-            if (in[u]) {
-                kx[u] = load(k0, a.k.token, j[u]);
-                vx[u] = load(v0, a.v.token, j[u]);
-            }
+            const uint32_t n = n0 + u * GROUPS + group, at = n < to ? n : to - 1;
+            j[u] = at < keys.sunk ? at : keys.lo + at - keys.sunk;
         }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            kx[u] = chunk_read<T, L == 8>(k0 + (uint64_t)j[u] * a.k.token, c0, a.width);
+            vx[u] = chunk_read<T, L == 8>(v0 + (uint64_t)j[u] * a.v.token, c0, a.width);
+            keep[u] = 1;
+        }
+        if (a.keep)
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) keep[u] = a.keep[(uint64_t)text * a.room + j[u]];
+    };
+    for (uint32_t n0 = from + wave * STEP; n0 < to; n0 += WAVES * STEP) {
+        fetch(n0);
+        bool in[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            in[u] = n0 + u * GROUPS + group < to && keep[u] && !(a.skip_self && j[u] == keys.last);
+        if (masked)                                   // what is not shown must not show, whatever it holds
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) vx[u] = in[u] ? vx[u] : vec{};
 #pragma unroll
         for (int g = 0; g < HEADS; ++g) {
             float x[AHEAD], most = m[g];
@@ -139,7 +145,8 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
         }
         if (group == 0) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) joined[wave][g][2 + part * N + e] = acc[g][e];
+            for (int e = 0; e < N; ++e)
+                if (start + e >= c0 && start + e < a.width) joined[wave][g][2 + start + e] = acc[g][e];
             if (part == 0) { joined[wave][g][0] = most; joined[wave][g][1] = total[g]; }
         }
     }
@@ -174,15 +181,24 @@ template <typename T> __global__ __launch_bounds__(THREADS) void step_join_kerne
     const uint32_t text = (uint32_t)(at / a.heads), head = (uint32_t)(at % a.heads);
     const Keys keys = step_keys(a, text);
     const uint32_t count = (keys.count + a.per_split - 1) / a.per_split;
-    const float* p = a.parts + at * a.splits * (a.width + 2);
+    const uint32_t row = a.width + 2;
+    const float* p = a.parts + at * a.splits * row;
     float most = -__builtin_inff(), sum = 0.f, o[2] = {0.f, 0.f};
-    for (uint32_t s = 0; s < count; ++s) most = fmaxf(most, p[(uint64_t)s * (a.width + 2)]);
-    for (uint32_t s = 0; s < count; ++s) {
-        const float* x = p + (uint64_t)s * (a.width + 2);
-        const float f = x[0] == -__builtin_inff() ? (x[1] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(x[0] - most);
-        sum = fmaf(f, x[1], sum);
+    for (uint32_t s = lane; s < count; s += WAVE) most = fmaxf(most, p[(uint64_t)s * row]);
+    most = wave_max(most);
+    for (uint32_t s0 = 0; s0 < count; s0 += WAVE) {
+        const uint32_t s = s0 + lane;
+        const float m = s < count ? p[(uint64_t)s * row] : -__builtin_inff(), part = s < count ? p[(uint64_t)s * row + 1] : 0.f;
+        const float f = m == -__builtin_inff() ? (part == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - most);
+        sum += lanes_sum<64>(f * part);
+        const uint32_t here = count - s0 < WAVE ? count - s0 : WAVE;
+#pragma unroll 8
+        for (uint32_t l = 0; l < here; ++l) {
+            const float fl = __shfl(f, (int)l, 64);
+            const float* x = p + (uint64_t)(s0 + l) * row + 2;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) o[c] = fmaf(f, x[2 + lane + c * WAVE], o[c]);
+            for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) o[c] = fmaf(fl, x[lane + c * WAVE], o[c]);
+        }
     }
     T* to = head_row<T>(a.o, text, head);
 #pragma unroll

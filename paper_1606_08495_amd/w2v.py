@@ -412,6 +412,8 @@ TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 _AS_IT_IS = contextlib.nullcontext()
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _on(stream, t):
@@ -446,14 +448,15 @@ def layer_norm(x, gain=None, offset=None, eps=1e-5, out=None, stream=None):
     xp, xs = _rows(x, None, "x")
     m, d = x.shape
     with _on(stream, x):
-        st = torch.cuda.current_stream()
-        y = torch.empty((m, d), dtype=x.dtype, device=x.device) if out is None else out
-        stats = torch.empty((2, m), dtype=torch.float32, device=x.device)
+        st = _raw_stream(x.device.index)
+        y = x.new_empty((m, d)) if out is None else out
+        stats = x.new_empty((2, m), dtype=torch.float32)
         yp, ys = _rows(y, x, "out")
+        at = stats.data_ptr()
         _check(lib().w2v_layer_norm(TYPES[x.dtype], xp, xs, m, d, _vec(gain, d, x.device, "gain"),
-                                    _vec(offset, d, x.device, "offset"), float(eps), yp, ys, stats.data_ptr(),
-                                    stats.data_ptr() + 4 * m, st.cuda_stream))
-    return y, stats[0], stats[1]
+                                    _vec(offset, d, x.device, "offset"), float(eps), yp, ys, at, at + 4 * m, st))
+    mean, rstd = stats.unbind(0)
+    return y, mean, rstd
 
 
 def layer_norm_backward(dy, x, gain, mean, rstd, out=None, workspace=None, stream=None):
@@ -463,18 +466,19 @@ def layer_norm_backward(dy, x, gain, mean, rstd, out=None, workspace=None, strea
     gp, gs = _rows(dy, x, "dy")
     m, d = x.shape
     with _on(stream, x):
-        st = torch.cuda.current_stream()
-        dx = torch.empty((m, d), dtype=x.dtype, device=x.device) if out is None else out
-        columns = torch.empty((2, d), dtype=torch.float32, device=x.device)
+        st = _raw_stream(x.device.index)
+        dx = x.new_empty((m, d)) if out is None else out
+        columns = x.new_empty((2, d), dtype=torch.float32)
         if workspace is None:
-            workspace = torch.empty(int(lib().w2v_layer_norm_backward_workspace(TYPES[x.dtype], m, d)),
-                                    dtype=torch.uint8, device=x.device)
+            workspace = x.new_empty(int(lib().w2v_layer_norm_backward_workspace(TYPES[x.dtype], m, d)),
+                                    dtype=torch.uint8)
         op, os_ = _rows(dx, x, "out")
         _check(lib().w2v_layer_norm_backward(TYPES[x.dtype], gp, gs, xp, xs, m, d, _vec(gain, d, x.device, "gain"),
                                              _vec(mean, m, x.device, "mean"), _vec(rstd, m, x.device, "rstd"), op,
                                              os_, columns.data_ptr(), columns.data_ptr() + 4 * d,
-                                             workspace.data_ptr(), workspace.numel(), st.cuda_stream))
-    return dx, columns[0], columns[1]
+                                             workspace.data_ptr(), workspace.numel(), st))
+    dgain, doffset = columns.unbind(0)
+    return dx, dgain, doffset
 
 
 class Heads(ctypes.Structure):
@@ -546,15 +550,15 @@ def attend(q, k, v, sent_off, left=None, right=None, sinks=0, skip_self=False, s
     T, H, _ = q.shape
     G = k.shape[1]
     with _on(stream, q):
-        st = torch.cuda.current_stream()
+        st = _raw_stream(q.device.index)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+            out = q.new_empty(q.shape)
+        lse = q.new_empty((H, T), dtype=torch.float32)
         spec = _spec(q, G, left, right, sinks, skip_self, scale, bias, buckets)
         off, n, t, kp = _texts(sent_off, keep, q)
         _check(lib().w2v_attend(ctypes.byref(spec), ctypes.byref(_heads(q, q, T, H, "q")),
                                 ctypes.byref(_heads(k, q, T, G, "k")), ctypes.byref(_heads(v, q, T, G, "v")), off, n, t, kp,
-                                ctypes.byref(_heads(out, q, T, H, "out")), lse.data_ptr(), st.cuda_stream))
+                                ctypes.byref(_heads(out, q, T, H, "out")), lse.data_ptr(), st))
     return out, lse
 
 
@@ -569,21 +573,20 @@ def attend_backward(dout, q, k, v, out, lse, sent_off, left=None, right=None, si
     if lse.shape != (H, T) or lse.device != q.device:
         raise ValueError("lse must be [heads, tokens]")
     with _on(stream, q):
-        st = torch.cuda.current_stream()
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        dk, dv = [torch.empty(k.shape, dtype=q.dtype, device=q.device) for _ in range(2)]
-        dbias = None if bias is None else torch.empty(bias.shape, dtype=torch.float32, device=q.device)
+        st = _raw_stream(q.device.index)
+        dq, dk, dv = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)
+        dbias = None if bias is None else bias.new_empty(bias.shape)
         spec = _spec(q, G, left, right, sinks, skip_self, scale, bias, buckets)
         if workspace is None:
             need = int(lib().w2v_attend_backward_workspace(ctypes.byref(spec), T))
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(max(need, 256), dtype=torch.uint8)
         off, n, t, kp = _texts(sent_off, keep, q)
         r = ctypes.byref
         _check(lib().w2v_attend_backward(
             r(spec), r(_heads(dout, q, T, H, "dout")), r(_heads(q, q, T, H, "q")), r(_heads(k, q, T, G, "k")),
             r(_heads(v, q, T, G, "v")), r(_heads(out, q, T, H, "out")), _dev(lse, torch.float32, "lse"), off, n, t, kp,
             r(_heads(dq, q, T, H, "dq")), r(_heads(dk, q, T, G, "dk")), r(_heads(dv, q, T, G, "dv")),
-            _dev(dbias, torch.float32, "dbias"), workspace.data_ptr(), workspace.numel(), st.cuda_stream))
+            _dev(dbias, torch.float32, "dbias"), workspace.data_ptr(), workspace.numel(), st))
     return dq, dk, dv, dbias
 
 
@@ -609,17 +612,17 @@ def attend_step(q, k, v, n, left=None, sinks=0, skip_self=False, scale=None, kee
     if n.shape != (B,) or n.device != q.device or (keep is not None and (keep.shape != (B, room) or keep.device != q.device)):
         raise ValueError("n must be [texts] and keep [texts, room] on the device of q")
     with _on(stream, q):
-        st = torch.cuda.current_stream()
+        st = _raw_stream(q.device.index)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         spec = _spec(q, G, left, 0, sinks, skip_self, scale, bias, buckets)
         r = ctypes.byref
         if workspace is None:
             need = int(lib().w2v_attend_step_workspace(r(spec), B, room))
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(max(need, 256), dtype=torch.uint8)
         shape = torch.Size((B, room, G, d))
         _check(lib().w2v_attend_step(r(spec), r(_heads(q, q, B, H, "q")), r(_cache(k, q, shape, "k")),
                                      r(_cache(v, q, shape, "v")), _dev(n, IDX, "n"), B, room, _dev(keep, torch.uint8, "keep"),
                                      r(_heads(out, q, B, H, "out")), workspace.data_ptr(), workspace.numel(),
-                                     st.cuda_stream))
+                                     st))
     return out
