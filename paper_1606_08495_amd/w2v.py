@@ -418,6 +418,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
 
 def _on(stream, t):
     """What is allocated for a call belongs to the stream the call runs on, and to the tensor's device."""
+    if not t.is_cuda:
+        raise TypeError("a CUDA tensor is wanted")
     if stream is not None:
         return torch.cuda.stream(stream)
     return _AS_IT_IS if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
