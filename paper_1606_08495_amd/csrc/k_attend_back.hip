@@ -284,6 +284,11 @@ __device__ inline uint32_t late_border(const BackwardArgs& b, uint32_t j) {
     return j / BLOCK_WORDS * BLOCK_WORDS + BLOCK_WORDS + b.reach;
 }
 
+// Heads whose rows as keys, beside the sums for dk and dv, leave no registers for a second wavefront on a SIMD: their blocks always
+// have both halves and read those rows from LDS (16384 words of 16 heads of 96 in a window of 1024, 16 bits: the backward pass
+// takes 635 us instead of 706; of 128: 872 instead of 904).
+template <typename T, int DB> constexpr bool own_rows_in_lds = DB * sizeof(T) >= 6;
+
 template <typename T, int DB, bool BIAS, int SPLIT>
 __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 ? 2 : 1) void key_kernel(const BackwardArgs b) {
     const AttendArgs& a = b.a;
@@ -292,7 +297,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     constexpr int ROOM = SPLIT == 2 ? GROUPS * DB * 16 * WAVE * 4 : 0;
     __shared__ __align__(16) char tiles[BUFFERS * 2 * Tl::BYTES > ROOM ? BUFFERS * 2 * Tl::BYTES : ROOM];
     // wide heads: the block's own keys and values as operands from LDS, registers do not hold them beside the sums
-    constexpr bool OWN = SPLIT == 2 && DB * sizeof(T) >= 6;
+    constexpr bool OWN = SPLIT == 2 && own_rows_in_lds<T, DB>;
     typedef Tile<T, DB, BLOCK_WORDS> Ow;
     __shared__ __align__(16) char own[OWN ? 2 * Ow::BYTES : 16];
     __shared__ float rows[BUFFERS][2][KEYS];          // the queries' logarithms to base two, and delta
@@ -619,9 +624,13 @@ template <typename T, int DB, bool BIAS> void backward_run(const BackwardArgs& b
         if (split) query_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, query_room<BIAS, 2>(b), st>>>(b);
     if (!split) query_kernel<T, DB, BIAS, 1><<<blocks, THREADS, query_room<BIAS, 1>(b), st>>>(b);
     blocks = (b.late + words) * a.kv_heads;
-    if constexpr (splits<T, DB>)
-        if (blocks < SPLIT_BELOW) return key_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(b);
-    key_kernel<T, DB, BIAS, 1><<<blocks, THREADS, table, st>>>(b);
+    if constexpr (splits<T, DB> && own_rows_in_lds<T, DB>) {
+        key_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(b);
+    } else {
+        if constexpr (splits<T, DB>)
+            if (blocks < SPLIT_BELOW) return key_kernel<T, DB, BIAS, 2><<<blocks, 2 * THREADS, table, st>>>(b);
+        key_kernel<T, DB, BIAS, 1><<<blocks, THREADS, table, st>>>(b);
+    }
 }
 template <typename T, int DB> void backward_bias(const BackwardArgs& b, hipStream_t st) {
     if (b.a.bias) backward_run<T, DB, true>(b, st);

@@ -54,16 +54,42 @@ template <typename T, int G, int NV> struct Row {
     }
 };
 
-// Columns' parameters (fp32) as a lane of the row's group holds them; `other` where there are none and past the row's end.
+// Columns' fp32 values as a lane of the row's group holds them, from memory (`other` where there are none and past the row's end)
+// and back.
 template <typename T, int G, int NV>
 __device__ inline void load_columns(float (&w)[NV][pack16<T>], const float* p, float other, uint32_t lane, uint32_t d) {
+    constexpr int N = pack16<T>;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t c = (i * G + lane) * N;
+        if (p && c + N <= d) {
 #pragma unroll
-        for (int e = 0; e < pack16<T>; ++e) {
-            const uint32_t c = (i * G + lane) * pack16<T> + e;
-            w[i][e] = p && c < d ? p[c] : other;
+            for (int e = 0; e < N; e += 4) {
+                const Pack<float, 4>::vec four = *(const Pack<float, 4>::mem*)(p + c + e);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[i][e + k] = four[k];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) w[i][e] = p && c + e < d ? p[c + e] : other;
         }
+    }
+}
+template <typename T, int G, int NV>
+__device__ inline void store_columns(const float (&w)[NV][pack16<T>], float* p, uint32_t lane, uint32_t d) {
+    constexpr int N = pack16<T>;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint32_t c = (i * G + lane) * N;
+        if (c + N <= d) {
+#pragma unroll
+            for (int e = 0; e < N; e += 4)
+                *(Pack<float, 4>::mem*)(p + c + e) = Pack<float, 4>::vec{w[i][e], w[i][e + 1], w[i][e + 2], w[i][e + 3]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) if (c + e < d) p[c + e] = w[i][e];
+        }
+    }
 }
 
 // Sum over the G lanes of a row.  Rows of more than a wavefront go through LDS, `turn` says which of the two halves.
@@ -186,13 +212,8 @@ void norm_backward_kernel(const NormBackwardArgs a) {
     if (!a.parts) return;
     float* part = a.parts + (size_t)blockIdx.x * 2 * d;
     if constexpr (G > 64) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const uint32_t c = (i * G + lane) * N + e;
-                if (c < d) { part[c] = dg[i][e]; part[d + c] = db[i][e]; }
-            }
+        store_columns<T, G, NV>(dg, part, lane, d);
+        store_columns<T, G, NV>(db, part + d, lane, d);
     } else {
         // the groups of a wavefront by exchange, then the wavefronts one after the other
 #pragma unroll
