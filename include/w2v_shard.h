@@ -373,7 +373,7 @@ int w2v_layer_norm_backward(int type, const void* dy_dev, uint64_t dy_stride, co
  * Scores, softmax and sums are fp32; weights are rounded to `type` for the product with v.  No call allocates or
  * synchronises; results repeat bit for bit.  Limits: 1 <= width <= W2V_HEAD_MAX, heads a multiple of kv_heads and at most
  * 1024, sinks <= W2V_SINKS_MAX, 1 <= span <= W2V_SPAN_MAX, 1 <= n_buckets <= W2V_BUCKETS_MAX, scale finite and > 0,
- * n_tokens heads < 2^38, n_tokens <= 2^31 - 2^12. */
+ * n_tokens * heads <= 2^29 (pass longer corpora in blocks). */
 #define W2V_HEAD_MAX 128
 #define W2V_SINKS_MAX 64
 #define W2V_SPAN_MAX 1023
@@ -413,7 +413,7 @@ int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads* dout, cons
  * token_stride leading from text to text.  out is what w2v_attend (right = 0) gives that word: over the words
  * i - left <= j <= i and the first `sinks` ones, i = n_dev[b] - 1, whose byte keep_dev[b room + j] is not 0 (NULL: all); no
  * words: zeros.  spec->right is not read.  workspace_dev: 256-byte aligned device memory of
- * w2v_attend_step_workspace bytes, contents irrelevant before and after.  batch * heads <= 2^24,
+ * w2v_attend_step_workspace bytes, contents irrelevant before and after.  batch * heads <= 2^23,
  * room <= 2^31 - 2^12. */
 typedef struct w2v_cache { const void* p; uint64_t text_stride, token_stride, head_stride; } w2v_cache;
 size_t w2v_attend_step_workspace(const w2v_attend_spec* spec, uint32_t batch, uint32_t room);

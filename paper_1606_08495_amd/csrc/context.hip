@@ -115,7 +115,7 @@ int check_spec(const w2v_attend_spec* s) {
 }
 
 int check_tokens(const w2v_attend_spec* s, const uint64_t* off, uint32_t n_sent, uint32_t n_tokens) {
-    if (n_tokens > 0x7FFFFFFFu - 4095u || (uint64_t)n_tokens * s->heads >= 1ull << 38)
+    if (n_tokens > 0x7FFFFFFFu - 4095u || (uint64_t)n_tokens * s->heads > 1ull << 29)      // (threads of a launch: below 2^32)
         return fail(W2V_ERR_ARG, "too many tokens; pass the texts in blocks");
     if (n_tokens && n_sent == 0) return fail(W2V_ERR_ARG, "tokens without texts");
     if (n_sent > 0x7FFFFFFFu) return fail(W2V_ERR_ARG, "too many texts");
@@ -274,7 +274,7 @@ namespace {
 int check_step(const w2v_attend_spec* s, uint32_t batch, uint32_t room) {
     if (int rc = check_spec(s)) return rc;
     if (room == 0 || room > 0x7FFFFFFFu - 4095u) return fail(W2V_ERR_ARG, "room = %u outside 1..2^31 - 2^12", room);
-    if ((uint64_t)batch * s->heads > 1u << 24) return fail(W2V_ERR_ARG, "too many texts at once");
+    if ((uint64_t)batch * s->heads > 1u << 23) return fail(W2V_ERR_ARG, "too many texts at once");
     return W2V_OK;
 }
 
