@@ -485,13 +485,28 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
                 dp[r] = s[r] * (dp[r] - dl[acc_row(r, 0)]);
             }
             __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const auto p = acc_operand<T>(s, k), ds = acc_operand<T>(dp, k);
+            if constexpr (sizeof(T) == 4) {
+                // a piece's sum first, then to the whole: a text's queries and heads would make one long chain of roundings
 #pragma unroll
                 for (int n = 0; n < DB; ++n) {
-                    mma(Tl::across(gp, at_across, 0, k, n), p, dv[n]);
-                    mma(Tl::across(qp, at_across, 0, k, n), ds, dk[n]);
+                    Acc v = {}, x = {};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        mma(Tl::across(gp, at_across, 0, k, n), acc_operand<T>(s, k), v);
+                        mma(Tl::across(qp, at_across, 0, k, n), acc_operand<T>(dp, k), x);
+                    }
+                    dv[n] += v;
+                    dk[n] += x;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const auto p = acc_operand<T>(s, k), ds = acc_operand<T>(dp, k);
+#pragma unroll
+                    for (int n = 0; n < DB; ++n) {
+                        mma(Tl::across(gp, at_across, 0, k, n), p, dv[n]);
+                        mma(Tl::across(qp, at_across, 0, k, n), ds, dk[n]);
+                    }
                 }
             }
         };
