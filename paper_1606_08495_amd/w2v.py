@@ -509,13 +509,19 @@ def relative_buckets(n_buckets, span, device="cuda"):
 
 def _heads(t, like, rows, heads, name):
     """[rows, heads, width], the elements of a head side by side."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype == like.dtype and
-            t.device == like.device and t.shape == (rows, heads, like.shape[2])):
-        raise TypeError("%s must be a CUDA tensor [%d, %d, %d] of %s" % (name, rows, heads, like.shape[2], like.dtype))
+    width = like.shape[2]
+    if not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.device != like.device or \
+            t.shape != (rows, heads, width):
+        raise TypeError("%s must be a CUDA tensor [%d, %d, %d] of %s" % (name, rows, heads, width, like.dtype))
     a, b, c = t.stride()
-    if (c != 1 and t.shape[2] > 1) or a < 0 or b < 0:
+    if (c != 1 and width > 1) or a < 0 or b < 0:
         raise ValueError("%s: the elements of a head must lie side by side" % name)
     return Heads(t.data_ptr(), a, b)
+
+
+def _dense(t, heads, width):
+    """A dense [rows, heads, width] of this module's own making."""
+    return Heads(t.data_ptr(), heads * width, width)
 
 
 def _spec(q, kv_heads, left, right, sinks, skip_self, scale, bias, buckets):
@@ -549,18 +555,20 @@ def attend(q, k, v, sent_off, left=None, right=None, sinks=0, skip_self=False, s
     uint8 [tokens], 0 where a word is not to be seen.  bias float32 [heads, buckets] with the map ``buckets`` (relative_buckets)."""
     if q.dim() != 3 or k.dim() != 3:
         raise TypeError("q, k and v must be [tokens, heads, width]")
-    T, H, _ = q.shape
+    T, H, d = q.shape
     G = k.shape[1]
     with _on(stream, q):
-        st = _raw_stream(q.device.index)
+        st, r = _raw_stream(q.device.index), ctypes.byref
         if out is None:
             out = q.new_empty(q.shape)
+            into = _dense(out, H, d)
+        else:
+            into = _heads(out, q, T, H, "out")
         lse = q.new_empty((H, T), dtype=torch.float32)
         spec = _spec(q, G, left, right, sinks, skip_self, scale, bias, buckets)
         off, n, t, kp = _texts(sent_off, keep, q)
-        _check(lib().w2v_attend(ctypes.byref(spec), ctypes.byref(_heads(q, q, T, H, "q")),
-                                ctypes.byref(_heads(k, q, T, G, "k")), ctypes.byref(_heads(v, q, T, G, "v")), off, n, t, kp,
-                                ctypes.byref(_heads(out, q, T, H, "out")), lse.data_ptr(), st))
+        _check(lib().w2v_attend(r(spec), r(_heads(q, q, T, H, "q")), r(_heads(k, q, T, G, "k")),
+                                r(_heads(v, q, T, G, "v")), off, n, t, kp, r(into), lse.data_ptr(), st))
     return out, lse
 
 
@@ -570,7 +578,7 @@ def attend_backward(dout, q, k, v, out, lse, sent_off, left=None, right=None, si
     a bias.  ``workspace``: optional uint8 device tensor to reuse."""
     if q.dim() != 3 or k.dim() != 3:
         raise TypeError("q, k and v must be [tokens, heads, width]")
-    T, H, _ = q.shape
+    T, H, d = q.shape
     G = k.shape[1]
     if lse.shape != (H, T) or lse.device != q.device:
         raise ValueError("lse must be [heads, tokens]")
@@ -587,7 +595,7 @@ def attend_backward(dout, q, k, v, out, lse, sent_off, left=None, right=None, si
         _check(lib().w2v_attend_backward(
             r(spec), r(_heads(dout, q, T, H, "dout")), r(_heads(q, q, T, H, "q")), r(_heads(k, q, T, G, "k")),
             r(_heads(v, q, T, G, "v")), r(_heads(out, q, T, H, "out")), _dev(lse, torch.float32, "lse"), off, n, t, kp,
-            r(_heads(dq, q, T, H, "dq")), r(_heads(dk, q, T, G, "dk")), r(_heads(dv, q, T, G, "dv")),
+            r(_dense(dq, H, d)), r(_dense(dk, G, d)), r(_dense(dv, G, d)),
             _dev(dbias, torch.float32, "dbias"), workspace.data_ptr(), workspace.numel(), st))
     return dq, dk, dv, dbias
 
