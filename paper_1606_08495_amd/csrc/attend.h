@@ -187,11 +187,12 @@ __device__ void attend_row(const AttendArgs& a, uint32_t head, uint32_t i, const
     lse = total == 0.f ? -__builtin_inff() : (base + log2f(total)) * LN2;
 }
 
-// p and dS of (i, j), from what the forward pass left.
+// p and dS of (i, j), from what the forward pass left.  (A word whose shown words all have a score of -infinity weighs none.)
 template <typename T>
 __device__ inline float2 row_gradient(const BackwardArgs& b, uint32_t head, uint32_t i, uint32_t j, float delta) {
     const AttendArgs& a = b.a;
-    const float p = exp2f(row_score<T>(a, head, i, j) - a.lse[(size_t)head * a.T + i] * LOG2E);
+    const float lse = a.lse[(size_t)head * a.T + i];
+    const float p = lse == -__builtin_inff() ? 0.f : exp2f(row_score<T>(a, head, i, j) - lse * LOG2E);
     const float dp = dot_rows(head_row<T>(b.dout, i, head), head_row<T>(a.v, j, head / a.group), a.width);
     return make_float2(p, p == 0.f ? 0.f : p * (dp - delta));
 }
