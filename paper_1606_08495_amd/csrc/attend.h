@@ -187,19 +187,25 @@ __device__ void attend_row(const AttendArgs& a, uint32_t head, uint32_t i, const
     lse = total == 0.f ? -__builtin_inff() : (base + log2f(total)) * LN2;
 }
 
-// p and dS of (i, j), from what the forward pass left.  (A word whose shown words all have a score of -infinity weighs none.)
+// Weights are formed anew as 2^(x - high - low), x to base two.  high is the row's logarithm and low zero, but where the logarithm
+// is so large that its own rounding would show (every shown word is masked by a large finite value, or scores are huge):
+// there high is the row's largest x and low the logarithm of its sum beside it, both found anew from the scores.
+constexpr float FAR = 1024.f;         // of a logarithm: its rounding, a few 2^-13, is the relative error of the row's weights
+__device__ inline bool is_far(float lse) { return fabsf(lse) > FAR && fabsf(lse) < __builtin_inff(); }
+struct RowSum { float high, low, delta; };
+
+// p and dS of (i, j).  (A word that is shown nothing, or only scores of -infinity, has high = 0: each of its weights is zero.)
 template <typename T>
-__device__ inline float2 row_gradient(const BackwardArgs& b, uint32_t head, uint32_t i, uint32_t j, float delta) {
+__device__ inline float2 row_gradient(const BackwardArgs& b, uint32_t head, uint32_t i, uint32_t j, const RowSum& r) {
     const AttendArgs& a = b.a;
-    const float lse = a.lse[(size_t)head * a.T + i];
-    const float p = lse == -__builtin_inff() ? 0.f : exp2f(row_score<T>(a, head, i, j) - lse * LOG2E);
+    const float p = exp2f(row_score<T>(a, head, i, j) - r.high - r.low);
     const float dp = dot_rows(head_row<T>(b.dout, i, head), head_row<T>(a.v, j, head / a.group), a.width);
-    return make_float2(p, p == 0.f ? 0.f : p * (dp - delta));
+    return make_float2(p, p == 0.f ? 0.f : p * (dp - r.delta));
 }
 
 // dq_i.
 template <typename T>
-__device__ void query_row(const BackwardArgs& b, uint32_t head, uint32_t i, const Shown& s, float delta, uint32_t lane,
+__device__ void query_row(const BackwardArgs& b, uint32_t head, uint32_t i, const Shown& s, const RowSum& r, uint32_t lane,
                           float (&dq)[2]) {
     const AttendArgs& a = b.a;
     const uint32_t sunk = s.sunk - s.first, n = sunk + s.hi - s.lo;
@@ -208,7 +214,7 @@ __device__ void query_row(const BackwardArgs& b, uint32_t head, uint32_t i, cons
         const uint32_t at = at0 + lane;
         const uint32_t j = at < sunk ? s.first + at : s.lo + at - sunk;
         const bool in = at < n && row_keeps(a, i, j);
-        const float ds = in ? row_gradient<T>(b, head, i, j, delta).y : 0.f;
+        const float ds = in ? row_gradient<T>(b, head, i, j, r).y : 0.f;
         for (uint64_t left = __ballot(in && ds != 0.f); left; left &= left - 1) {
             const int l = __builtin_ctzll(left);
             const uint32_t jl = (uint32_t)__shfl((int)j, l, 64);
@@ -232,7 +238,8 @@ __device__ void key_row(const BackwardArgs& b, uint32_t kv_head, uint32_t j, uin
             const uint32_t i = i0 + lane;
             const bool in = i < hi && row_keeps(a, i, j);
             float2 g = make_float2(0.f, 0.f);
-            if (in) g = row_gradient<T>(b, head, i, j, b.delta[(size_t)head * a.T + i]);
+            const size_t at = (size_t)head * a.T + i;
+            if (in) g = row_gradient<T>(b, head, i, j, RowSum{b.high[at], b.low[at], b.delta[at]});
             for (uint64_t left = __ballot(in && g.x != 0.f); left; left &= left - 1) {
                 const int l = __builtin_ctzll(left);
                 const uint32_t il = (uint32_t)__shfl((int)i, l, 64);

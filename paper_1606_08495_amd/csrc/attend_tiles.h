@@ -84,6 +84,32 @@ struct Axis {
     __device__ __forceinline__ uint32_t token(uint32_t n) const { return n < sunk ? first + n : shift + n; }
 };
 
+// Tiles [from, to) of a block's axis.
+struct Tiles { uint32_t from, to; };
+// Keys [from, to) of the axis that those of a wavefront's words are shown which need something: words follow each other, so do
+// what they are shown.  The same in all lanes; none where from >= to.
+__device__ __forceinline__ Tiles keys_of(const Words& w, const Axis& x, bool need) {
+    const uint32_t who = (uint32_t)__ballot(need);
+    if (!who) return Tiles{~0u, 0};
+    const int one = __builtin_ctz(who), last = 31 - __builtin_clz(who);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane(w.s.lo, one), hi = (uint32_t)__builtin_amdgcn_readlane(w.s.hi, last);
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readlane(w.s.first, one), sunk = (uint32_t)__builtin_amdgcn_readlane(w.s.sunk, one);
+    const uint32_t j = sunk > first ? first : lo;
+    const uint32_t from = j - x.first < x.sunk ? j - x.first : j - x.shift, to = hi - x.shift;
+    return Tiles{from < x.count ? from : x.count, to < x.count ? to : x.count};
+}
+// The tiles of the block's, from those of its four groups of words (behind a barrier).
+__device__ __forceinline__ Tiles tiles_of(const Tiles (&groups)[GROUPS]) {
+    Tiles t{~0u, 0};
+#pragma unroll
+    for (int n = 0; n < GROUPS; ++n) {
+        t.from = groups[n].from < t.from ? groups[n].from : t.from;
+        t.to = groups[n].to > t.to ? groups[n].to : t.to;
+    }
+    if (t.from >= t.to) return Tiles{0, 0};
+    return Tiles{(uint32_t)__builtin_amdgcn_readfirstlane(t.from / KEYS), (uint32_t)__builtin_amdgcn_readfirstlane((t.to + KEYS - 1) / KEYS)};
+}
+
 // Bias by distance, times log2 e, with the outermost values repeated on both sides so that every distance within a
 // 32 x 32 piece that is not wholly past the span is in the table.
 constexpr int BIAS_SIDE = 64;
@@ -151,9 +177,10 @@ __device__ __forceinline__ void piece_scores(const AttendArgs& a, const Words& w
 template <typename T, int DB, int SPLIT> struct KeyTiles {
     Transit<T, DB, KEYS, SPLIT * THREADS> k, v;
     uint8_t keep;
-    __device__ __forceinline__ void start(const AttendArgs& a, uint32_t kv_head, const Axis& x) {
-        k.start(a.k, kv_head, (int64_t)(int32_t)x.shift);
-        v.start(a.v, kv_head, (int64_t)(int32_t)x.shift);
+    // the tile that is fetched first is tile t
+    __device__ __forceinline__ void start(const AttendArgs& a, uint32_t kv_head, const Axis& x, uint32_t t) {
+        k.start(a.k, kv_head, (int64_t)(int32_t)x.shift + (int64_t)t * KEYS);
+        v.start(a.v, kv_head, (int64_t)(int32_t)x.shift + (int64_t)t * KEYS);
         keep = 1;
     }
     __device__ __forceinline__ void fetch(const AttendArgs& a, uint32_t kv_head, const Axis& x, uint32_t t, uint32_t lane) {

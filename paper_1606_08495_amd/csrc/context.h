@@ -46,7 +46,7 @@ struct BackwardArgs {
     AttendArgs a;                                        // a.o and a.lse as the forward pass left them
     Heads dout;
     HeadsOut dq, dk, dv; float* dbias;                   // dbias [heads][n_buckets], may be null
-    float* delta;                                        // workspace: [heads][T] sums of dout o
+    float *high, *low, *delta;                           // workspace, [heads][T]: weights are 2^(x - high - low); sums of dout o
     float* by_distance; float* distance_sums;            // workspace: [heads][bias_parts][2 span + 1], [heads][2 span + 1]
     // first words that stay visible: queries further than `reach` behind their block are taken in `late` pieces of
     // late_words queries, whose sums (and those of the text's own block) lie in workspace: [late][kv_heads][sinks][2][width]

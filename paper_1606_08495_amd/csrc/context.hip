@@ -199,7 +199,7 @@ extern "C" int w2v_attend(const w2v_attend_spec* spec, const w2v_heads* q, const
 namespace {
 // The parts of the backward pass's workspace, each from a 256-byte border on.
 struct BackwardSpace {
-    size_t delta, by_distance, distance_sums, late_sums, own_sums, bytes;
+    size_t high, low, delta, by_distance, distance_sums, late_sums, own_sums, bytes;
     BackwardSpace(const w2v_attend_spec* s, uint32_t T) {
         size_t at = 0;
         const auto part = [&](size_t count) {
@@ -207,6 +207,8 @@ struct BackwardSpace {
             at += (count * sizeof(float) + 255) / 256 * 256;
             return from;
         };
+        high = part((size_t)s->heads * T);
+        low = part((size_t)s->heads * T);
         delta = part((size_t)s->heads * T);
         by_distance = part(s->bias_dev ? (size_t)s->heads * attend_bias_parts(T) * (2 * s->span + 1) : 0);
         distance_sums = part(s->bias_dev ? (size_t)s->heads * (2 * s->span + 1) : 0);
@@ -252,6 +254,8 @@ extern "C" int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads*
         b.a = attend_args(spec, q, k, v, sent_off, n_sent, n_tokens, keep, out, const_cast<float*>(lse));
         b.dout = heads_of(dout);
         b.dq = heads_out(dq); b.dk = heads_out(dk); b.dv = heads_out(dv);
+        b.high = (float*)((char*)workspace + space.high);
+        b.low = (float*)((char*)workspace + space.low);
         b.delta = (float*)((char*)workspace + space.delta);
         b.by_distance = (float*)((char*)workspace + space.by_distance);
         b.distance_sums = (float*)((char*)workspace + space.distance_sums);

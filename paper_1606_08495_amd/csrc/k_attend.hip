@@ -60,7 +60,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
 
     KeyTiles<T, DB, SPLIT> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
-    next.start(a, kv_head, x);
+    next.start(a, kv_head, x, 0);
     uint64_t kept = ~0ull;
     if (count) {
         next.fetch(a, kv_head, x, 0, lane);

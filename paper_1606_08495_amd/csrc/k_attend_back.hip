@@ -84,7 +84,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
     constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= (BIAS ? 40 : 72) * 1024 ? 2 : 1;
     constexpr int ROOM = SPLIT == 2 ? GROUPS * DB * 16 * WAVE * 4 : 0;
     __shared__ __align__(16) char tiles[BUFFERS * 2 * Tl::BYTES > ROOM ? BUFFERS * 2 * Tl::BYTES : ROOM];
-    __shared__ float deltas[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS];
+    __shared__ float deltas[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS], largest[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS];
+    __shared__ Tiles far_keys[GROUPS];
     extern __shared__ float dynamic[];
     const int32_t span = (int32_t)a.span, reach = span + BIAS_SIDE;
     const Place place;
@@ -110,8 +111,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         }
     }
     delta = real ? halves_sum(delta) : 0.f;
-    float lse2 = a.lse[(size_t)head * a.T + w.i];
-    lse2 = lse2 == -__builtin_inff() ? 0.f : lse2 * LOG2E;      // of a word that is shown nothing: every score is masked
+    const float lse = a.lse[(size_t)head * a.T + w.i];
+    const bool far = real && is_far(lse);
+    float high = lse == -__builtin_inff() ? 0.f : lse * LOG2E, low = 0.f;      // (0: of a word that is shown nothing, every score is masked)
     const Texts texts(a, word0, last, w.i_first, w.i_last, lane);
     const Axis x(a, word0, last, texts);
     w.find(a, texts, lane);
@@ -122,10 +124,6 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         fill_bias(a, head, table);
         if (b.dbias) for (int32_t c = lane; c < SKEW_FLOATS + (int32_t)bias_table(a.span); c += WAVE) skew[c] = 0.f;
     }
-    Acc dq[DB];
-#pragma unroll
-    for (int n = 0; n < DB; ++n) dq[n] = Acc{};
-    float low = 0.f, high = 0.f;
     const float unit = BIAS ? 1.f : a.scale2;
     // a half's piece of every tile is the same one: its rows are part of the lane's bases
     const uint32_t own_rows = SPLIT == 2 ? half * 32 : 0;
@@ -134,21 +132,27 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
     KeyTiles<T, DB, SPLIT> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
     const bool exact = sizeof(T) == 2 && ((BIAS && b.dbias) || x.count <= EXACT_KEYS);
-    float formed = 0.f;
-    const auto walk = [&](auto PASS) __attribute__((always_inline)) {
+    // Passes over tiles [from, to): LOGARITHMS are formed anew where they are far, then DELTA, then the GRADIENTS.
+    constexpr int LOGARITHMS = 0, DELTA = 1, GRADIENTS = 2;
+    bool walked = false;
+    float formed = 0.f, most = -__builtin_inff(), total = 0.f, before = 0.f, after = 0.f;
+    bool lowered = false;                             // whether any of the wavefront's words has a low part
+    Acc dq[DB];
+#pragma unroll
+    for (int n = 0; n < DB; ++n) dq[n] = Acc{};
+    const auto walk = [&](auto PASS, const Tiles range) __attribute__((always_inline)) {
         constexpr int pass = PASS.value;
-        next.start(a, kv_head, x);
-        uint64_t kept = ~0ull;
-        if (count) {
-            next.fetch(a, kv_head, x, 0, lane);
-            if (pass == 1 && exact) __syncthreads();  // the last tiles of the pass before
-            next.k.store(tiles, a.width);
-            next.v.store(tiles + Tl::BYTES, a.width);
-            kept = __ballot(next.keep != 0);
-        }
+        if (range.from >= range.to) return;
+        next.start(a, kv_head, x, range.from);
+        next.fetch(a, kv_head, x, range.from, lane);
+        if (walked) __syncthreads();                  // the last tiles of the pass before
+        walked = true;
+        next.k.store(tiles + range.from % BUFFERS * 2 * Tl::BYTES, a.width);
+        next.v.store(tiles + range.from % BUFFERS * 2 * Tl::BYTES + Tl::BYTES, a.width);
+        uint64_t kept = __ballot(next.keep != 0);
         __syncthreads();
-        for (uint32_t t = 0; t < count; ++t) {
-            if (t + 1 < count) next.fetch(a, kv_head, x, t + 1, lane);
+        for (uint32_t t = range.from; t < range.to; ++t) {
+            if (t + 1 < range.to) next.fetch(a, kv_head, x, t + 1, lane);
             const char *kt = tiles + t % BUFFERS * 2 * Tl::BYTES, *vt = kt + Tl::BYTES;
             const auto one = [&](uint32_t piece) __attribute__((always_inline)) {
                 const uint32_t row0 = piece * 32 + own_rows, n0 = t * KEYS + row0, j0 = n0 + x.shift;
@@ -159,31 +163,48 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
 #pragma unroll
                 for (int k = 0; k < 2 * DB; ++k) {
                     mma(Tl::along(kp, at_along, 0, k), q[k], s);
-                    mma(Tl::along(vp, at_along, 0, k), g[k], dp);
+                    if constexpr (pass != LOGARITHMS) mma(Tl::along(vp, at_along, 0, k), g[k], dp);
                 }
                 piece_scores<BIAS>(a, w, x, n0, kept >> row0, linear, table, h, s);
-                if constexpr (pass == 0) {
+                if constexpr (pass == LOGARITHMS) {
+                    float to = s[0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) to = fmaxf(to, s[r]);
+                    to = fmaxf(most, halves_max(to) * unit);
+                    if (to == -__builtin_inff()) return;      // (the same in a word's two lanes)
+                    total *= __builtin_amdgcn_exp2f(most - to);
+                    most = to;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) total += __builtin_amdgcn_exp2f(fmaf(s[r], unit, -most));
+                    return;
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit, -high);
+                if (lowered)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] -= low;
+                if constexpr (pass == DELTA) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -lse2));
+                        const float p = __builtin_amdgcn_exp2f(s[r]);
                         formed = fmaf(p, p == 0.f ? 0.f : dp[r], formed);
                     }
                     return;
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -lse2));
+                    const float p = __builtin_amdgcn_exp2f(s[r]);
                     s[r] = p * (dp[r] - delta);
                     if (BIAS && p == 0.f) s[r] = 0.f;     // the sums by distance are not formed anew
                 }
                 if constexpr (BIAS) {
                     if (b.dbias) {
-                        const int32_t far = (int32_t)j0 - (int32_t)w.i_first + 31, near = (int32_t)j0 - (int32_t)w.i_last;
-                        if (linear && (far <= -span || near >= span)) {
+                        const int32_t distant = (int32_t)j0 - (int32_t)w.i_first + 31, near = (int32_t)j0 - (int32_t)w.i_last;
+                        if (linear && (distant <= -span || near >= span)) {
                             float all = 0.f;
 #pragma unroll
                             for (int r = 0; r < 16; ++r) all += s[r];
-                            if (far <= -span) low += all; else high += all;
+                            if (distant <= -span) before += all; else after += all;
                         } else if (linear) {
                             float* const to = skew + 4 * h * (SKEW + 1) + 31 - lane % 32;
 #pragma unroll
@@ -201,8 +222,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                             for (int r = 0; r < 16; ++r) {
                                 const int32_t dist = (int32_t)x.token(per_piece(n0 + 4 * h) + acc_row(r, 0)) - (int32_t)w.i;
                                 const bool inside = dist > -span && dist < span;
-                                low += dist <= -span ? s[r] : 0.f;
-                                high += dist >= span ? s[r] : 0.f;
+                                before += dist <= -span ? s[r] : 0.f;
+                                after += dist >= span ? s[r] : 0.f;
                                 float* const to = sums + (inside ? dist + reach : 0);
                                 if (inside && h == 0) __hip_atomic_fetch_add(to, s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
                                 if (inside && h == 1) __hip_atomic_fetch_add(to, s[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
@@ -221,7 +242,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
             else
 #pragma unroll 1
                 for (uint32_t piece = 0; piece < KEYS / 32; ++piece) one(piece);
-            if (t + 1 < count) {
+            if (t + 1 < range.to) {
                 if (BUFFERS == 1) __syncthreads();
                 char* const to = tiles + (t + 1) % BUFFERS * 2 * Tl::BYTES;
                 next.k.store(to, a.width);
@@ -231,9 +252,33 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
             }
         }
     };
+    {
+        const Tiles keys = keys_of(w, x, far);
+        if (half == 0 && lane == 0) far_keys[wave] = keys;
+        __syncthreads();
+        const Tiles range = tiles_of(far_keys);
+        walk(std::integral_constant<int, LOGARITHMS>{}, range);
+        if (range.to) {
+            total = halves_sum(total);
+            if constexpr (SPLIT == 2) {
+                if (h == 0) { deltas[half][wave][lane] = total; largest[half][wave][lane] = most; }
+                __syncthreads();
+                const float m0 = largest[0][wave][lane % 32], m1 = largest[1][wave][lane % 32];
+                const float t0 = deltas[0][wave][lane % 32], t1 = deltas[1][wave][lane % 32];
+                most = fmaxf(m0, m1);
+                total = (t0 == 0.f ? 0.f : t0 * __builtin_amdgcn_exp2f(m0 - most)) + (t1 == 0.f ? 0.f : t1 * __builtin_amdgcn_exp2f(m1 - most));
+            }
+            if (far && total != 0.f) {
+                high = most;
+                low = __builtin_log2f(total);
+            }
+            lowered = __any(low != 0.f);
+        }
+    }
+    const Tiles whole{0, count};
     if constexpr (sizeof(T) == 2) {
         if (exact) {
-            walk(std::integral_constant<int, 0>{});
+            walk(std::integral_constant<int, DELTA>{}, whole);
             delta = halves_sum(formed);
             if constexpr (SPLIT == 2) {
                 if (h == 0) deltas[half][wave][lane] = delta;
@@ -242,8 +287,13 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
             }
         }
     }
-    walk(std::integral_constant<int, 1>{});
-    if (real && h == 0 && half == 0) b.delta[(size_t)head * a.T + w.i] = delta;
+    walk(std::integral_constant<int, GRADIENTS>{}, whole);
+    if (real && h == 0 && half == 0) {
+        const size_t at = (size_t)head * a.T + w.i;
+        b.high[at] = high;
+        b.low[at] = low;
+        b.delta[at] = delta;
+    }
     bool mine = true;
     if constexpr (SPLIT == 2) mine = join_halves(( float*)tiles, dq, wave, half, lane);
     if (some && mine) {
@@ -256,7 +306,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
             s.first = __shfl(w.s.first, l, 64); s.sunk = __shfl(w.s.sunk, l, 64);
             const uint32_t i = __shfl(w.i, l, 64);
             float row[2];
-            query_row<T>(b, head, i, s, __shfl(delta, l, 64), lane, row);
+            query_row<T>(b, head, i, s, RowSum{__shfl(high, l, 64), __shfl(low, l, 64), __shfl(delta, l, 64)}, lane, row);
             T* to = head_row<T>(b.dq, i, head);
 #pragma unroll
             for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) to[lane + c * WAVE] = (T)row[c];
@@ -267,9 +317,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         // the outermost distances: what lies past the span in the array, and what went by registers
         __syncthreads();
         static_assert(BIAS_SIDE == 64, "one place a lane on either side");
-        low = lanes_sum<64>(low + sums[lane]);
-        high = lanes_sum<64>(high + sums[2 * reach - lane]);
-        if (lane == 0) { sums[BIAS_SIDE] += low; sums[2 * reach - BIAS_SIDE] += high; }
+        before = lanes_sum<64>(before + sums[lane]);
+        after = lanes_sum<64>(after + sums[2 * reach - lane]);
+        if (lane == 0) { sums[BIAS_SIDE] += before; sums[2 * reach - BIAS_SIDE] += after; }
         __syncthreads();
         float* to = b.by_distance + ((size_t)head * words + part) * (2 * span + 1);
         for (int32_t c = threadIdx.x; c <= 2 * span; c += SPLIT * THREADS) {
@@ -304,7 +354,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     constexpr bool OWN = SPLIT == 2 && own_rows_in_lds<T, DB>;
     typedef Tile<T, DB, BLOCK_WORDS> Ow;
     __shared__ __align__(16) char own[OWN ? 2 * Ow::BYTES : 16];
-    __shared__ float rows[BUFFERS][2][KEYS];          // the queries' logarithms to base two, and delta
+    __shared__ float rows[BUFFERS][3][KEYS];          // of the queries: high, delta, low
     extern __shared__ float table[];
     const Place place;
     const uint32_t lane = place.lane, h = place.h, wave = place.wave, half = place.half;
@@ -395,7 +445,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     // a half's piece of every tile is the same one: its rows are part of the lane's bases
     const uint32_t own_rows = SPLIT == 2 ? half * 32 : 0;
     const uint32_t at_along = Tl::base_along(lane) + own_rows / 4 * Tl::STRIDE, at_across = Tl::base_across(lane) + own_rows / 4 * Tl::STRIDE;
-    float lse2 = 0.f, delta = 0.f;
+    float high = 0.f, low = 0.f, delta = 0.f;
+    bool lowered = false;                             // whether any of a tile's queries has a low part
     const uint32_t per_head = q1 > q0 ? (q1 - q0 + KEYS - 1) / KEYS : 0, count = per_head * a.group;
     const auto fetch = [&](uint32_t t) __attribute__((always_inline)) {
         const uint32_t head = kv_head * a.group + t / per_head, i0 = q0 + t % per_head * KEYS;
@@ -414,16 +465,19 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
         tq.load(a.width);
         tg.load(a.width);
         const uint32_t i = i0 + threadIdx.x % KEYS < q1 ? i0 + threadIdx.x % KEYS : q1 - 1;
-        lse2 = a.lse[(size_t)head * a.T + i];
+        high = b.high[(size_t)head * a.T + i];
+        low = b.low[(size_t)head * a.T + i];
         delta = b.delta[(size_t)head * a.T + i];
     };
     const auto put = [&](uint32_t t) __attribute__((always_inline)) {
         tq.store(tiles + t % BUFFERS * 2 * Tl::BYTES, a.width);
         tg.store(tiles + t % BUFFERS * 2 * Tl::BYTES + Tl::BYTES, a.width);
         if (threadIdx.x < KEYS) {
-            rows[t % BUFFERS][0][threadIdx.x] = lse2 == -__builtin_inff() ? 0.f : lse2 * LOG2E;
+            rows[t % BUFFERS][0][threadIdx.x] = high;
             rows[t % BUFFERS][1][threadIdx.x] = delta;
+            rows[t % BUFFERS][2][threadIdx.x] = low;
         }
+        lowered = __any(low != 0.f);                  // (a wavefront's lanes hold all of the tile's queries)
     };
     if (count) {
         fetch(0);
@@ -454,13 +508,13 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
                 }
             }
             __builtin_amdgcn_sched_barrier(0);        // (what the next products read is not asked for before: registers)
-            const float *l2 = &rows[t % BUFFERS][0][row0 + 4 * h], *dl = l2 + KEYS;
+            const float *l2 = &rows[t % BUFFERS][0][row0 + 4 * h], *dl = l2 + KEYS, *ll = dl + KEYS;
             if constexpr (BIAS) {
                 const int32_t far = (int32_t)j_last - (int32_t)i0, near = (int32_t)j_first - (int32_t)i0 - 31;
                 if (far <= -(int32_t)a.span || near >= (int32_t)a.span) {
                     const float c = table[far <= -(int32_t)a.span ? 0 : 2 * reach];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, c - l2[acc_row(r, 0)]);
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, c) - l2[acc_row(r, 0)];
                 } else {
                     const float* at = table + ((int32_t)j - (int32_t)i0 + reach - 4 * (int32_t)h);
 #pragma unroll
@@ -470,6 +524,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, -l2[acc_row(r, 0)]);
             }
+            if (lowered)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] -= ll[acc_row(r, 0)];
             if (!(i0 >= lo_most && i0 + 32 <= hi_least && !(a.skip_self && i0 <= j_last && i0 + 32 > j_first))) {
                 const uint32_t base = per_piece(i0 + 4 * h);
 #pragma unroll

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from attend_reference import attend_reference, check
+from attend_reference import E_SUM, ROUND, attend_reference, check
 from paper_1606_08495_amd import w2v
 from test_gpu_attend import offsets_of, rows, whole
 
@@ -54,3 +54,104 @@ def test_words_that_an_infinite_bias_leaves_nothing(ty):
     for at in (0, 40, 41):
         assert not got[0][at].any() and not got[2][at].any() and (got[1][:, at] == -math.inf).all()
     assert not got[3][40].any() and not got[4][40].any()     # a text of one word
+
+
+FAR = [-1e30, -1e37, -1e9, -3e5, 1e9]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("low", FAR)
+def test_words_that_see_only_what_a_finite_mask_hides(low, ty):
+    """A word's own place carries a mask of a finite value.  Where others are shown, the mask leaves it no weight (or, where it is
+    positive, all of it); the first word of a text has nothing else and weighs itself with one."""
+    lengths, H, d = [140, 1, 3, 300, 33], 2, 60
+    T, off = sum(lengths), offsets_of(lengths)
+    first = torch.tensor(off[:-1])
+    q, k, v, dout = rows(T, H, 2, d, ty, 12)
+    bias, bmap = by_distance(0.0, low, 0.0)
+    for see in (dict(left=None, right=0), dict(left=20, right=0, sinks=2)):
+        if low < 0:                                          # as with the word itself left out, but for the first words
+            ref = attend_reference(q, k, v, off, skip_self=True, dout=dout, **see)
+            u, one = ROUND[ty], [t[first].double() for t in (q, k, v, dout)]
+            rough = (u + E_SUM) * 2 * (one[3].abs() * one[2].abs()).sum(2, keepdim=True)      # of dS, with a weight of one
+            for name, t in (("out", one[2]), ("dv", one[3])):
+                ref[name][first] += t
+                ref[name + "_bound"][first] += (2 * u + E_SUM) * t.abs()
+            ref["dq_bound"][first] += d ** -0.5 * rough * one[1].abs()
+            ref["dk_bound"][first] += d ** -0.5 * rough * one[0].abs()
+        else:
+            ref = attend_reference(q, k, v, off, left=0, right=0, dout=dout)
+        # scores beside a mask: theirs is all that the logarithm says
+        own = (q[:, :, None] * k[:, :, None]).double().sum(3)[:, :, 0].T * d ** -0.5 + low
+        at = first if low < 0 else torch.arange(T)
+        ref["lse"][:, at], ref["lse_bound"][:, at] = own[:, at], 2.0 ** -21 * own[:, at].abs()
+        got = whole(q.cuda(), k.cuda(), v.cuda(), dout.cuda(), torch.tensor(off, device="cuda"), bias=bias.repeat(H, 1).cuda(),
+                    buckets=bmap.cuda(), **see)
+        compare(got[:5], ref, ty)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("low", FAR[:2])
+def test_texts_that_a_finite_mask_hides_wholly(low, ty):
+    """Every word carries the mask: scores are lost beside it (in 64 bits too), and all weights are equal."""
+    n, H, d = 300, 2, 48
+    q, k, v, dout = rows(n, H, 1, d, ty, 13)
+    u, scale = ROUND[ty], d ** -0.5
+    bias, bmap = torch.full((H, 2), low), w2v.relative_buckets(2, 5, device="cpu")
+    got = whole(q.cuda(), k.cuda(), v.cuda(), dout.cuda(), device_offsets([n]), bias=bias.cuda(), buckets=bmap.cuda())
+    Q, K, V, G = [t.double() for t in (q, k[:, 0], v[:, 0], dout)]
+    ref = dict(dk=torch.zeros(n, 1, d), dv=torch.zeros(n, 1, d), dk_bound=torch.zeros(n, 1, d), dv_bound=torch.zeros(n, 1, d))
+    ref = {name: t.double() for name, t in ref.items()}
+    ref.update({name: torch.zeros(n, H, d, dtype=torch.float64) for name in ("out", "dq", "out_bound", "dq_bound")})
+    for h in range(H):
+        o = V.mean(0)
+        delta, size = G[:, h] @ o, G[:, h].abs() @ o.abs()
+        ds = (G[:, h] @ V.T - delta[:, None]) / n
+        rough = ((G[:, h].abs() @ V.abs().T + size[:, None]) * E_SUM + u * size[:, None]) / n + (u + E_SUM) * ds.abs()
+        ref["out"][:, h], ref["out_bound"][:, h] = o, (u + E_SUM) * V.abs().mean(0) + u * o.abs()
+        ref["dq"][:, h], ref["dq_bound"][:, h] = scale * ds @ K, scale * rough @ K.abs()
+        ref["dk"][:, 0] += scale * ds.T @ Q[:, h]
+        ref["dk_bound"][:, 0] += scale * rough.T @ Q[:, h].abs()
+        ref["dv"][:, 0] += G[:, h].mean(0)
+        ref["dv_bound"][:, 0] += (u + E_SUM) * G[:, h].abs().mean(0)
+    for name in ("dq", "dk", "dv"):
+        ref[name + "_bound"] += u * ref[name].abs()
+    ref["lse"] = torch.full((H, n), low, dtype=torch.float64)
+    ref["lse_bound"] = 2.0 ** -21 * ref["lse"].abs()
+    compare(got[:5], ref, ty)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, BF16])
+def test_scores_of_many_millions(ty):
+    """Rows that one word takes wholly: its weight is one, whatever the scores' size."""
+    n, H, d = 200, 2, 64
+    q, k, v, dout = rows(n, H, H, d, ty, 14)
+    q, k = q * 3000, k * 3000
+    got = whole(q.cuda(), k.cuda(), v.cuda(), dout.cuda(), device_offsets([n]), right=0)
+    ref = {name: torch.zeros(n, H, d, dtype=torch.float64) for name in ("out", "dq", "dk", "dv")}
+    ref["lse"] = torch.zeros(H, n, dtype=torch.float64)
+    for h in range(H):
+        x = q[:, h].double() @ k[:, h].double().T / 8
+        x = torch.where(torch.ones(n, n).tril() > 0, x, -math.inf)
+        best, at = x.max(1)
+        gap = x[1:].topk(2).values
+        clear = torch.ones(n, dtype=torch.bool)
+        clear[1:] = gap[:, 0] - gap[:, 1] > 1000             # (a score is off by 128 2^-24 of a few 10^8 at most)
+        assert clear.all()
+        ref["out"][:, h], ref["lse"][h] = v[at, h].double(), best
+        ref["dv"][:, h].index_add_(0, at, dout[:, h].double())
+    u = ROUND[ty]
+    ref["out_bound"], ref["lse_bound"] = (2 * u + E_SUM) * ref["out"].abs(), 2.0 ** -19 * ref["lse"].abs()
+    ref["dv_bound"] = u * ref["dv"].abs()
+    for h in range(H):
+        at = (torch.where(torch.ones(n, n).tril() > 0, q[:, h].double() @ k[:, h].double().T, -math.inf)).argmax(1)
+        ref["dv_bound"][:, h].index_add_(0, at, 2 * (u + E_SUM) * dout[:, h].double().abs())
+    compare((got[0], got[1]), ref, ty)
+    check(got[4], ref, "dv", ty)
+    # dS = p (dP - delta) with p = 1: what the rounding of delta leaves, times rows of some thousands
+    size = (dout.double().abs() * v.double().abs().max()).sum(2).max()
+    for t in got[2:4]:
+        assert float(t.double().abs().max()) <= float(n * (2 * u + E_SUM) * size * q.double().abs().max())
