@@ -105,18 +105,22 @@ __device__ inline Shown sees(const AttendArgs& a, uint32_t j, Text t) {
 }
 
 // ---- bias --------------------------------------------------------------------------------------------
-// The bias of a distance, times log2 e.  Values that would leave fp32 with that factor are held at the last that do
-// not, infinities are kept; a bucket past the last adds nothing.
-__device__ inline float scaled_bias(const float* bias, const uint32_t* buckets, uint32_t n_buckets, uint32_t reach, uint32_t head,
-                                    int32_t dist) {
+// The bias of a distance; a bucket past the last adds nothing.
+__device__ inline float plain_bias(const float* bias, const uint32_t* buckets, uint32_t n_buckets, uint32_t reach, uint32_t head,
+                                   int32_t dist) {
     const int32_t span = (int32_t)reach;
     const int32_t at = (dist < -span ? -span : dist > span ? span : dist) + span;
     const uint32_t b = buckets[at];
-    if (b >= n_buckets) return 0.f;
-    const float x = bias[(size_t)head * n_buckets + b];
+    return b < n_buckets ? bias[(size_t)head * n_buckets + b] : 0.f;
+}
+// The same times log2 e.  Values that would leave fp32 with that factor are held where they do not; infinities are kept.  A row
+// whose largest score is about as large as a held value is formed a word at a time, without the factor.
+constexpr float BIAS_HELD = 2.3e38f, HELD = 3.2e38f;
+__device__ inline float scaled_bias(const float* bias, const uint32_t* buckets, uint32_t n_buckets, uint32_t reach, uint32_t head,
+                                    int32_t dist) {
+    const float x = plain_bias(bias, buckets, n_buckets, reach, head, dist);
     if (!(fabsf(x) < __builtin_inff())) return x;
-    const float most = 1.7e38f;
-    return fminf(fmaxf(x, -most), most) * LOG2E;
+    return fminf(fmaxf(x, -BIAS_HELD), BIAS_HELD) * LOG2E;
 }
 __device__ inline float scaled_bias(const AttendArgs& a, uint32_t head, int32_t dist) {
     return scaled_bias(a.bias, a.buckets, a.n_buckets, a.span, head, dist);
@@ -132,7 +136,12 @@ template <typename T> __device__ inline float dot_rows(const T* x, const T* y, u
     return s;
 }
 
-// The score of (i, j) to base two; whether j is kept is the caller's to ask.
+// The score of (i, j), as it is and to base two; whether j is kept is the caller's to ask.
+template <typename T>
+__device__ inline float row_plain_score(const AttendArgs& a, uint32_t head, uint32_t i, uint32_t j) {
+    const float s = dot_rows(head_row<T>(a.q, i, head), head_row<T>(a.k, j, head / a.group), a.width) * a.scale;
+    return a.bias ? s + plain_bias(a.bias, a.buckets, a.n_buckets, a.span, head, (int32_t)j - (int32_t)i) : s;
+}
 template <typename T>
 __device__ inline float row_score(const AttendArgs& a, uint32_t head, uint32_t i, uint32_t j) {
     const float s = dot_rows(head_row<T>(a.q, i, head), head_row<T>(a.k, j, head / a.group), a.width) * a.scale2;
@@ -156,7 +165,7 @@ __device__ void attend_row(const AttendArgs& a, uint32_t head, uint32_t i, const
     for (uint32_t at = lane; at < n; at += WAVE) {
         const uint32_t j = at < sunk ? s.first + at : s.lo + at - sunk;
         if (!row_keeps(a, i, j)) continue;
-        const float x = row_score<T>(a, head, i, j);
+        const float x = row_plain_score<T>(a, head, i, j);
         nan |= x != x;
         m = fmaxf(m, x);
     }
@@ -169,7 +178,7 @@ __device__ void attend_row(const AttendArgs& a, uint32_t head, uint32_t i, const
         const uint32_t at = at0 + lane;
         const uint32_t j = at < sunk ? s.first + at : s.lo + at - sunk;
         const bool in = at < n && row_keeps(a, i, j);
-        const float p = in ? exp2f(row_score<T>(a, head, i, j) - base) : 0.f;
+        const float p = in ? exp2f((row_plain_score<T>(a, head, i, j) - base) * LOG2E) : 0.f;
         total += p;
         for (uint64_t left = __ballot(in && p != 0.f); left; left &= left - 1) {
             const int l = __builtin_ctzll(left);
@@ -184,7 +193,7 @@ __device__ void attend_row(const AttendArgs& a, uint32_t head, uint32_t i, const
     const float inv = total == 0.f ? 0.f : 1.f / total;
     o[0] *= inv;
     o[1] *= inv;
-    lse = total == 0.f ? -__builtin_inff() : (base + log2f(total)) * LN2;
+    lse = total == 0.f ? -__builtin_inff() : base + log2f(total) * LN2;
 }
 
 // Weights are formed anew as 2^(x - high - low), x to base two.  high is the row's logarithm and low zero, but where the logarithm

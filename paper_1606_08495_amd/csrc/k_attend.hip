@@ -184,7 +184,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
             worst = fmaf(o[b][r], 0.f, worst);
         }
     worst = halves_sum(worst);
-    const bool redo = worst != 0.f;
+    const bool redo = worst != 0.f || (BIAS && total != 0.f && fabsf(m) >= HELD);
     if (real && !redo) {
         T* out = head_row<T>(a.o, w.i, head);
 #pragma unroll

@@ -56,7 +56,7 @@ def test_words_that_an_infinite_bias_leaves_nothing(ty):
     assert not got[3][40].any() and not got[4][40].any()     # a text of one word
 
 
-FAR = [-1e30, -1e37, -1e9, -3e5, 1e9]
+FAR = [torch.finfo(F32).min, -1e30, -1e37, -1e9, -3e5, 1e9]
 
 
 @pytest.mark.gpu
@@ -93,7 +93,7 @@ def test_words_that_see_only_what_a_finite_mask_hides(low, ty):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("ty", [F32, F16, BF16])
-@pytest.mark.parametrize("low", FAR[:2])
+@pytest.mark.parametrize("low", FAR[:3])
 def test_texts_that_a_finite_mask_hides_wholly(low, ty):
     """Every word carries the mask: scores are lost beside it (in 64 bits too), and all weights are equal."""
     n, H, d = 300, 2, 48
