@@ -7,7 +7,7 @@
 // products a pair), another holds 128 words as keys and walks over the queries they are shown to (dk, dv; four products a
 // pair).  That is seven products instead of the five of a kernel that adds dq up in memory.  In both a
 // wavefront's own 32 words are the lanes, their rows feed the B operands from registers, and p and dS feed the last
-// products from the registers they are formed in; p and dS are rounded to the rows' type there, all sums are fp32.
+// products from the registers they are formed in; p and dS are rounded to the rows' type there (in fp16 behind a power of two, see lift_piece), all sums are fp32.
 //
 // A text's first words that stay visible are seen by every later word.  The keys' kernel takes the queries up to a
 // border behind its block; those behind go in pieces to blocks of their own (late), whose sums are joined in
@@ -45,6 +45,30 @@ template <int DB> __device__ inline bool not_finite(const Acc (&c)[DB]) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) worst = fmaf(c[b][r], 0.f, worst);
     return halves_sum(worst) != 0.f;
+}
+
+// fp16 holds 2^-24 .. 2^16, and dS = p (dP - delta) is as small as the outputs' gradient over the number of words: rounded as it
+// is, a mean's gradient over some thousand words would lose most of its bits.  Before it is rounded, a word's dS (a lane's column)
+// is therefore multiplied by a power of two, `lift`, which its sums carry too: as high as its largest value so far allows, so
+// that this one lies at 2^9 or above, terms down to 2^-23 of it keep all bits, and none overflows.  Weights as they enter dv's products
+// are lifted by 2^14 from the start: none is above one.  (bf16 and fp32 have fp32's range and need neither.)
+template <typename T> constexpr bool lifts = std::is_same<T, _Float16>::value;
+template <typename T> constexpr float WEIGHT_LIFT = lifts<T> ? 14.f : 0.f;      // to base two
+constexpr float FIRST_LIFT = 0x1p100f, LIFTED_MOST = 0x1p15f;
+template <int N> __device__ __forceinline__ void lift_piece(Acc& ds, Acc (&sum)[N], float& lift) {
+    float most = fabsf(ds[0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) most = fmaxf(most, fabsf(ds[r]));
+    most = halves_max(most);
+    if (__any(most * lift >= LIFTED_MOST)) {
+        const float to = most * lift >= LIFTED_MOST ? __builtin_amdgcn_ldexpf(1.f, 10 - __builtin_amdgcn_frexp_expf(most)) : lift;
+        const float factor = to / lift;
+#pragma unroll
+        for (int n = 0; n < N; ++n) sum[n] *= factor;
+        lift = to;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ds[r] *= lift;
 }
 
 // Joins what two halves of a block have summed for the same words: the second's through LDS to the first.  True for the half
@@ -137,6 +161,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
     bool walked = false;
     float formed = 0.f, most = -__builtin_inff(), total = 0.f, before = 0.f, after = 0.f;
     bool lowered = false;                             // whether any of the wavefront's words has a low part
+    float lift = lifts<T> ? FIRST_LIFT : 1.f;
     Acc dq[DB];
 #pragma unroll
     for (int n = 0; n < DB; ++n) dq[n] = Acc{};
@@ -231,6 +256,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                         }
                     }
                 }
+                if constexpr (lifts<T>) lift_piece(s, dq, lift);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const auto ds = acc_operand<T>(s, k);
@@ -294,6 +320,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         b.low[at] = low;
         b.delta[at] = delta;
     }
+    if constexpr (lifts<T>)
+#pragma unroll
+        for (int n = 0; n < DB; ++n) dq[n] *= 1.f / lift;
     bool mine = true;
     if constexpr (SPLIT == 2) mine = join_halves(( float*)tiles, dq, wave, half, lane);
     if (some && mine) {
@@ -447,6 +476,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     const uint32_t at_along = Tl::base_along(lane) + own_rows / 4 * Tl::STRIDE, at_across = Tl::base_across(lane) + own_rows / 4 * Tl::STRIDE;
     float high = 0.f, low = 0.f, delta = 0.f;
     bool lowered = false;                             // whether any of a tile's queries has a low part
+    float lift = lifts<T> ? FIRST_LIFT : 1.f;
     const uint32_t per_head = q1 > q0 ? (q1 - q0 + KEYS - 1) / KEYS : 0, count = per_head * a.group;
     const auto fetch = [&](uint32_t t) __attribute__((always_inline)) {
         const uint32_t head = kv_head * a.group + t / per_head, i0 = q0 + t % per_head * KEYS;
@@ -472,6 +502,11 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
     const auto put = [&](uint32_t t) __attribute__((always_inline)) {
         tq.store(tiles + t % BUFFERS * 2 * Tl::BYTES, a.width);
         tg.store(tiles + t % BUFFERS * 2 * Tl::BYTES + Tl::BYTES, a.width);
+        if constexpr (lifts<T>) {                     // 2^14 p: from high, unless that is so large that it would be lost there
+            const bool far = fabsf(high) > FAR;
+            high -= far ? 0.f : WEIGHT_LIFT<T>;
+            low -= far ? WEIGHT_LIFT<T> : 0.f;
+        }
         if (threadIdx.x < KEYS) {
             rows[t % BUFFERS][0][threadIdx.x] = high;
             rows[t % BUFFERS][1][threadIdx.x] = delta;
@@ -541,6 +576,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
                 s[r] = __builtin_amdgcn_exp2f(s[r]);
                 dp[r] = s[r] * (dp[r] - dl[acc_row(r, 0)]);
             }
+            if constexpr (lifts<T>) lift_piece(dp, dk, lift);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (sizeof(T) == 4) {
                 // a piece's sum first, then to the whole: a text's queries and heads would make one long chain of roundings
@@ -577,6 +613,12 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
             if (BUFFERS == 2) __syncthreads();
         }
     }
+    if constexpr (lifts<T>)
+#pragma unroll
+        for (int n = 0; n < DB; ++n) {
+            dk[n] *= 0x1p-14f / lift;
+            dv[n] *= 0x1p-14f;
+        }
     if constexpr (SPLIT == 2) {
         const bool mine = join_halves((float*)tiles, dk, wave, half, lane);
         join_halves((float*)tiles, dv, wave, half, lane);

@@ -155,3 +155,25 @@ def test_scores_of_many_millions(ty):
     size = (dout.double().abs() * v.double().abs().max()).sum(2).max()
     for t in got[2:4]:
         assert float(t.double().abs().max()) <= float(n * (2 * u + E_SUM) * size * q.double().abs().max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [1.0, 1e-3, 1e-4, 1e-5, 3e3])
+@pytest.mark.parametrize("d", [32, 100])
+def test_small_and_large_gradients_in_16_bits(d, size):
+    """Gradients of fp16 outputs as training has them: a mean over thousands of words, or a scaled loss.  What is rounded on the way
+    must not cost more than the results' own rounding, whatever the size."""
+    lengths = [3000, 200]
+    T, off = sum(lengths), offsets_of(lengths)
+    q, k, v, dout = rows(T, 1, 1, d, F16, 15)
+    dout = (dout * size).to(F16)
+    with torch.device("cuda"):
+        ref = attend_reference(*[t.cuda() for t in (q, k, v)], off, right=0, dout=dout.cuda())
+    ref = {name: t.cpu() for name, t in ref.items()}
+    got = whole(q.cuda(), k.cuda(), v.cuda(), dout.cuda(), torch.tensor(off, device="cuda"), right=0)
+    compare(got, ref, F16)
+    for t, name in zip(got[2:], ("dq", "dk", "dv")):
+        exact = ref[name]
+        own = float((exact.to(F16).double() - exact).norm() / exact.norm())
+        # beside the result's rounding: dS's and delta's, relative ones of 2^-11 at most, of terms that add up at random
+        assert float((t.double().cpu() - exact).norm() / exact.norm()) <= 1.2 * own + 2.0 ** -11, name
