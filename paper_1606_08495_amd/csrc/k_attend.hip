@@ -10,7 +10,7 @@
 // its words is shown are skipped, those that all of them are shown take no mask.
 //
 // Scores, maxima, sums and outputs are fp32.  Weights are rounded to the type of v for the second product, relative to the
-// row's maximum (or to one at most 2^8 below it: outputs are rescaled only when the maximum has risen by more), which
+// row's maximum (or to one a little below it: outputs are rescaled only when the maximum has risen by more, see RISE), which
 // leaves them the relative rounding that v has; their sum is taken before the rounding.  Heads of up to 32 columns add
 // what the rounding left in a second product: the gradient's dout . out is then a sum of few terms, which
 // may cancel down to the weights' rounding, and the matrix cores wait for the exponentials there anyway.
@@ -23,7 +23,11 @@
 namespace w2v {
 namespace {
 
-constexpr float RISE = 8.f;           // how far (to base two) a maximum may rise before outputs are rescaled
+// How far (to base two) a maximum may rise before outputs are rescaled, and what weights are lifted by before they are rounded.
+// fp16 would lose weights below 2^-25 of the row's maximum altogether, of which a long text may hold 10^5, and round those below 2^-14
+// coarsely; lifted, these are 2^-38 and 2^-27, and none is above 2^15.
+template <typename T> constexpr float RISE = std::is_same<T, _Float16>::value ? 2.f : 8.f;
+template <typename T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 13.f : 0.f;
 
 template <typename T, int DB, bool BIAS, int SPLIT>
 __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void attend_kernel(const AttendArgs a) {
@@ -90,7 +94,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[p][r]);
             }
             most = halves_max(most) * unit;
-            if (__any(most > m + RISE)) {
+            if (__any(most > m + RISE<T>)) {
                 const float to = fmaxf(m, most);
                 const float factor = to == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - to);
                 m = to;
@@ -98,7 +102,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
 #pragma unroll
                 for (int b = 0; b < DB; ++b) o[b] *= factor;
             }
-            const float base = m == -__builtin_inff() ? 0.f : m;
+            const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
 #pragma unroll
             for (int g = 0; g < 2 * P.value; ++g) {   // 16 keys
                 const int p = g / 2;
@@ -201,7 +205,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
                     for (int e = 0; e < 4; ++e) if (c + e < a.width) out[c + e] = four[e];
             }
         if (h == 0 && a.lse)
-            a.lse[(size_t)head * a.T + w.i] = total == 0.f ? -__builtin_inff() : (m + __builtin_log2f(total)) * LN2;
+            a.lse[(size_t)head * a.T + w.i] = total == 0.f ? -__builtin_inff() : (m - LIFT<T> + __builtin_log2f(total)) * LN2;
     }
     // what a word is not shown must not show: rows that are not finite are formed from their words alone
     for (uint64_t rows = __ballot(redo && real && h == 0); rows; rows &= rows - 1) {

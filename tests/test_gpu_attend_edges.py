@@ -177,3 +177,15 @@ def test_small_and_large_gradients_in_16_bits(d, size):
         own = float((exact.to(F16).double() - exact).norm() / exact.norm())
         # beside the result's rounding: dS's and delta's, relative ones of 2^-11 at most, of terms that add up at random
         assert float((t.double().cpu() - exact).norm() / exact.norm()) <= 1.2 * own + 2.0 ** -11, name
+
+
+@pytest.mark.gpu
+def test_small_weights_in_16_bits():
+    """One word far above very many others that share a part of the weight: theirs are 2^-26 of the largest."""
+    n, d = 1 << 17, 16
+    q, k, v = torch.zeros(n, 1, d), torch.zeros(n, 1, d), torch.ones(n, 1, d)
+    q[-1, 0, 0], k[0, 0, 0], v[0] = 8.0, 26 * math.log(2) / 2, 0.0       # scale 1/4: 26 ln 2 above the rest
+    out, _ = w2v.attend(q.to(F16).cuda(), k.to(F16).cuda(), v.to(F16).cuda(), device_offsets([n]), right=0)
+    x = 2 * float(k[0, 0, 0].to(F16))
+    want = (n - 1) * math.exp(-x) / (1 + (n - 1) * math.exp(-x))         # about 2^-9
+    assert torch.allclose(out[-1].double().cpu(), torch.full((1, d), want, dtype=torch.float64), rtol=2.0 ** -9, atol=0)
