@@ -93,8 +93,10 @@ template <int N> __device__ __forceinline__ bool join_halves(float* room, Acc (&
 // ---- queries: dq, delta, the bias' sums -----------------------------------------------------------------
 // delta is taken from out as it was rounded, or, where that would show, formed from the scores in a pass of its own before the
 // others (sum of p dP, which needs neither out nor its rounding): for the bias' gradient, an fp32 sum over all pairs, and for
-// words that are shown few others, whose out is large.  EXACT_KEYS is from where on the rounding of dS hides that of out.
-constexpr uint32_t EXACT_KEYS = 512;
+// words that are shown few others (kept or not), whose out is large.  Which it is depends on the word alone, not on
+// those that share its block.  With normal inputs, out's rounding adds to the error of dq, whose own rounding and dS' make most of
+// it: 56 % of it at 2 words, 10 % at 8, 3 % at 32, 2 % at 64, below 1.5 % from 128 on.
+constexpr uint32_t EXACT_WORDS = 128;
 
 // Sums of dS by distance.  A piece's 32 x 32 values have 63 distances.  They go through LDS, each row moved by its number so that a
 // distance is a column (SKEW floats a row; what a row does not fill stays zero), and a lane adds up one column.
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
     constexpr int ROOM = SPLIT == 2 ? GROUPS * DB * 16 * WAVE * 4 : 0;
     __shared__ __align__(16) char tiles[BUFFERS * 2 * Tl::BYTES > ROOM ? BUFFERS * 2 * Tl::BYTES : ROOM];
     __shared__ float deltas[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS], largest[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS];
-    __shared__ Tiles far_keys[GROUPS];
+    __shared__ Tiles far_keys[GROUPS], delta_keys[GROUPS];
     extern __shared__ float dynamic[];
     const int32_t span = (int32_t)a.span, reach = span + BIAS_SIDE;
     const Place place;
@@ -155,7 +157,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
 
     KeyTiles<T, DB, SPLIT> next;
     const uint32_t count = (x.count + KEYS - 1) / KEYS;
-    const bool exact = sizeof(T) == 2 && ((BIAS && b.dbias) || x.count <= EXACT_KEYS);
+    const bool exact = sizeof(T) == 2 && real &&
+                       ((BIAS && b.dbias) || w.s.hi - w.s.lo + w.s.sunk - w.s.first <= EXACT_WORDS);
+    const bool some_exact = __any(exact);
     // Passes over tiles [from, to): LOGARITHMS are formed anew where they are far, then DELTA, then the GRADIENTS.
     constexpr int LOGARITHMS = 0, DELTA = 1, GRADIENTS = 2;
     bool walked = false;
@@ -184,6 +188,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                 const char *kp = kt + piece * (32 / 4) * Tl::STRIDE, *vp = vt + piece * (32 / 4) * Tl::STRIDE;
                 const bool linear = n0 >= x.sunk;
                 if (!some || n0 >= x.count || (linear && !w.shown_any(j0))) return;
+                if (pass == DELTA && !some_exact) return;
                 Acc s = {}, dp = {};
 #pragma unroll
                 for (int k = 0; k < 2 * DB; ++k) {
@@ -279,8 +284,11 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         }
     };
     {
-        const Tiles keys = keys_of(w, x, far);
-        if (half == 0 && lane == 0) far_keys[wave] = keys;
+        const Tiles keys = keys_of(w, x, far), more = keys_of(w, x, exact);
+        if (half == 0 && lane == 0) {
+            far_keys[wave] = keys;
+            delta_keys[wave] = more;
+        }
         __syncthreads();
         const Tiles range = tiles_of(far_keys);
         walk(std::integral_constant<int, LOGARITHMS>{}, range);
@@ -303,14 +311,16 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
     }
     const Tiles whole{0, count};
     if constexpr (sizeof(T) == 2) {
-        if (exact) {
-            walk(std::integral_constant<int, DELTA>{}, whole);
-            delta = halves_sum(formed);
+        const Tiles range = tiles_of(delta_keys);
+        if (range.to) {
+            walk(std::integral_constant<int, DELTA>{}, range);
+            formed = halves_sum(formed);
             if constexpr (SPLIT == 2) {
-                if (h == 0) deltas[half][wave][lane] = delta;
+                if (h == 0) deltas[half][wave][lane] = formed;
                 __syncthreads();
-                delta = deltas[0][wave][lane % 32] + deltas[1][wave][lane % 32];
+                formed = deltas[0][wave][lane % 32] + deltas[1][wave][lane % 32];
             }
+            delta = exact ? formed : delta;
         }
     }
     walk(std::integral_constant<int, GRADIENTS>{}, whole);

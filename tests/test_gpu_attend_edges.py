@@ -189,3 +189,40 @@ def test_small_weights_in_16_bits():
     x = 2 * float(k[0, 0, 0].to(F16))
     want = (n - 1) * math.exp(-x) / (1 + (n - 1) * math.exp(-x))         # about 2^-9
     assert torch.allclose(out[-1].double().cpu(), torch.full((1, d), want, dtype=torch.float64), rtol=2.0 ** -9, atol=0)
+
+
+def strict(q, k, v, dout, see):
+    """dq of one text and its bound where delta is not taken from outputs that were rounded."""
+    r = attend_reference(q, k, v, [0, q.shape[0]], dout=dout, **see)
+    n, d, u = q.shape[0], q.shape[2], ROUND[q.dtype]
+    Q, K, V, G = [t[:, 0].double() for t in (q, k, v, dout)]
+    i, j = torch.arange(n)[:, None], torch.arange(n)[None]
+    x = torch.where((j <= i) & (j >= i - see["left"]), d ** -0.5 * Q @ K.T, -math.inf)
+    p = torch.softmax(x, 1)
+    o = p @ V
+    E = d * 2.0 ** -24 * d ** -0.5 * (Q.abs() @ K.abs().T).max(1, keepdim=True).values + 2.0 ** -21 * 10
+    ds = p * (G @ V.T - (G * o).sum(1, keepdim=True))
+    err = p * (4 * E + E_SUM) * (G.abs() @ V.abs().T + (G.abs() * o.abs()).sum(1, keepdim=True)) + (u + E_SUM) * ds.abs()
+    return dict(dq=r["dq"], dq_bound=(d ** -0.5 * err @ K.abs() + u * r["dq"][:, 0].abs())[:, None])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F16, BF16])
+def test_gradients_of_a_short_text_do_not_depend_on_its_neighbours(ty):
+    """Few words, one of which takes nearly all: what the rounding of the output would cost shows."""
+    n, d, see = 40, 16, dict(left=2, right=0)
+    q, k, v, dout = rows(n, 1, 1, d, ty, 16)
+    q = k = (q * 1.25).to(ty)
+    ref = strict(q, k, v, dout, see)
+    for before, after in ((0, 0), (4000, 0), (4000, 1500), (77, 900)):
+        a, b = [[t[:m] for t in rows(max(m, 1), 1, 1, d, ty, 17)] for m in (before, after)]
+        parts = [torch.cat([x, y, z]).cuda() for x, y, z in zip(a, (q, k, v, dout), b)]
+        for left in (2, None):
+            off = device_offsets([before, n, after])
+            out, lse = w2v.attend(*parts[:3], off, left=left, right=0)
+            dq = w2v.attend_backward(parts[3], *parts[:3], out, lse, off, left=left, right=0)[0]
+            if left:
+                check(dq[before:before + n], ref, "dq", ty)
+            else:
+                r = strict(q, k, v, dout, dict(left=n, right=0))
+                check(dq[before:before + n], r, "dq", ty)
