@@ -129,7 +129,9 @@ __device__ inline float scaled_bias(const AttendArgs& a, uint32_t head, int32_t 
 // ---- a row at a time ---------------------------------------------------------------------------------
 // One wavefront, one query and head (or one key and key head), nothing rounded on the way and nothing touched that the
 // word is not shown.  The tiled kernels come back to these for rows whose result is not finite: there a
-// masked word's infinity or NaN, which a matrix product multiplies by zero, must not show.
+// masked word's infinity or NaN, which a matrix product multiplies by zero, must not show.  That costs a thousand times a tile's
+// share of a row.  It is paid where infinities or NaN are shown, and for words within a tile's reach of a text or
+// window that holds them; not for words that `keep` leaves out, whose rows enter the tiles as zeros.
 template <typename T> __device__ inline float dot_rows(const T* x, const T* y, uint32_t d) {
     float s = 0.f;
     for (uint32_t c = 0; c < d; ++c) s = fmaf((float)x[c], (float)y[c], s);

@@ -68,9 +68,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
     uint64_t kept = ~0ull;
     if (count) {
         next.fetch(a, kv_head, x, 0, lane);
-        next.k.store(tiles[0][0], a.width);
-        next.v.store(tiles[0][1], a.width);
         kept = __ballot(next.keep != 0);
+        next.k.store(tiles[0][0], a.width);
+        next.v.store(tiles[0][1], a.width, kept);
     }
     __syncthreads();
     for (uint32_t t = 0; t < count; ++t) {
@@ -144,9 +144,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
         }
         if (t + 1 < count) {
             if (BUFFERS == 1) __syncthreads();
-            next.k.store(tiles[(t + 1) % BUFFERS][0], a.width);
-            next.v.store(tiles[(t + 1) % BUFFERS][1], a.width);
             kept = __ballot(next.keep != 0);
+            next.k.store(tiles[(t + 1) % BUFFERS][0], a.width);
+            next.v.store(tiles[(t + 1) % BUFFERS][1], a.width, kept);
             __syncthreads();
         }
     }

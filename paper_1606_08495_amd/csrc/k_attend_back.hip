@@ -176,9 +176,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         next.fetch(a, kv_head, x, range.from, lane);
         if (walked) __syncthreads();                  // the last tiles of the pass before
         walked = true;
-        next.k.store(tiles + range.from % BUFFERS * 2 * Tl::BYTES, a.width);
-        next.v.store(tiles + range.from % BUFFERS * 2 * Tl::BYTES + Tl::BYTES, a.width);
         uint64_t kept = __ballot(next.keep != 0);
+        next.k.store(tiles + range.from % BUFFERS * 2 * Tl::BYTES, a.width, kept);
+        next.v.store(tiles + range.from % BUFFERS * 2 * Tl::BYTES + Tl::BYTES, a.width, kept);
         __syncthreads();
         for (uint32_t t = range.from; t < range.to; ++t) {
             if (t + 1 < range.to) next.fetch(a, kv_head, x, t + 1, lane);
@@ -276,9 +276,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
             if (t + 1 < range.to) {
                 if (BUFFERS == 1) __syncthreads();
                 char* const to = tiles + (t + 1) % BUFFERS * 2 * Tl::BYTES;
-                next.k.store(to, a.width);
-                next.v.store(to + Tl::BYTES, a.width);
                 kept = __ballot(next.keep != 0);
+                next.k.store(to, a.width, kept);
+                next.v.store(to + Tl::BYTES, a.width, kept);
                 __syncthreads();
             }
         }

@@ -188,14 +188,20 @@ template <typename T, int DB, int ROWS, int THREADS> struct Transit {
         for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_read<T, DB == 1>(at[n], c0, width);
         tile += ROWS * stride;
     }
-    // CLEAN: zeros past the width
-    template <bool CLEAN = false> __device__ __forceinline__ void store(char* to, uint32_t width) {
+    // CLEAN: zeros past the width.  Rows whose bit of `kept` is not set become zeros (tiles of 64 rows).
+    template <bool CLEAN = false> __device__ __forceinline__ void store(char* to, uint32_t width, uint64_t kept = ~0ull) {
         if (c0 >= (uint32_t)Tl::CHUNKS * Tl::N || threadIdx.x / LANES >= (uint32_t)ROWS) return;
         if (CLEAN || width % Tl::N)
 #pragma unroll
             for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_fit<T>(x[n], c0, width);
 #pragma unroll
         for (uint32_t n = 0; n < PER; ++n) *(typename Tl::Chunk*)(to + Tl::place(r0 + n * RS, c0 / Tl::N)) = x[n];
+        if (__builtin_expect(kept != ~0ull, 0)) {     // (over what was stored: selecting before it costs registers)
+            const uint64_t gone = ~kept >> r0;
+#pragma unroll
+            for (uint32_t n = 0; n < PER; ++n)
+                if (gone >> n * RS & 1) *(typename Tl::Chunk*)(to + Tl::place(r0 + n * RS, c0 / Tl::N)) = typename Tl::Chunk{};
+        }
     }
 };
 

@@ -226,3 +226,22 @@ def test_gradients_of_a_short_text_do_not_depend_on_its_neighbours(ty):
             else:
                 r = strict(q, k, v, dout, dict(left=n, right=0))
                 check(dq[before:before + n], r, "dq", ty)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("d", [16, 60, 100, 128])
+def test_what_dropped_words_hold_changes_no_bit(d, ty):
+    """Their rows are taken as zeros on the way in: no row is formed again for them."""
+    lengths, H = [300, 5, 200, 0, 400], 4
+    T = sum(lengths)
+    q, k, v, dout = [t.cuda() for t in rows(T, H, 2, d, ty, 18)]
+    keep = (torch.rand(T, generator=torch.Generator().manual_seed(19)) > 0.3).to(torch.uint8).cuda()
+    bias, bmap = torch.randn(H, 8, device="cuda"), w2v.relative_buckets(8, 30)
+    for see in (dict(left=None, right=0), dict(left=40, right=3, sinks=4, bias=bias, buckets=bmap)):
+        want = None
+        for bad in (0.0, 1.5, math.inf, math.nan):
+            k[keep == 0], v[keep == 0] = bad, bad
+            got = whole(q, k, v, dout, device_offsets(lengths), keep=keep, **see)
+            want = want or got
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), bad
