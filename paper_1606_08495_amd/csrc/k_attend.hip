@@ -103,6 +103,28 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
                 for (int b = 0; b < DB; ++b) o[b] *= factor;
             }
             const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
+            // What is summed here is the pieces' first, then the whole row's: a long row would make one long chain of roundings.
+            // (In 16 bits that of the weights hides the chain of o.)
+            float sum = 0.f;
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int p = 0; p < P.value; ++p)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[p][r] = __builtin_amdgcn_exp2f(fmaf(s[p][r], unit, -base));
+                        sum += s[p][r];
+                    }
+#pragma unroll
+                for (int b = 0; b < DB; ++b) {
+                    Acc part = {};
+#pragma unroll
+                    for (int g = 0; g < 2 * P.value; ++g)
+                        mma(Tl::across(vt, at_across, (p0 + g / 2) * 32, g % 2, b), acc_operand<T>(s[g / 2], g % 2), part);
+                    o[b] += part;
+                }
+                total += sum;
+                return;
+            }
 #pragma unroll
             for (int g = 0; g < 2 * P.value; ++g) {   // 16 keys
                 const int p = g / 2;
@@ -110,7 +132,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     const float y = __builtin_amdgcn_exp2f(fmaf(s[p][8 * (g % 2) + c], unit, -base));
-                    total += y;
+                    sum += y;
                     e[c] = (T)y;
                     s[p][8 * (g % 2) + c] = y;
                 }
@@ -127,6 +149,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
                     mma(v[0], rest, o[0]);
                 }
             }
+            total += sum;
         };
         const auto needs = [&](uint32_t piece) __attribute__((always_inline)) {
             const uint32_t n0 = t * KEYS + piece * 32 + own_rows;

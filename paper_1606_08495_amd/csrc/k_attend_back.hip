@@ -204,8 +204,10 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                     if (to == -__builtin_inff()) return;      // (the same in a word's two lanes)
                     total *= __builtin_amdgcn_exp2f(most - to);
                     most = to;
+                    float sum = 0.f;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) total += __builtin_amdgcn_exp2f(fmaf(s[r], unit, -most));
+                    for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(fmaf(s[r], unit, -most));
+                    total += sum;
                     return;
                 }
 #pragma unroll
@@ -214,11 +216,13 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] -= low;
                 if constexpr (pass == DELTA) {
+                    float sum = 0.f;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const float p = __builtin_amdgcn_exp2f(s[r]);
-                        formed = fmaf(p, p == 0.f ? 0.f : dp[r], formed);
+                        sum = fmaf(p, p == 0.f ? 0.f : dp[r], sum);
                     }
+                    formed += sum;
                     return;
                 }
 #pragma unroll
@@ -262,11 +266,22 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                     }
                 }
                 if constexpr (lifts<T>) lift_piece(s, dq, lift);
+                if constexpr (sizeof(T) == 4) {
+                    // a piece's sum first, then to the whole: a long row would make one long chain of roundings
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const auto ds = acc_operand<T>(s, k);
+                    for (int n = 0; n < DB; ++n) {
+                        Acc part = {};
 #pragma unroll
-                    for (int n = 0; n < DB; ++n) mma(Tl::across(kp, at_across, 0, k, n), ds, dq[n]);
+                        for (int k = 0; k < 2; ++k) mma(Tl::across(kp, at_across, 0, k, n), acc_operand<T>(s, k), part);
+                        dq[n] += part;
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const auto ds = acc_operand<T>(s, k);
+#pragma unroll
+                        for (int n = 0; n < DB; ++n) mma(Tl::across(kp, at_across, 0, k, n), ds, dq[n]);
+                    }
                 }
             };
             if constexpr (SPLIT == 2) one(0);
@@ -589,7 +604,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
             if constexpr (lifts<T>) lift_piece(dp, dk, lift);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (sizeof(T) == 4) {
-                // a piece's sum first, then to the whole: a text's queries and heads would make one long chain of roundings
+                // the same for a text's queries and heads
 #pragma unroll
                 for (int n = 0; n < DB; ++n) {
                     Acc v = {}, x = {};

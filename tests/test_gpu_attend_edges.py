@@ -245,3 +245,28 @@ def test_what_dropped_words_hold_changes_no_bit(d, ty):
             got = whole(q, k, v, dout, device_offsets(lengths), keep=keep, **see)
             want = want or got
             assert all(torch.equal(a, b) for a, b in zip(got, want)), bad
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("buckets", [0, 8])
+def test_sums_over_many_words_in_32_bits(buckets):
+    """Sums of 30000 terms: a piece of at most 64 words first, 470 such sums one after the other.  A random walk of N steps gathers
+    about 0.6 2^-24 sqrt(N / 2) of its end's size: 5e-7 for the pieces' sums and 2e-7 within one; all 30000 in a row would gather
+    3e-6."""
+    n, d = 30000, 16
+    q, k, v, dout = [t.cuda() for t in rows(n, 1, 1, d, F32, 20)]
+    see = dict(bias=torch.randn(1, buckets, device="cuda"), buckets=w2v.relative_buckets(buckets, 100)) if buckets else {}
+    got = whole(q, k, v, dout, device_offsets([n]), **see)[:3]
+    Q, K, V, G = [t[:, 0].double() for t in (q, k, v, dout)]
+    o, dq = torch.empty(n, d, dtype=torch.float64, device="cuda"), torch.empty(n, d, dtype=torch.float64, device="cuda")
+    for a in range(0, n, 2000):
+        x = Q[a:a + 2000] @ K.T.contiguous() / 4
+        if buckets:
+            dist = (torch.arange(n, device="cuda")[None] - torch.arange(a, min(n, a + 2000), device="cuda")[:, None]).clamp(-100, 100)
+            x = x + see["bias"][0].double()[see["buckets"].long()[dist + 100]]
+        p = torch.softmax(x, 1)
+        o[a:a + 2000] = p @ V
+        ds = p * (G[a:a + 2000] @ V.T.contiguous() - (G[a:a + 2000] * o[a:a + 2000]).sum(1, keepdim=True))
+        dq[a:a + 2000] = ds @ K / 4
+    for t, exact in ((got[0], o), (got[2], dq)):
+        assert float((t[:, 0].double() - exact).norm() / exact.norm()) <= 1.5e-6
