@@ -7,6 +7,8 @@
 // `keep` leaves out are read but not used.  All arithmetic is fp32.
 // Measured: 32 texts of up to 32768 words (574335 in all), 32 heads of 128 over 8, 16 bits: 588 us (4.0 TB/s; a large copy moves
 // 4.8; vector units busy half the time).  One text of 500 words, 5 heads of 60: 8 us and 4 us for the join.
+#include <type_traits>
+
 #include "attend.h"
 #include "tiles.h"
 
@@ -28,8 +30,11 @@ __device__ inline Keys step_keys(const StepArgs& a, uint32_t text) {
     return k;
 }
 
+// Wavefronts a SIMD that the registers are held to: what the plain walk needs by itself.
+template <typename T, int HEADS> constexpr int step_waves = (HEADS == 1 ? 5 : HEADS == 2 ? 4 : HEADS == 4 ? 3 : 2) + (sizeof(T) == 4);
+
 template <typename T, int L, int HEADS>
-__global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
+__global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(const StepArgs a) {
     constexpr int N = pack16<T>, GROUPS = WAVE / L;
     typedef typename Pack<T, N>::vec vec;
     extern __shared__ float dynamic[];                // bias by distance 0 .. -span for each head, times log2 e
@@ -55,16 +60,12 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
     const uint32_t c0 = part * N, start = a.width < N ? 0 : c0 < a.width - N ? c0 : a.width - N;
     float q[HEADS][N], acc[HEADS][N], m[HEADS], total[HEADS];
 #pragma unroll
-    for (int g = 0; g < HEADS; ++g) {
-        m[g] = -__builtin_inff();
-        total[g] = 0.f;
+    for (int g = 0; g < HEADS; ++g)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const uint32_t c = start + e;
             q[g][e] = g < (int)heads && c >= c0 && c < a.width ? (float)head_row<T>(a.q, text, head0 + g)[c] * a.scale2 : 0.f;
-            acc[g][e] = 0.f;
         }
-    }
     const T* const k0 = (const T*)a.k.p + (uint64_t)text * a.k.text + (uint64_t)kv_head * a.k.head;
     const T* const v0 = (const T*)a.v.p + (uint64_t)text * a.v.text + (uint64_t)kv_head * a.v.head;
 
@@ -89,46 +90,72 @@ __global__ __launch_bounds__(THREADS) void step_kernel(const StepArgs a) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) keep[u] = a.keep[(uint64_t)text * a.room + j[u]];
     };
-    for (uint32_t n0 = from + wave * STEP; n0 < to; n0 += WAVES * STEP) {
-        fetch(n0);
-        bool in[AHEAD];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            in[u] = n0 + u * GROUPS + group < to && keep[u] && !(a.skip_self && j[u] == keys.last);
-        if (masked || n0 + STEP > to)                 // what is not shown must not show, whatever it holds
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) vx[u] = in[u] ? vx[u] : vec{};
+    // CAREFUL: what has no part in a sum is left out of it, not multiplied by zero -- a neighbour's columns, and values of weight
+    // zero, which may be infinite.  Taken where the plain walk, whose finite sums are the same, meets a value that is not finite.
+    const auto walk = [&](auto CAREFUL) __attribute__((always_inline)) {
 #pragma unroll
         for (int g = 0; g < HEADS; ++g) {
-            float x[AHEAD], most = m[g];
+            m[g] = -__builtin_inff();
+            total[g] = 0.f;
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                float s = 0.f;
+            for (int e = 0; e < N; ++e) acc[g][e] = 0.f;
+        }
+        for (uint32_t n0 = from + wave * STEP; n0 < to; n0 += WAVES * STEP) {
+            fetch(n0);
+            if constexpr (CAREFUL.value)
 #pragma unroll
-                for (int e = 0; e < N; ++e) s = fmaf((float)kx[u][e], q[g][e], s);
-                s = lanes_sum<L>(s);
-                if (a.bias && g < (int)heads) {
-                    const uint32_t back = keys.last - j[u] < a.span ? keys.last - j[u] : a.span;
-                    s += dynamic[(in[u] ? back : 0) * heads + g];
+                for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) if (!(start + e >= c0 && start + e < a.width)) kx[u][e] = (T)0.f;
+            bool in[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                in[u] = n0 + u * GROUPS + group < to && keep[u] && !(a.skip_self && j[u] == keys.last);
+            if (masked || n0 + STEP > to)                 // what is not shown must not show, whatever it holds
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) vx[u] = in[u] ? vx[u] : vec{};
+#pragma unroll
+            for (int g = 0; g < HEADS; ++g) {
+                float x[AHEAD], most = m[g];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) s = fmaf((float)kx[u][e], q[g][e], s);
+                    s = lanes_sum<L>(s);
+                    if (a.bias && g < (int)heads) {
+                        const uint32_t back = keys.last - j[u] < a.span ? keys.last - j[u] : a.span;
+                        s += dynamic[(in[u] ? back : 0) * heads + g];
+                    }
+                    x[u] = in[u] ? s : -__builtin_inff();
+                    most = fmaxf(most, x[u]);
                 }
-                x[u] = in[u] ? s : -__builtin_inff();
-                most = fmaxf(most, x[u]);
-            }
-            const float base = most == -__builtin_inff() ? 0.f : most;
-            const float factor = __builtin_amdgcn_exp2f(m[g] - base);
-            m[g] = most;
-            total[g] *= factor;
+                const float base = most == -__builtin_inff() ? 0.f : most;
+                const float factor = __builtin_amdgcn_exp2f(m[g] - base);
+                m[g] = most;
+                total[g] *= factor;
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc[g][e] *= factor;
+                for (int e = 0; e < N; ++e) acc[g][e] *= factor;
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const float p = __builtin_amdgcn_exp2f(x[u] - base);
-                total[g] += p;
+                for (int u = 0; u < AHEAD; ++u) {
+                    const float p = __builtin_amdgcn_exp2f(x[u] - base);
+                    total[g] += p;
 #pragma unroll
-                for (int e = 0; e < N; ++e) acc[g][e] = fmaf(p, (float)vx[u][e], acc[g][e]);
+                    for (int e = 0; e < N; ++e)
+                        acc[g][e] = CAREFUL.value && p == 0.f ? acc[g][e] : fmaf(p, (float)vx[u][e], acc[g][e]);
+                }
             }
         }
+    };
+    walk(std::false_type{});
+    float worst = 0.f;                                // not a number, if any sum is not finite
+#pragma unroll
+    for (int g = 0; g < HEADS; ++g) {
+        worst = fmaf(total[g], 0.f, worst);
+#pragma unroll
+        for (int e = 0; e < N; ++e) worst = fmaf(acc[g][e], 0.f, worst);
     }
+    if (__any(worst != 0.f)) walk(std::true_type{});
     // the groups of a wavefront, then the wavefronts
 #pragma unroll
     for (int g = 0; g < HEADS; ++g) {
