@@ -170,9 +170,10 @@ extern "C" int w2v_relative_buckets(uint32_t n_buckets, uint32_t span, uint32_t*
     for (uint32_t r = 0; r <= span; ++r) {
         uint32_t b = r < half - 1 ? r : half - 1;
         if (r >= near && far) {
-            // a distance that meets a border in exact arithmetic is past it: the quotients of the logarithms of two
-            // such numbers below 2^10 are farther than 1e-9 from the border or on it
-            while (t + 1 < far && far * std::log((double)r / near) >= (t + 1) * std::log((double)span / near) - 1e-9) ++t;
+            // a distance that meets a border in exact arithmetic is past it.  Of all maps within the limits, the one whose
+            // distance comes nearest to a border without meeting it is 42 buckets over 1006 (435: 5.03e-11 past it); the logarithms'
+            // rounding is below 1e-12
+            while (t + 1 < far && far * std::log((double)r / near) >= (t + 1) * std::log((double)span / near) - 1e-11) ++t;
             b = near + t;
         }
         map[span - r] = b;
