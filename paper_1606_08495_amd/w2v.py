@@ -500,10 +500,19 @@ class AttendSpec(ctypes.Structure):
                 ("n_buckets", c_u32), ("span", c_u32), ("bias_dev", c_vp), ("bucket_dev", c_vp)]
 
 
+def _number(x, name):
+    """A count as the library takes it: what lies past 32 bits is past every limit too."""
+    x = int(x)
+    if x < 0:
+        raise ValueError("%s = %d is negative" % (name, x))
+    return min(x, UNBOUNDED)
+
+
 def relative_buckets(n_buckets, span, device="cuda"):
     """The bucket of every distance -span..span (w2v_relative_buckets), int32 [2 span + 1] on the device."""
-    m = np.empty(2 * max(int(span), 0) + 1, np.uint32)
-    _check(lib().w2v_relative_buckets(int(n_buckets), int(span), c_vp(m.ctypes.data)))
+    n_buckets, span = _number(n_buckets, "n_buckets"), _number(span, "span")
+    m = np.empty(2 * min(span, SPAN_MAX) + 1, np.uint32)      # (a longer span is refused)
+    _check(lib().w2v_relative_buckets(n_buckets, span, c_vp(m.ctypes.data)))
     return as_index_tensor(m, device)
 
 
@@ -528,8 +537,8 @@ def _spec(q, kv_heads, left, right, sinks, skip_self, scale, bias, buckets):
     if q.dtype not in TYPES:
         raise TypeError("q must be float32, float16 or bfloat16")
     heads, width = q.shape[1], q.shape[2]
-    s = AttendSpec(TYPES[q.dtype], heads, kv_heads, width, UNBOUNDED if left is None else int(left),
-                   UNBOUNDED if right is None else int(right), int(sinks), 1 if skip_self else 0,
+    s = AttendSpec(TYPES[q.dtype], heads, kv_heads, width, UNBOUNDED if left is None else _number(left, "left"),
+                   UNBOUNDED if right is None else _number(right, "right"), _number(sinks, "sinks"), 1 if skip_self else 0,
                    width ** -0.5 if scale is None else float(scale))
     if bias is not None:
         if bias.dim() != 2 or bias.shape[0] != heads or bias.device != q.device:
