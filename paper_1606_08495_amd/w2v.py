@@ -129,6 +129,15 @@ def _dev(t, dtype, name):
     return c_vp(t.data_ptr())
 
 
+def _room(t, device):
+    """(pointer, bytes) of a workspace that the caller keeps."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()):
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    if t.device != device:
+        raise ValueError("workspace must be on %s" % device)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 # uint32 index arrays are carried in int32 tensors (torch has no arithmetic on uint32; the bit
 # patterns are what the library reads).
 IDX = torch.int32
@@ -396,14 +405,14 @@ def topk_cosine(queries, cands, K, tau=-2.0, round_candidates=32768, workspace=N
     if workspace is None:
         need = int(lib().w2v_topk_cosine_workspace(Q, N, int(round_candidates)))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=queries.device)
+    at, size = _room(workspace, queries.device)
     idx = torch.empty((Q, K), dtype=IDX, device=queries.device)
     score = torch.empty((Q, K), dtype=torch.float32, device=queries.device)
     count = torch.empty(Q, dtype=IDX, device=queries.device)
     _check(lib().w2v_topk_cosine(_dev(queries, torch.float32, "queries"), Q,
                                  _dev(cands, torch.float32, "cands"), N, d, int(K), float(tau),
                                  _dev(idx, IDX, "out_idx"), _dev(score, torch.float32, "out_score"),
-                                 _dev(count, IDX, "out_count"), c_vp(workspace.data_ptr()),
-                                 workspace.numel(), _stream(stream)))
+                                 _dev(count, IDX, "out_count"), c_vp(at), size, _stream(stream)))
     return idx, score, count
 
 
@@ -474,11 +483,12 @@ def layer_norm_backward(dy, x, gain, mean, rstd, out=None, workspace=None, strea
         if workspace is None:
             workspace = x.new_empty(int(lib().w2v_layer_norm_backward_workspace(TYPES[x.dtype], m, d)),
                                     dtype=torch.uint8)
+        at, size = _room(workspace, x.device)
         op, os_ = _rows(dx, x, "out")
         _check(lib().w2v_layer_norm_backward(TYPES[x.dtype], gp, gs, xp, xs, m, d, _vec(gain, d, x.device, "gain"),
                                              _vec(mean, m, x.device, "mean"), _vec(rstd, m, x.device, "rstd"), op,
                                              os_, columns.data_ptr(), columns.data_ptr() + 4 * d,
-                                             workspace.data_ptr(), workspace.numel(), st))
+                                             at, size, st))
     dgain, doffset = columns.unbind(0)
     return dx, dgain, doffset
 
@@ -599,13 +609,14 @@ def attend_backward(dout, q, k, v, out, lse, sent_off, left=None, right=None, si
         if workspace is None:
             need = int(lib().w2v_attend_backward_workspace(ctypes.byref(spec), T))
             workspace = q.new_empty(max(need, 256), dtype=torch.uint8)
+        at, size = _room(workspace, q.device)
         off, n, t, kp = _texts(sent_off, keep, q)
         r = ctypes.byref
         _check(lib().w2v_attend_backward(
             r(spec), r(_heads(dout, q, T, H, "dout")), r(_heads(q, q, T, H, "q")), r(_heads(k, q, T, G, "k")),
             r(_heads(v, q, T, G, "v")), r(_heads(out, q, T, H, "out")), _dev(lse, torch.float32, "lse"), off, n, t, kp,
             r(_dense(dq, H, d)), r(_dense(dk, G, d)), r(_dense(dv, G, d)),
-            _dev(dbias, torch.float32, "dbias"), workspace.data_ptr(), workspace.numel(), st))
+            _dev(dbias, torch.float32, "dbias"), at, size, st))
     return dq, dk, dv, dbias
 
 
@@ -639,9 +650,9 @@ def attend_step(q, k, v, n, left=None, sinks=0, skip_self=False, scale=None, kee
         if workspace is None:
             need = int(lib().w2v_attend_step_workspace(r(spec), B, room))
             workspace = q.new_empty(max(need, 256), dtype=torch.uint8)
+        at, size = _room(workspace, q.device)
         shape = torch.Size((B, room, G, d))
         _check(lib().w2v_attend_step(r(spec), r(_heads(q, q, B, H, "q")), r(_cache(k, q, shape, "k")),
                                      r(_cache(v, q, shape, "v")), _dev(n, IDX, "n"), B, room, _dev(keep, torch.uint8, "keep"),
-                                     r(_heads(out, q, B, H, "out")), workspace.data_ptr(), workspace.numel(),
-                                     st))
+                                     r(_heads(out, q, B, H, "out")), at, size, st))
     return out
