@@ -3,7 +3,7 @@
 #include "../../include/w2v_shard.h"
 
 #include <cmath>
-#include <cstring>
+#include <cstdlib>
 
 #include "common.h"
 #include "context.h"
@@ -139,6 +139,28 @@ int check_heads(const w2v_heads* x, const w2v_attend_spec* s, uint32_t heads, ui
     return W2V_OK;
 }
 
+// Whether an output's heads and another array's touch.  Arrays apart from each other are told by their ends; others, as q, k and v of a
+// word side by side, have to have one stride from word to word, where a head of one meets a head of the other or does not.
+int check_apart(const w2v_heads* out, uint32_t out_heads, const char* out_name, const w2v_heads* in, uint32_t in_heads,
+                const char* in_name, const w2v_attend_spec* s, uint32_t rows) {
+    const uint64_t size = elem_bytes(s->type), a = (uint64_t)(uintptr_t)out->p / size, b = (uint64_t)(uintptr_t)in->p / size;
+    const auto reach = [&](const w2v_heads* x, uint32_t heads) {
+        return (uint64_t)(rows - 1) * x->token_stride + (uint64_t)(heads - 1) * x->head_stride + s->width;
+    };
+    if (a + reach(out, out_heads) <= b || b + reach(in, in_heads) <= a) return W2V_OK;
+    const int64_t step = rows > 1 ? (int64_t)out->token_stride : 0, width = s->width;
+    bool meet = rows > 1 && out->token_stride != in->token_stride;
+    for (uint32_t h = 0; h < out_heads && !meet; ++h)
+        for (uint32_t g = 0; g < in_heads && !meet; ++g) {
+            // words `from` and from + 1 of the input apart are the nearest to the output's head on either side
+            const int64_t far = (int64_t)(a + h * out->head_stride) - (int64_t)(b + g * in->head_stride);
+            const int64_t from = step ? far / step : 0;
+            for (int64_t w = from - 1; w <= from + 1; ++w)
+                meet |= std::llabs(far - w * step) < width && std::llabs(w) < (int64_t)rows;
+        }
+    return meet ? fail(W2V_ERR_ARG, "%s overlaps %s", out_name, in_name) : W2V_OK;
+}
+
 Heads heads_of(const w2v_heads* x) { return Heads{x->p, x->token_stride, x->head_stride}; }
 HeadsOut heads_out(const w2v_heads* x) { return HeadsOut{x->p, x->token_stride, x->head_stride}; }
 
@@ -192,6 +214,9 @@ extern "C" int w2v_attend(const w2v_attend_spec* spec, const w2v_heads* q, const
     if (int rc = check_heads(k, spec, spec->kv_heads, n_tokens, false, "k")) return rc;
     if (int rc = check_heads(v, spec, spec->kv_heads, n_tokens, false, "v")) return rc;
     if (int rc = check_heads(out, spec, spec->heads, n_tokens, true, "out")) return rc;
+    if (int rc = check_apart(out, spec->heads, "out", q, spec->heads, "q", spec, n_tokens)) return rc;
+    if (int rc = check_apart(out, spec->heads, "out", k, spec->kv_heads, "k", spec, n_tokens)) return rc;
+    if (int rc = check_apart(out, spec->heads, "out", v, spec->kv_heads, "v", spec, n_tokens)) return rc;
     launch_attend(attend_args(spec, q, k, v, sent_off, n_sent, n_tokens, keep, out, lse), (uint32_t)spec->type,
                   (hipStream_t)stream);
     return launched();
@@ -252,6 +277,13 @@ extern "C" int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads*
         if (!aligned(workspace, 256)) return fail(W2V_ERR_ARG, "workspace must be 256-byte aligned");
         if (workspace_bytes < space.bytes)
             return fail(W2V_ERR_ARG, "workspace of %zu bytes is too small: %zu are needed", workspace_bytes, space.bytes);
+        struct { const w2v_heads* x; uint32_t heads; const char* name; } arrays[] = {
+            {dq, spec->heads, "dq"}, {dk, spec->kv_heads, "dk"}, {dv, spec->kv_heads, "dv"}, {dout, spec->heads, "dout"},
+            {q, spec->heads, "q"}, {k, spec->kv_heads, "k"}, {v, spec->kv_heads, "v"}, {out, spec->heads, "out"}};
+        for (int n = 0; n < 3; ++n)
+            for (int m = n + 1; m < 8; ++m)
+                if (int rc = check_apart(arrays[n].x, arrays[n].heads, arrays[n].name, arrays[m].x, arrays[m].heads,
+                                         arrays[m].name, spec, n_tokens)) return rc;
         b.a = attend_args(spec, q, k, v, sent_off, n_sent, n_tokens, keep, out, const_cast<float*>(lse));
         b.dout = heads_of(dout);
         b.dq = heads_out(dq); b.dk = heads_out(dk); b.dv = heads_out(dv);

@@ -35,3 +35,35 @@ def test_a_workspace_of_another_type_counts_its_bytes():
     for call in calls(torch.empty(4, dtype=torch.float64, device="cuda")):
         with pytest.raises(w2v.W2VError):
             call()
+
+
+@pytest.mark.gpu
+def test_outputs_beside_their_inputs_in_one_buffer():
+    """q, k, v and the result of a word side by side do not touch; a result on its inputs is refused."""
+    T, H, d = 200, 3, 20
+    off = torch.tensor([0, T], dtype=torch.int64, device="cuda")
+    packed = torch.randn(T, 4, H, d, device="cuda")
+    q, k, v, out = packed.unbind(1)
+    want = w2v.attend(q.contiguous(), k.contiguous(), v.contiguous(), off, right=0)[0]
+    w2v.attend(q, k, v, off, right=0, out=out)
+    assert torch.equal(out, want)
+    before = packed.clone()
+    flat = packed.view(-1)
+    shifted = flat[d // 2:d // 2 + (T - 1) * 4 * H * d + H * d].as_strided((T, H, d), (4 * H * d, d, 1))      # half a head on
+    heads_first = flat[:T * H * d].view(H, T, d).transpose(0, 1)
+    for bad in (q, k, v, shifted, heads_first, packed.view(T, 4 * H, d)[:, 1:1 + H]):
+        with pytest.raises(w2v.W2VError):
+            w2v.attend(q, k, v, off, right=0, out=bad)
+    torch.cuda.synchronize()
+    assert torch.equal(packed, before)
+    shared = torch.randn(T, 8, d, device="cuda")              # six query heads, one key head, one value head; results elsewhere
+    w2v.attend(shared[:, :6], shared[:, 6:7], shared[:, 7:], off, out=torch.empty(T, 6, d, device="cuda"))
+    with pytest.raises(w2v.W2VError):
+        w2v.attend(shared[:, :6], shared[:, 6:7], shared[:, 7:], off, out=shared[:, 2:])
+    one = torch.randn(1, 4, H, d, device="cuda")              # a single word: strides from word to word mean nothing
+    w2v.attend(*one.unbind(1)[:3], torch.tensor([0, 1], device="cuda"), out=one[:, 3])
+    assert torch.equal(one[:, 3], one[:, 2])
+    n = torch.tensor([600, 3], dtype=torch.int32, device="cuda")
+    cache, q = torch.randn(2, 600, 2, 16, device="cuda"), torch.randn(2, 2, 16, device="cuda")
+    want = w2v.attend_step(q, cache, cache, n)
+    assert torch.equal(w2v.attend_step(q, cache, cache, n, out=q), want)      # a step's result may take the place of its q
