@@ -313,8 +313,8 @@ template <typename T, typename A> void norm_any(const A& a, uint32_t most, hipSt
         case 64: return norm_nv<T, 64>(a, nv, blocks, st);
         case 128: return norm_nv<T, 128>(a, nv, blocks, st);
         case 256: return norm_nv<T, 256>(a, nv, blocks, st);
-        default: return norm_nv<T, 512>(a, nv, blocks, st);
     }
+    if constexpr (sizeof(T) == 4) norm_nv<T, 512>(a, nv, blocks, st);      // (16 bits: 16384 elements are 2048 vectors, 256 lanes)
 }
 
 }  // namespace
