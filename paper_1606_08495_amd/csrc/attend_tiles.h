@@ -113,7 +113,7 @@ __device__ __forceinline__ Tiles tiles_of(const Tiles (&groups)[GROUPS]) {
 // Bias by distance, times log2 e, with the outermost values repeated on both sides so that every distance within a
 // 32 x 32 piece that is not wholly past the span is in the table.
 constexpr int BIAS_SIDE = 64;
-__host__ __device__ inline uint32_t bias_table(uint32_t span) { return (2 * (span + BIAS_SIDE) + 1 + 3) / 4 * 4; }
+__host__ __device__ constexpr uint32_t bias_table(uint32_t span) { return (2 * (span + BIAS_SIDE) + 1 + 3) / 4 * 4; }
 __device__ __forceinline__ void fill_bias(const AttendArgs& a, uint32_t head, float* table) {
     const int32_t reach = (int32_t)a.span + BIAS_SIDE;
     for (int32_t at = threadIdx.x; at <= 2 * reach; at += (int32_t)blockDim.x) table[at] = scaled_bias(a, head, at - reach);

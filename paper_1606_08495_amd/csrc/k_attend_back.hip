@@ -103,15 +103,26 @@ constexpr uint32_t EXACT_WORDS = 128;
 // (Atomic adds in LDS take a cycle a lane: sixteen times that.)
 constexpr int SKEW = 64, SKEW_FLOATS = 32 * SKEW;
 
+// LDS of a block beside what depends on the span: tiles, in whose place the halves are joined, and what its wavefronts exchange.
+template <typename T, int DB, bool BIAS, int SPLIT> struct QueryRoom {
+    static constexpr int PAIR = 2 * Tile<T, DB, KEYS>::BYTES, BUFFERS = 2 * PAIR <= (BIAS ? 40 : 72) * 1024 ? 2 : 1;
+    static constexpr int JOINED = SPLIT == 2 ? GROUPS * DB * 16 * WAVE * 4 : 0;
+    __attribute__((aligned(16))) char tiles[BUFFERS * PAIR > JOINED ? BUFFERS * PAIR : JOINED];
+    typedef float OfWords[SPLIT][SPLIT == 2 ? GROUPS : 1][SPLIT == 2 ? WAVE_WORDS : 1];      // (nothing to exchange in one half)
+    OfWords deltas, largest;
+    Tiles far_keys[GROUPS], delta_keys[GROUPS];
+};
+
 template <typename T, int DB, bool BIAS, int SPLIT>
 __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void query_kernel(const BackwardArgs b) {
     const AttendArgs& a = b.a;
     typedef Tile<T, DB, KEYS> Tl;
-    constexpr int BUFFERS = 2 * 2 * Tl::BYTES <= (BIAS ? 40 : 72) * 1024 ? 2 : 1;
-    constexpr int ROOM = SPLIT == 2 ? GROUPS * DB * 16 * WAVE * 4 : 0;
-    __shared__ __align__(16) char tiles[BUFFERS * 2 * Tl::BYTES > ROOM ? BUFFERS * 2 * Tl::BYTES : ROOM];
-    __shared__ float deltas[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS], largest[SPLIT == 2 ? 2 : 1][GROUPS][WAVE_WORDS];
-    __shared__ Tiles far_keys[GROUPS], delta_keys[GROUPS];
+    typedef QueryRoom<T, DB, BIAS, SPLIT> Room;
+    constexpr int BUFFERS = Room::BUFFERS;
+    __shared__ Room room;
+    auto& tiles = room.tiles;
+    auto &deltas = room.deltas, &largest = room.largest;
+    auto &far_keys = room.far_keys, &delta_keys = room.delta_keys;
     extern __shared__ float dynamic[];
     const int32_t span = (int32_t)a.span, reach = span + BIAS_SIDE;
     const Place place;
@@ -349,7 +360,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
 #pragma unroll
         for (int n = 0; n < DB; ++n) dq[n] *= 1.f / lift;
     bool mine = true;
-    if constexpr (SPLIT == 2) mine = join_halves(( float*)tiles, dq, wave, half, lane);
+    if constexpr (SPLIT == 2) mine = join_halves((float*)tiles, dq, wave, half, lane);
     if (some && mine) {
         const bool redo = not_finite(dq);
         if (real && !redo) store_column<T>(head_row<T>(b.dq, w.i, head), a.width, dq, a.scale, h);
@@ -749,17 +760,18 @@ __global__ __launch_bounds__(END_THREADS) void buckets_kernel(const BackwardArgs
     }
 }
 
-// LDS of a block of the queries' kernel beside its tiles: the bias' table and, where its gradient is wanted, room for it.
+// LDS of a block of the queries' kernel that depends on the span: the bias' table and, where its gradient is wanted, room for it.
 template <bool BIAS, int SPLIT> size_t query_room(const BackwardArgs& b) {
     const uint32_t table = BIAS ? bias_table(b.a.span) : 0;
     return (table + (BIAS && b.dbias ? SPLIT * GROUPS * (SKEW_FLOATS + table) : 0)) * sizeof(float);
 }
 template <typename T, int DB, bool BIAS> bool query_split(const BackwardArgs& b, uint32_t blocks) {
-    constexpr size_t tiles = 4 * Tile<T, DB, KEYS>::BYTES, joined = GROUPS * DB * 16 * WAVE * 4;      // at most
-    return blocks < SPLIT_BELOW && query_room<BIAS, 2>(b) + (tiles > joined ? tiles : joined) + 2 * BLOCK_WORDS * 4 <= LDS_BYTES;
+    return blocks < SPLIT_BELOW && query_room<BIAS, 2>(b) + sizeof(QueryRoom<T, DB, BIAS, 2>) <= LDS_BYTES;
 }
 template <typename T, int DB, bool BIAS> void backward_run(const BackwardArgs& b, hipStream_t st) {
     const AttendArgs& a = b.a;
+    static_assert(sizeof(QueryRoom<T, DB, BIAS, 1>) + (BIAS ? (5 * bias_table(SPAN_MAX) + 4 * SKEW_FLOATS) * sizeof(float) : 0) <= LDS_BYTES,
+                  "blocks of one half have room at every span");
     const uint32_t words = attend_bias_parts(a.T), table = BIAS ? bias_table(a.span) * sizeof(float) : 0;
     uint32_t blocks = words * a.heads;
     bool split = splits<T, DB> && query_split<T, DB, BIAS>(b, blocks);

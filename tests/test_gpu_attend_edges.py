@@ -270,3 +270,21 @@ def test_sums_over_many_words_in_32_bits(buckets):
         dq[a:a + 2000] = ds @ K / 4
     for t, exact in ((got[0], o), (got[2], dq)):
         assert float((t[:, 0].double() - exact).norm() / exact.norm()) <= 1.5e-6
+
+
+# spans on both sides of the one where a block of two halves no longer has room for its sums by distance, for each width and type
+ROOM = [(BF16, 20, 971), (F16, 32, 971), (BF16, 60, 742), (F16, 64, 742), (BF16, 96, 589), (F16, 100, 359), (BF16, 128, 359),
+        (F32, 32, 742), (F32, 64, 781)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty,d,span", ROOM)
+def test_spans_around_the_room_of_a_block(ty, d, span):
+    lengths = [70, 9]
+    q, k, v, dout = rows(sum(lengths), 2, 1, d, ty, 21)
+    for s in list(range(span - 4, span + 5)) + list(range(span + 5, min(span + 40, 1023), 5)) + [1023]:
+        bias, bmap = torch.randn(2, 32, generator=torch.Generator().manual_seed(s)), w2v.relative_buckets(32, s, device="cpu")
+        ref = attend_reference(q, k, v, offsets_of(lengths), bias=bias, buckets=bmap, dout=dout)
+        print("span", ty, d, s, flush=True)
+        got = whole(q.cuda(), k.cuda(), v.cuda(), dout.cuda(), device_offsets(lengths), bias=bias.cuda(), buckets=bmap.cuda())
+        compare(got, ref, ty)
