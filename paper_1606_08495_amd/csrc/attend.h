@@ -133,8 +133,16 @@ __device__ inline float scaled_bias(const AttendArgs& a, uint32_t head, int32_t 
 // share of a row.  It is paid where infinities or NaN are shown, and for words within a tile's reach of a text or
 // window that holds them; not for words that `keep` leaves out, whose rows enter the tiles as zeros.
 template <typename T> __device__ inline float dot_rows(const T* x, const T* y, uint32_t d) {
+    constexpr uint32_t N = pack16<T>;
+    typedef typename Pack<T, N>::mem mem;
     float s = 0.f;
-    for (uint32_t c = 0; c < d; ++c) s = fmaf((float)x[c], (float)y[c], s);
+    uint32_t c = 0;
+    for (; c + N <= d; c += N) {
+        const typename Pack<T, N>::vec a = *(const mem*)(x + c), b = *(const mem*)(y + c);
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) s = fmaf((float)a[e], (float)b[e], s);
+    }
+    for (; c < d; ++c) s = fmaf((float)x[c], (float)y[c], s);
     return s;
 }
 
@@ -172,7 +180,10 @@ __device__ void attend_row(const AttendArgs& a, uint32_t head, uint32_t i, const
         m = fmaxf(m, x);
     }
     m = wave_max(m);
-    if (__any(nan)) m = __builtin_nanf("");
+    if (__any(nan) || m == __builtin_inff()) {        // every weight is not a number, and so is every column
+        o[0] = o[1] = lse = __builtin_nanf("");
+        return;
+    }
     const float base = m == -__builtin_inff() ? 0.f : m;
     float total = 0.f;
     o[0] = o[1] = 0.f;
@@ -220,7 +231,8 @@ __device__ void query_row(const BackwardArgs& b, uint32_t head, uint32_t i, cons
                           float (&dq)[2]) {
     const AttendArgs& a = b.a;
     const uint32_t sunk = s.sunk - s.first, n = sunk + s.hi - s.lo;
-    dq[0] = dq[1] = 0.f;
+    dq[0] = dq[1] = r.high != r.high ? __builtin_nanf("") : 0.f;
+    if (r.high != r.high) return;                     // its weights are not numbers, and so is every column
     for (uint32_t at0 = 0; at0 < n; at0 += WAVE) {
         const uint32_t at = at0 + lane;
         const uint32_t j = at < sunk ? s.first + at : s.lo + at - sunk;
@@ -250,6 +262,10 @@ __device__ void key_row(const BackwardArgs& b, uint32_t kv_head, uint32_t j, uin
             const bool in = i < hi && row_keeps(a, i, j);
             float2 g = make_float2(0.f, 0.f);
             const size_t at = (size_t)head * a.T + i;
+            if (__any(in && b.high[at] != b.high[at])) {      // one such query is enough
+                dk[0] = dk[1] = dv[0] = dv[1] = __builtin_nanf("");
+                return;
+            }
             if (in) g = row_gradient<T>(b, head, i, j, RowSum{b.high[at], b.low[at], b.delta[at]});
             for (uint64_t left = __ballot(in && g.x != 0.f); left; left &= left - 1) {
                 const int l = __builtin_ctzll(left);

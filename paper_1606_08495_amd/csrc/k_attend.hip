@@ -1,6 +1,6 @@
 // Attention over texts, forward.
 //
-// Four products and two exponentials' worth of work per pair of words and head: for a long window the matrix cores and the
+// Two products (four operations a column) and an exponential per pair of words and head: for a long window the matrix cores and the
 // vector units bound it, for short texts its way through memory does.  A block holds 128 consecutive words of
 // the whole token stream, whichever texts they belong to -- short texts share a block instead of filling one
 // each -- and walks over the words that any of them is shown: the text's first words that stay visible, then the span of
@@ -15,9 +15,9 @@
 // what the rounding left in a second product: the gradient's dout . out is then a sum of few terms, which
 // may cancel down to the weights' rounding, and the matrix cores wait for the exponentials there anyway.
 //
-// Measured: 32768 words, 16 heads of 128 over 4, 16 bits, window of 1024: 476 us (571 TFLOP/s of the pairs shown; products
+// Measured: 32768 words, 16 heads of 128 over 4, 16 bits, window of 1024: 473 us (574 TFLOP/s of the pairs shown; products
 // and exponentials take turns in the two wavefronts of a SIMD).  131333 words in texts of 10 to 40, 5 heads of 60, 32 bits, window
-// of 10 on either side: 360 us (633 MB; a block's chain of dependent accesses).
+// of 10 on either side: 368 us (633 MB; a block's chain of dependent accesses).
 #include "attend_tiles.h"
 
 namespace w2v {
@@ -231,7 +231,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void at
             a.lse[(size_t)head * a.T + w.i] = total == 0.f ? -__builtin_inff() : (m - LIFT<T> + __builtin_log2f(total)) * LN2;
     }
     // what a word is not shown must not show: rows that are not finite are formed from their words alone
-    for (uint64_t rows = __ballot(redo && real && h == 0); rows; rows &= rows - 1) {
+    uint64_t rows = __ballot(redo && real && h == 0);
+    if (rare(rows)) for (; rows; rows &= rows - 1) {
         const int l = __builtin_ctzll(rows);
         Shown s;
         s.lo = __shfl(w.s.lo, l, 64); s.hi = __shfl(w.s.hi, l, 64);

@@ -2,8 +2,8 @@
 //
 //   dS = p (dP - delta),  dP = dout v^T,  delta = rowsum(dout out)
 //   dq = scale dS k,  dk = scale dS^T q,  dv = p^T dout,  dbias[b] = sum of dS over the pairs of bucket b
-// Weights are formed anew from q, k and the rows' logarithms.  No sum is shared between blocks, so no atomics and the
-// same bits every time: one kernel holds 128 words as queries and walks over their keys (dq, and the bias' sums; three
+// Weights are formed anew from q, k and the rows' logarithms, or what these are made of where they are large (attend.h).
+// No sum is shared between blocks, so no atomics and the same bits every time: one kernel holds 128 words as queries and walks over their keys (dq, and the bias' sums; three
 // products a pair), another holds 128 words as keys and walks over the queries they are shown to (dk, dv; four products a
 // pair).  That is seven products instead of the five of a kernel that adds dq up in memory.  In both a
 // wavefront's own 32 words are the lanes, their rows feed the B operands from registers, and p and dS feed the last
@@ -13,9 +13,10 @@
 // border behind its block; those behind go in pieces to blocks of their own (late), whose sums are joined in
 // order at the end.
 //
-// Measured, forward and backward: 9139 words in whole texts, 6 heads of 100, 16 bits 559 us; 17676 words, 8 heads of 64 over 2, window of
-// 512, bias and its gradient, 16 bits 466 us (of that the queries' kernel 224, the keys' 150); 65135 words in texts of 10 to 40, 5 heads of
-// 60, 32 bits, bias 861 us.  Vector work and latency bound them: the matrix cores are busy a quarter of the time.
+// Measured, forward and backward: 9139 words in whole texts, 6 heads of 100, fp16 601 us (in a profile: forward 172, queries' kernel
+// 216, keys' 249); 17676 words, 8 heads of 64 over 2, window of 512, bias and its gradient, bf16 469 us; 65135 words in texts of
+// 10 to 40, 5 heads of 60, 32 bits, bias 882 us.  Vector work and latency bound them.
+// In 16 bits the queries' kernel of heads wider than 96 keeps 48 to 108 bytes a lane in scratch, the keys' up to 60.
 #include "attend_tiles.h"
 
 namespace w2v {
@@ -60,7 +61,7 @@ template <int N> __device__ __forceinline__ void lift_piece(Acc& ds, Acc (&sum)[
 #pragma unroll
     for (int r = 1; r < 16; ++r) most = fmaxf(most, fabsf(ds[r]));
     most = halves_max(most);
-    if (__any(most * lift >= LIFTED_MOST)) {
+    if (rare(__any(most * lift >= LIFTED_MOST))) {
         const float to = most * lift >= LIFTED_MOST ? __builtin_amdgcn_ldexpf(1.f, 10 - __builtin_amdgcn_frexp_expf(most)) : lift;
         const float factor = to / lift;
 #pragma unroll
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
     constexpr int LOGARITHMS = 0, DELTA = 1, GRADIENTS = 2;
     bool walked = false;
     float formed = 0.f, most = -__builtin_inff(), total = 0.f, before = 0.f, after = 0.f;
-    bool lowered = false;                             // whether any of the wavefront's words has a low part
+    float share = 1.f;                                // 2^-low
     float lift = lifts<T> ? FIRST_LIFT : 1.f;
     Acc dq[DB];
 #pragma unroll
@@ -221,16 +222,11 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                     total += sum;
                     return;
                 }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], unit, -high);
-                if (lowered)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] -= low;
                 if constexpr (pass == DELTA) {
                     float sum = 0.f;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const float p = __builtin_amdgcn_exp2f(s[r]);
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -high));
                         sum = fmaf(p, p == 0.f ? 0.f : dp[r], sum);
                     }
                     formed += sum;
@@ -238,8 +234,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(s[r]);
-                    s[r] = p * (dp[r] - delta);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[r], unit, -high));      // 2^low times the weight
+                    s[r] = p * fmaf(dp[r], share, -delta);
                     if (BIAS && p == 0.f) s[r] = 0.f;     // the sums by distance are not formed anew
                 }
                 if constexpr (BIAS) {
@@ -317,8 +313,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         }
         __syncthreads();
         const Tiles range = tiles_of(far_keys);
-        walk(std::integral_constant<int, LOGARITHMS>{}, range);
-        if (range.to) {
+        if (rare(range.to)) {
+            walk(std::integral_constant<int, LOGARITHMS>{}, range);
             total = halves_sum(total);
             if constexpr (SPLIT == 2) {
                 if (h == 0) { deltas[half][wave][lane] = total; largest[half][wave][lane] = most; }
@@ -332,7 +328,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
                 high = most;
                 low = __builtin_log2f(total);
             }
-            lowered = __any(low != 0.f);
+            share = __builtin_amdgcn_exp2f(-low);
         }
     }
     const Tiles whole{0, count};
@@ -340,7 +336,7 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
         const Tiles range = tiles_of(delta_keys);
         if (range.to) {
             walk(std::integral_constant<int, DELTA>{}, range);
-            formed = halves_sum(formed);
+            formed = halves_sum(formed) * share;
             if constexpr (SPLIT == 2) {
                 if (h == 0) deltas[half][wave][lane] = formed;
                 __syncthreads();
@@ -349,13 +345,14 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
             delta = exact ? formed : delta;
         }
     }
-    walk(std::integral_constant<int, GRADIENTS>{}, whole);
     if (real && h == 0 && half == 0) {
         const size_t at = (size_t)head * a.T + w.i;
         b.high[at] = high;
         b.low[at] = low;
         b.delta[at] = delta;
     }
+    delta *= share;                                   // as the walk takes it
+    walk(std::integral_constant<int, GRADIENTS>{}, whole);
     if constexpr (lifts<T>)
 #pragma unroll
         for (int n = 0; n < DB; ++n) dq[n] *= 1.f / lift;
@@ -364,14 +361,16 @@ __global__ __launch_bounds__(SPLIT * THREADS, ((splits<T, DB>) ? 2 : 1)) void qu
     if (some && mine) {
         const bool redo = not_finite(dq);
         if (real && !redo) store_column<T>(head_row<T>(b.dq, w.i, head), a.width, dq, a.scale, h);
-        for (uint64_t rows = __ballot(redo && real && h == 0); rows; rows &= rows - 1) {
+        uint64_t rows = __ballot(redo && real && h == 0);
+        if (rare(rows)) for (; rows; rows &= rows - 1) {
             const int l = __builtin_ctzll(rows);
             Shown s;
             s.lo = __shfl(w.s.lo, l, 64); s.hi = __shfl(w.s.hi, l, 64);
             s.first = __shfl(w.s.first, l, 64); s.sunk = __shfl(w.s.sunk, l, 64);
             const uint32_t i = __shfl(w.i, l, 64);
             float row[2];
-            query_row<T>(b, head, i, s, RowSum{__shfl(high, l, 64), __shfl(low, l, 64), __shfl(delta, l, 64)}, lane, row);
+            const size_t at = (size_t)head * a.T + i;
+            query_row<T>(b, head, i, s, RowSum{b.high[at], b.low[at], b.delta[at]}, lane, row);
             T* to = head_row<T>(b.dq, i, head);
 #pragma unroll
             for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) to[lane + c * WAVE] = (T)row[c];
@@ -595,10 +594,9 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, -l2[acc_row(r, 0)]);
             }
-            if (lowered)
+            if (rare(lowered) || !(i0 >= lo_most && i0 + 32 <= hi_least && !(a.skip_self && i0 <= j_last && i0 + 32 > j_first))) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] -= ll[acc_row(r, 0)];
-            if (!(i0 >= lo_most && i0 + 32 <= hi_least && !(a.skip_self && i0 <= j_last && i0 + 32 > j_first))) {
+                for (int r = 0; r < 16; ++r) s[r] -= ll[acc_row(r, 0)];      // (zero nearly always)
                 const uint32_t base = per_piece(i0 + 4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -680,7 +678,8 @@ __global__ __launch_bounds__(SPLIT * THREADS, SPLIT == 2 || DB * sizeof(T) <= 4 
             store_column<T>(head_row<T>(b.dv, j, kv_head), a.width, dv, 1.f, h);
         }
     }
-    for (uint64_t again = __ballot(redo && real && h == 0); again; again &= again - 1) {
+    uint64_t again = __ballot(redo && real && h == 0);
+    if (rare(again)) for (; again; again &= again - 1) {
         const int l = __builtin_ctzll(again);
         const uint32_t jl = __shfl(j, l, 64);
         float ck[2] = {0.f, 0.f}, cv[2] = {0.f, 0.f};

@@ -18,6 +18,9 @@ namespace w2v {
 
 typedef float Acc __attribute__((ext_vector_type(16)));      // a 32 x 32 result
 
+// A condition that hardly ever holds: what it guards, loops in loops, must not take registers from the walks.
+__device__ __forceinline__ bool rare(uint64_t x) { return __builtin_expect(x != 0, 0); }
+
 template <typename T> struct Frag { typedef typename Pack<T, 8>::vec vec; };      // a lane's eight values of an operand
 
 __device__ __forceinline__ void mma(const Frag<_Float16>::vec& a, const Frag<_Float16>::vec& b, Acc& c) {
@@ -196,7 +199,7 @@ template <typename T, int DB, int ROWS, int THREADS> struct Transit {
             for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_fit<T>(x[n], c0, width);
 #pragma unroll
         for (uint32_t n = 0; n < PER; ++n) *(typename Tl::Chunk*)(to + Tl::place(r0 + n * RS, c0 / Tl::N)) = x[n];
-        if (__builtin_expect(kept != ~0ull, 0)) {     // (over what was stored: selecting before it costs registers)
+        if (rare(~kept)) {                            // (over what was stored: selecting before it costs registers)
             const uint64_t gone = ~kept >> r0;
 #pragma unroll
             for (uint32_t n = 0; n < PER; ++n)

@@ -288,3 +288,42 @@ def test_spans_around_the_room_of_a_block(ty, d, span):
         print("span", ty, d, s, flush=True)
         got = whole(q.cuda(), k.cuda(), v.cuda(), dout.cuda(), device_offsets(lengths), bias=bias.cuda(), buckets=bmap.cuda())
         compare(got, ref, ty)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, BF16])
+def test_not_a_number_reaches_exactly_what_it_is_shown_to(ty):
+    """One key, one value or one query that is not a number, or an infinite score: forward and back, every column that the formulas
+    give it and no other."""
+    T, H, d, see = 400, 2, 60, dict(left=30, right=4, sinks=2)
+    q, k, v, dout = [t.cuda() for t in rows(T, H, 1, d, ty, 22)]
+    off = torch.tensor([0, 250, 400], dtype=torch.int64, device="cuda")
+    i, j = torch.arange(T, device="cuda")[:, None], torch.arange(T, device="cuda")[None]
+    first = torch.where(torch.arange(T, device="cuda") < 250, 0, 250)
+    shown = (first[:, None] == first[None]) & (j <= i + 4) & ((j >= i - 30) | (j - first[None] < 2))
+    clean = whole(q, k, v, dout, off, **see)
+    for at in (1, 120, 399):
+        for what, bad in (("k", math.nan), ("k", math.inf), ("v", math.nan), ("q", math.nan)):
+            a = dict(q=q.clone(), k=k.clone(), v=v.clone())
+            if bad == math.inf:
+                a["q"][..., 3] = 1.0
+                base = whole(a["q"], k, v, dout, off, **see)
+            else:
+                base = clean
+            if what == "v" or bad == math.inf:
+                a[what][at, :, 3] = bad
+            else:
+                a[what][at] = bad
+            out, lse, dq, dk, dv = whole(a["q"], a["k"], a["v"], dout, off, **see)
+            queries = shown[:, at] if what != "q" else torch.arange(T, device="cuda") == at
+            keys = (shown & queries[:, None]).any(0)
+            if what == "v":                                   # its own column forward; dP, and with it all of dS, back
+                column = torch.arange(d, device="cuda") == 3
+                assert torch.isnan(out[queries][..., column]).all() and torch.isfinite(lse).all()
+                assert torch.isfinite(out[..., ~column]).all() and torch.isfinite(dv).all()
+            else:
+                assert torch.isnan(out[queries]).all() and torch.isnan(lse[:, queries]).all() and torch.isnan(dv[keys]).all()
+            assert torch.isnan(dq[queries]).all() and torch.isnan(dk[keys]).all()
+            u = {F32: 1e-5, BF16: 2e-2}[ty]
+            for t, ref, rest in ((out, base[0], ~queries), (dq, base[2], ~queries), (dk, base[3], ~keys), (dv, base[4], ~keys)):
+                assert torch.allclose(t[rest].float(), ref[rest].float(), rtol=u, atol=u), (at, what, bad)
