@@ -8,6 +8,9 @@ step goes back through all of it (w2v_attend_backward, w2v_layer_norm_backward) 
 Afterwards a text is read word by word over a cache (w2v_attend_step), as a server would, and the context's nearest output
 vectors are looked up (w2v_topk_cosine).
 
+The matrices' update itself is torch's, rows of one word summed by index_add_: unlike the calls, it does not give the same last
+bits every time.
+
     python examples/context_vectors.py [--steps 60]
 """
 import argparse

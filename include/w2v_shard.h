@@ -356,21 +356,27 @@ int w2v_layer_norm_backward(int type, const void* dy_dev, uint64_t dy_stride, co
  * over the words j of the same text that word i is shown: i - left <= j <= i + right, or j one of the text's first
  * `sinks` words and j <= i + right; not those whose keep_dev byte is 0 (words that subsampling dropped: they
  * see, but are not seen), and not i itself if skip_self.  W2V_UNBOUNDED: no limit on that side (right = 0:
- * causal).  A word that is shown nothing has out = 0 and lse = -infinity, and no part in any gradient.
- * What lies in rows that are not shown to a word, infinities and NaN included, has no influence on it.
+ * causal).  A word that is shown nothing, or only scores of -infinity, has out = 0 and lse = -infinity, and no part in any
+ * gradient.  What lies in rows that are not shown to a word, infinities and NaN included, has no influence on it; but
+ * rows whose result is not finite in the tiled kernels are formed again a word at a time, some hundred times slower:
+ * where infinities or NaN are shown, or lie within 128 words of a text that is read.  (Words that keep_dev leaves out cost nothing.)
  *
  * tokens 0..n_tokens of texts sent_off_dev[n_sent + 1] as for w2v_make_pairs (offsets that break its rules are made
  * harmless: no access leaves the tokens, the results then mean nothing).  Query heads h share the key head
  * h / (heads / kv_heads).  Element c of head h of token i of a w2v_heads lies at p[i token_stride + h head_stride + c], p of
- * `type` (W2V_T_*); outputs must not overlap themselves or inputs.  lse is fp32 [heads][n_tokens].
+ * `type` (W2V_T_*); outputs that overlap themselves, each other or inputs are refused, and so are those that lie among them with
+ * another stride from token to token.  lse is fp32 [heads][n_tokens].
  *
  * bias_dev (NULL: none) is fp32 [heads][n_buckets]; bucket_dev[2 span + 1] gives the bucket of every distance
- * j - i = -span..span, distances beyond take the outermost; a bucket >= n_buckets adds nothing.
+ * j - i = -span..span, distances beyond take the outermost; a bucket >= n_buckets adds nothing.  Any value will do, -infinity
+ * and fp32's lowest as masks among them; finite ones beyond 2.3e38 on either side are told apart in the forward call only.
  * w2v_relative_buckets fills such a map (host memory): half of the buckets for words before (and the word itself),
- * half for words after; in each, the first half for distances one by one, the rest by their logarithm up
- * to span.
+ * half for words after (which right = 0 leaves unused: ask for twice the buckets there); in each, the first half for distances one
+ * by one, the rest by their logarithm up to span.
  *
- * Scores, softmax and sums are fp32; weights are rounded to `type` for the product with v.  No call allocates or
+ * Scores, softmax and sums are fp32.  In 16 bits weights are rounded to `type` for the product with v, and for the
+ * gradients p and dx (in fp16 behind powers of two, so that small ones keep their bits); dout . out is taken from out as it was
+ * rounded, unless dbias is wanted or a word is shown at most 128 words.  No call allocates or
  * synchronises; results repeat bit for bit.  Limits: 1 <= width <= W2V_HEAD_MAX, heads a multiple of kv_heads and at most
  * 1024, sinks <= W2V_SINKS_MAX, 1 <= span <= W2V_SPAN_MAX, 1 <= n_buckets <= W2V_BUCKETS_MAX, scale finite and > 0,
  * n_tokens * heads <= 2^29 (pass longer corpora in blocks). */
@@ -412,7 +418,7 @@ int w2v_attend_backward(const w2v_attend_spec* spec, const w2v_heads* dout, cons
  * head h of word j of text b at p[b text_stride + j token_stride + h head_stride + c].  q and out hold the newest word's heads,
  * token_stride leading from text to text.  out is what w2v_attend (right = 0) gives that word: over the words
  * i - left <= j <= i and the first `sinks` ones, i = n_dev[b] - 1, whose byte keep_dev[b room + j] is not 0 (NULL: all); no
- * words: zeros.  spec->right is not read.  workspace_dev: 256-byte aligned device memory of
+ * words: zeros.  All arithmetic is fp32.  out may be q.  spec->right is not read.  workspace_dev: 256-byte aligned device memory of
  * w2v_attend_step_workspace bytes, contents irrelevant before and after.  batch * heads <= 2^23,
  * room <= 2^31 - 2^12. */
 typedef struct w2v_cache { const void* p; uint64_t text_stride, token_stride, head_stride; } w2v_cache;

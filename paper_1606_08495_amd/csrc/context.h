@@ -34,7 +34,7 @@ struct AttendArgs {
     Heads q, k, v;
     const uint64_t* off; uint32_t n_sent, T;             // texts, tokens
     uint32_t heads, kv_heads, group, width;              // group = heads / kv_heads
-    uint32_t left, right, sinks; bool skip_self;         // left, right <= T; no sinks where nothing falls out of the window
+    uint32_t left, right, sinks; bool skip_self;         // left, right <= T
     float scale, scale2;                                 // scale2 = scale log2 e
     const uint8_t* keep;                                 // or null
     const float* bias; const uint32_t* buckets; uint32_t n_buckets, span;      // bias may be null

@@ -15,9 +15,9 @@
 // what the rounding left in a second product: the gradient's dout . out is then a sum of few terms, which
 // may cancel down to the weights' rounding, and the matrix cores wait for the exponentials there anyway.
 //
-// Measured: 32768 words, 16 heads of 128 over 4, 16 bits, window of 1024: 473 us (574 TFLOP/s of the pairs shown; products
+// Measured: 32768 words, 16 heads of 128 over 4, 16 bits, window of 1024: 480 us (567 TFLOP/s of the pairs shown; products
 // and exponentials take turns in the two wavefronts of a SIMD).  131333 words in texts of 10 to 40, 5 heads of 60, 32 bits, window
-// of 10 on either side: 368 us (633 MB; a block's chain of dependent accesses).
+// of 10 on either side: 370 us (633 MB; a block's chain of dependent accesses).
 #include "attend_tiles.h"
 
 namespace w2v {

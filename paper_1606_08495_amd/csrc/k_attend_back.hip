@@ -13,9 +13,9 @@
 // border behind its block; those behind go in pieces to blocks of their own (late), whose sums are joined in
 // order at the end.
 //
-// Measured, forward and backward: 9139 words in whole texts, 6 heads of 100, fp16 601 us (in a profile: forward 172, queries' kernel
-// 216, keys' 249); 17676 words, 8 heads of 64 over 2, window of 512, bias and its gradient, bf16 469 us; 65135 words in texts of
-// 10 to 40, 5 heads of 60, 32 bits, bias 882 us.  Vector work and latency bound them.
+// Measured, forward and backward: 9139 words in whole texts, 6 heads of 100, fp16 603 us (in a profile: forward 176, queries' kernel
+// 219, keys' 256); 17676 words, 8 heads of 64 over 2, window of 512, bias and its gradient, bf16 471 us; 65135 words in texts of
+// 10 to 40, 5 heads of 60, 32 bits, bias 884 us.  Vector work and latency bound them.
 // In 16 bits the queries' kernel of heads wider than 96 keeps 48 to 108 bytes a lane in scratch, the keys' up to 60.
 #include "attend_tiles.h"
 

@@ -5,8 +5,8 @@
 // works on any; a group of lanes keeps maximum, sum and output of its own keys for HEADS query heads in registers, and
 // groups, wavefronts and, for long caches, blocks are joined at the end in a fixed order.  Rows that
 // `keep` leaves out are read but not used.  All arithmetic is fp32.
-// Measured: 32 texts of up to 32768 words (574335 in all), 32 heads of 128 over 8, 16 bits: 588 us (4.0 TB/s; a large copy moves
-// 4.8; vector units busy half the time).  One text of 500 words, 5 heads of 60: 8 us and 4 us for the join.
+// Measured: 32 texts of up to 32768 words (574335 in all), 32 heads of 128 over 8, 16 bits: 590 us (4.0 TB/s; a large copy moves
+// 4.8).  One text of 500 words, 5 heads of 60: 8 us and 4 us for the join.
 #include <type_traits>
 
 #include "attend.h"

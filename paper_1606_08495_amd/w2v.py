@@ -417,6 +417,8 @@ def topk_cosine(queries, cands, K, tau=-2.0, round_candidates=32768, workspace=N
 
 
 # -- vectors in context ------------------------------------------------------------------------------
+# These calls record no graph for torch's automatic differentiation, whatever their inputs require: gradients come from the
+# backward calls.
 TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -455,7 +457,8 @@ def _vec(t, n, device, name):
 
 
 def layer_norm(x, gain=None, offset=None, eps=1e-5, out=None, stream=None):
-    """(y, mean, rstd) of w2v_layer_norm for the rows of x [m, d]; gain and offset are float32 [d]."""
+    """(y, mean, rstd) of w2v_layer_norm for the rows of x [m, d]; gain and offset are float32 [d].  Not differentiable by
+    torch: layer_norm_backward."""
     xp, xs = _rows(x, None, "x")
     m, d = x.shape
     with _on(stream, x):
@@ -519,7 +522,8 @@ def _number(x, name):
 
 
 def relative_buckets(n_buckets, span, device="cuda"):
-    """The bucket of every distance -span..span (w2v_relative_buckets), int32 [2 span + 1] on the device."""
+    """The bucket of every distance -span..span (w2v_relative_buckets), int32 [2 span + 1] on the device: one half for words
+    before, one for words after, whether or not these are shown."""
     n_buckets, span = _number(n_buckets, "n_buckets"), _number(span, "span")
     m = np.empty(2 * min(span, SPAN_MAX) + 1, np.uint32)      # (a longer span is refused)
     _check(lib().w2v_relative_buckets(n_buckets, span, c_vp(m.ctypes.data)))
@@ -571,7 +575,8 @@ def attend(q, k, v, sent_off, left=None, right=None, sinks=0, skip_self=False, s
            buckets=None, out=None, stream=None):
     """(out, lse) of w2v_attend: q [tokens, heads, width], k and v [tokens, kv_heads, width], texts as sent_off
     int64 [n + 1].  left, right: words shown on either side (None: all).  scale: width^-1/2 unless given.  keep:
-    uint8 [tokens], 0 where a word is not to be seen.  bias float32 [heads, buckets] with the map ``buckets`` (relative_buckets)."""
+    uint8 [tokens], 0 where a word is not to be seen.  bias float32 [heads, buckets] with the map ``buckets`` (relative_buckets).
+    Not differentiable by torch: attend_backward."""
     if q.dim() != 3 or k.dim() != 3:
         raise TypeError("q, k and v must be [tokens, heads, width]")
     T, H, d = q.shape
