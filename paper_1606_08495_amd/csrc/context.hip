@@ -149,15 +149,22 @@ int check_apart(const w2v_heads* out, uint32_t out_heads, const char* out_name, 
     };
     if (a + reach(out, out_heads) <= b || b + reach(in, in_heads) <= a) return W2V_OK;
     const int64_t step = rows > 1 ? (int64_t)out->token_stride : 0, width = s->width;
+    // words w of the input on either side of an output's head that lies `far` elements on from one of the input's
+    const auto touches = [&](int64_t far) {
+        const int64_t from = step ? far / step : 0;
+        bool meet = false;
+        for (int64_t w = from - 1; w <= from + 1; ++w) meet |= std::llabs(far - w * step) < width && std::llabs(w) < (int64_t)rows;
+        return meet;
+    };
     bool meet = rows > 1 && out->token_stride != in->token_stride;
-    for (uint32_t h = 0; h < out_heads && !meet; ++h)
-        for (uint32_t g = 0; g < in_heads && !meet; ++g) {
-            // words `from` and from + 1 of the input apart are the nearest to the output's head on either side
-            const int64_t far = (int64_t)(a + h * out->head_stride) - (int64_t)(b + g * in->head_stride);
-            const int64_t from = step ? far / step : 0;
-            for (int64_t w = from - 1; w <= from + 1; ++w)
-                meet |= std::llabs(far - w * step) < width && std::llabs(w) < (int64_t)rows;
-        }
+    if (out->head_stride == in->head_stride) {        // what counts is how many heads apart two are
+        for (int64_t d = 1 - (int64_t)in_heads; d < (int64_t)out_heads && !meet; ++d)
+            meet = touches((int64_t)(a - b) + d * (int64_t)out->head_stride);
+    } else {
+        for (uint32_t h = 0; h < out_heads && !meet; ++h)
+            for (uint32_t g = 0; g < in_heads && !meet; ++g)
+                meet = touches((int64_t)(a + h * out->head_stride) - (int64_t)(b + g * in->head_stride));
+    }
     return meet ? fail(W2V_ERR_ARG, "%s overlaps %s", out_name, in_name) : W2V_OK;
 }
 
