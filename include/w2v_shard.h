@@ -427,6 +427,81 @@ int w2v_attend_step(const w2v_attend_spec* spec, const w2v_heads* q, const w2v_c
                     const uint32_t* n_dev, uint32_t batch, uint32_t room, const uint8_t* keep_dev,
                     const w2v_heads* out, void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/* ---- positions that turn ---------------------------------------------------------------------------------
+ * The other way to tell a word's place than a bias by distance: the first `rotated` elements of each head of a query or key are
+ * r / 2 pairs, and pair c of the word at position p is turned by p f_c, so that scores depend on distances alone:
+ *     y_a = gain (x_a cos(p f_c) - x_b sin(p f_c)),   y_b = gain (x_a sin(p f_c) + x_b cos(p f_c)),
+ * (a, b) = (2 c, 2 c + 1), or with halves (c, c + r / 2).  Elements from `rotated` on pass as they are, and gain does not touch them.
+ * turns_dev[r / 2] holds f_c as a whole number of 2^-64 of a full turn, modulo 2^64: angles are exact modulo a turn at every
+ * position.  Sines and products are fp32, the result is rounded once.
+ *
+ * w2v_rotary_turns fills such an array (host memory) with f_c = base^(-2 c / r), or for texts longer than those trained on
+ *     W2V_ROTARY_LINEAR   f_c / factor
+ *     W2V_ROTARY_BASE     f_c factor^(-2 c / (r - 2)): the first pair as it was, the last divided by factor
+ *     W2V_ROTARY_PARTS    f_c (w + (1 - w) / factor), w = (t - low) / (high - low) held to 0..1, t = trained f_c / 2 pi: pairs of more
+ *                         than `high` turns over the `trained` words stay, those of less than `low` are divided by factor
+ * base > 1 and factor >= 1 finite, 0 <= low < high, trained > 0 (these three are read for W2V_ROTARY_PARTS alone).
+ *
+ * w2v_rotate turns x and, if y is not NULL, y (queries and keys of the same words) into x_out and y_out, which may be x and
+ * y; outputs that otherwise overlap inputs, themselves or each other are refused.  A word's position is its place in its text by
+ * sent_off_dev[n_sent + 1], as for w2v_attend, or position_dev[n_tokens] (int32, negative ones too) where that is not NULL; sent_off_dev is
+ * not read then.  Words that no text has are left as they were in the outputs.  back: by the angles' negatives, gain as
+ * before, which gives the gradients by x and y from those by x_out and y_out.  Nothing is allocated or synchronised. */
+#define W2V_ROTARY_PLAIN  0
+#define W2V_ROTARY_LINEAR 1
+#define W2V_ROTARY_BASE   2
+#define W2V_ROTARY_PARTS  3
+typedef struct w2v_rotary {
+    uint32_t rotated;                    /* even, 2 .. width */
+    uint32_t halves;
+    float gain;                          /* finite */
+    const uint64_t* turns_dev;
+} w2v_rotary;
+int w2v_rotary_turns(uint32_t rotated, double base, int scaling, double factor, uint32_t trained, double low, double high,
+                     uint64_t* turns_host);
+int w2v_rotate(int type, uint32_t width, const w2v_rotary* rotary, int back, const w2v_heads* x, uint32_t heads,
+               const w2v_heads* y, uint32_t y_heads, const uint64_t* sent_off_dev, uint32_t n_sent, uint32_t n_tokens,
+               const int32_t* position_dev, const w2v_heads* x_out, const w2v_heads* y_out, void* stream);
+
+/* ---- a cache in pages, and one new word per text over it ---------------------------------------------------
+ * Keys and values of many texts lie in one pool of n_pages pages of page_words words each (a power of two, at most
+ * W2V_PAGE_WORDS_MAX): element c of head h of place s of page g at p[g page_stride + s token_stride + h head_stride + c].  Word j of
+ * text b is at place j % page_words of page page_dev[b stride + j / page_words]; a text's row of the table has `slots` pages, room for
+ * slots * page_words words.  A number >= n_pages is no page: nothing is written there, and words there are not shown.
+ *
+ * w2v_pages_append puts new words behind what their texts have.  Tokens 0..n_tokens are new words of texts sent_off_dev[n_sent + 1], any
+ * number each, or with sent_off_dev = NULL one word of each of n_sent = n_tokens texts.  n_dev[b] counts text b's words with the
+ * new ones, as w2v_attend_pages wants it: the last new word of text b is its word n_dev[b] - 1.  Words that would lie before the
+ * text's first or past its room are not kept.  k (turned by the word's number in its text, or by position_dev, unless rotary is NULL)
+ * and v go into the pages; q, if not NULL, is turned alike into q_out (which may be q).  Words that no text has, and all other
+ * places of the pools, are left as they were.  Two words at one place of the pools: one of them is kept, element by element.  A place that
+ * another text's row lists too (a common prefix) is written for both.  Pools that overlap each other or an input are refused.
+ *
+ * w2v_attend_pages gives what w2v_attend_step does, over pages: spec, n_dev, q and out are as there (out may be q),
+ * keep_dev is [batch][slots * page_words].  shared (a multiple of page_words, at most the room; 0: none): the first `shared` words of all
+ * texts lie in the pages of row 0 of the table, whatever the other rows hold there; they are read once for all texts and not
+ * once for each.  A text that has fewer words is shown those it has.
+ * Scores, softmax and sums are fp32; in 16 bits weights may be rounded to `type` for the product with v.
+ * workspace_dev: 256-byte aligned device memory of w2v_attend_pages_workspace bytes, contents irrelevant before and after; calls that
+ * may run at the same time need one each.  Nothing is allocated or synchronised; results repeat bit for bit.
+ * batch * heads <= 2^23, slots * page_words <= 2^31 - 2^12, n_pages >= 1. */
+#define W2V_PAGE_WORDS_MAX 4096
+typedef struct w2v_pages { void* p; uint64_t page_stride, token_stride, head_stride; } w2v_pages;
+typedef struct w2v_page_table {
+    const uint32_t* page_dev;
+    uint64_t stride;
+    uint32_t slots, page_words, n_pages;
+} w2v_page_table;
+int w2v_pages_append(int type, uint32_t width, const w2v_rotary* rotary /* may be NULL */, const w2v_heads* k,
+                     const w2v_heads* v, uint32_t kv_heads, const w2v_heads* q, uint32_t heads, const w2v_heads* q_out,
+                     const uint64_t* sent_off_dev, uint32_t n_sent, uint32_t n_tokens, const uint32_t* n_dev,
+                     const int32_t* position_dev, const w2v_page_table* table, const w2v_pages* k_pages,
+                     const w2v_pages* v_pages, void* stream);
+size_t w2v_attend_pages_workspace(const w2v_attend_spec* spec, uint32_t batch, const w2v_page_table* table, uint32_t shared);
+int w2v_attend_pages(const w2v_attend_spec* spec, const w2v_heads* q, const w2v_pages* k_pages, const w2v_pages* v_pages,
+                     const w2v_page_table* table, uint32_t shared, const uint32_t* n_dev, uint32_t batch,
+                     const uint8_t* keep_dev, const w2v_heads* out, void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* Seed of minibatch number h (the client picks a fresh seed per minibatch), a function of a master seed. */
 uint64_t w2v_minibatch_seed(uint64_t master_seed, uint64_t h);
 

@@ -1,4 +1,5 @@
-// Launches of the context operators (layer norm, attention over texts) for context.hip, which checks what callers pass.
+// Launches of the context operators (layer norm, attention over texts, positions, pages) for context.hip and pages.hip, which
+// check what callers pass.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stddef.h>
@@ -68,9 +69,30 @@ struct StepArgs {
     const uint8_t* keep;                                 // [batch][room] or null
     const float* bias; const uint32_t* buckets; uint32_t n_buckets, span;
     uint32_t splits, per_split; float* parts;            // workspace: [batch][heads][splits][width + 2]
+    // over pages: k.text and v.text lead from page to page, word j of a text is on page table[text table_stride + (j >> shift)] (row 0
+    // for j < shared); room is the table's
+    const uint32_t* table; uint64_t table_stride; uint32_t shift, n_pages, shared;
 };
 struct StepSplits { uint32_t splits, per_split; };
 StepSplits step_splits(uint32_t batch, uint32_t kv_heads, uint32_t room, uint32_t left, uint32_t sinks);
 void launch_step(const StepArgs& a, uint32_t type, hipStream_t st);
+void launch_step_pages(const StepArgs& a, uint32_t type, hipStream_t st);
+
+// ---- positions that turn, and words on their way into pages ------------------------------------------
+struct Pages { void* p; uint64_t page, token, head; };
+struct TurnArray { Heads in; void* out; uint64_t out_token, out_head; uint32_t heads; };      // heads = 0: none
+struct TurnArgs {
+    // rotate: x, y turned.  append: q, k turned, v as it is; k and v go into pages, out_token leading from place to place there
+    TurnArray x, y, z;
+    uint32_t width, rotated; bool halves, back; float gain;
+    const uint64_t* turns;                               // [rotated / 2]
+    const uint64_t* off; uint32_t n_sent, T;             // off null: token i is of text i, or positions are given
+    const int32_t* position;                             // or null
+    uint32_t tokens;                                     // of a block
+    // append
+    const uint32_t* n; const uint32_t* table; uint64_t table_stride, y_page, z_page; uint32_t room, shift, n_pages;
+};
+void launch_rotate(TurnArgs a, uint32_t type, hipStream_t st);
+void launch_append(TurnArgs a, uint32_t type, hipStream_t st);
 
 }  // namespace w2v

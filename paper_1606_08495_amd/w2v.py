@@ -22,6 +22,8 @@ NOALLOC_SCRATCH_U32 = 1 << 21
 
 UNBOUNDED = 0xFFFFFFFF
 HEAD_MAX, SINKS_MAX, SPAN_MAX, BUCKETS_MAX = 128, 64, 1023, 1024
+ROTARY_SCALING = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+PAGE_WORDS_MAX = 4096
 
 c_u32, c_u64, c_vp = ctypes.c_uint32, ctypes.c_uint64, ctypes.c_void_p
 
@@ -81,6 +83,15 @@ _SIGNATURES = {
     "w2v_attend_step_workspace": (ctypes.c_size_t, [c_vp, c_u32, c_u32]),
     "w2v_attend_step": (ctypes.c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_u32, c_u32, c_vp, c_vp, c_vp, ctypes.c_size_t,
                                        c_vp]),
+    "w2v_rotary_turns": (ctypes.c_int, [c_u32, ctypes.c_double, ctypes.c_int, ctypes.c_double, c_u32, ctypes.c_double,
+                                        ctypes.c_double, c_vp]),
+    "w2v_rotate": (ctypes.c_int, [ctypes.c_int, c_u32, c_vp, ctypes.c_int, c_vp, c_u32, c_vp, c_u32, c_vp, c_u32, c_u32, c_vp,
+                                  c_vp, c_vp, c_vp]),
+    "w2v_pages_append": (ctypes.c_int, [ctypes.c_int, c_u32, c_vp, c_vp, c_vp, c_u32, c_vp, c_u32, c_vp, c_vp, c_u32, c_u32, c_vp,
+                                        c_vp, c_vp, c_vp, c_vp, c_vp]),
+    "w2v_attend_pages_workspace": (ctypes.c_size_t, [c_vp, c_u32, c_vp, c_u32]),
+    "w2v_attend_pages": (ctypes.c_int, [c_vp, c_vp, c_vp, c_vp, c_vp, c_u32, c_vp, c_u32, c_vp, c_vp, c_vp, ctypes.c_size_t,
+                                        c_vp]),
     "w2v_minibatch_seed": (c_u64, [c_u64, c_u64]),
     "w2v_shard_timing_enable": (ctypes.c_int, [c_vp, ctypes.c_int]),
     "w2v_shard_timing_read": (ctypes.c_int, [c_vp, c_vp, c_vp]),
@@ -660,4 +671,176 @@ def attend_step(q, k, v, n, left=None, sinks=0, skip_self=False, scale=None, kee
         _check(lib().w2v_attend_step(r(spec), r(_heads(q, q, B, H, "q")), r(_cache(k, q, shape, "k")),
                                      r(_cache(v, q, shape, "v")), _dev(n, IDX, "n"), B, room, _dev(keep, torch.uint8, "keep"),
                                      r(_heads(out, q, B, H, "out")), at, size, st))
+    return out
+
+
+# -- positions that turn, and a cache in pages --------------------------------------------------------
+class Rotary(ctypes.Structure):
+    """w2v_rotary."""
+    _fields_ = [("rotated", c_u32), ("halves", c_u32), ("gain", ctypes.c_float), ("turns_dev", c_vp)]
+
+
+class Pages(ctypes.Structure):
+    """w2v_pages: element c of head h of place s of page g at p[g page_stride + s token_stride + h head_stride + c]."""
+    _fields_ = [("p", c_vp), ("page_stride", c_u64), ("token_stride", c_u64), ("head_stride", c_u64)]
+
+
+class PageTable(ctypes.Structure):
+    """w2v_page_table."""
+    _fields_ = [("page_dev", c_vp), ("stride", c_u64), ("slots", c_u32), ("page_words", c_u32), ("n_pages", c_u32)]
+
+
+def rotary_turns(rotated, base=10000.0, scaling="plain", factor=1.0, trained=0, low=1.0, high=32.0, device="cuda"):
+    """What each pair of the first ``rotated`` columns turns from word to word (w2v_rotary_turns), in 2^-64 of a turn: int64
+    (uint64 bits) [rotated / 2] on the device.  ``scaling``: "plain", or for longer texts than trained on "linear", "base", "parts"."""
+    if scaling not in ROTARY_SCALING:
+        raise ValueError("scaling %r is none of %s" % (scaling, ", ".join(ROTARY_SCALING)))
+    rotated = _number(rotated, "rotated")
+    turns = np.empty(min(rotated, HEAD_MAX) // 2 + 1, np.uint64)      # (more are refused)
+    _check(lib().w2v_rotary_turns(rotated, float(base), ROTARY_SCALING[scaling], float(factor), _number(trained, "trained"),
+                                  float(low), float(high), c_vp(turns.ctypes.data)))
+    return torch.from_numpy(turns[:rotated // 2].view(np.int64).copy()).to(device)
+
+
+def _rotary(turns, halves, gain, q):
+    if turns.dim() != 1 or turns.device != q.device:
+        raise ValueError("turns must be [rotated / 2] on the device of q")
+    return Rotary(2 * turns.numel(), 1 if halves else 0, float(gain), _dev(turns, torch.int64, "turns"))
+
+
+def _positions(positions, q):
+    if positions is None:
+        return None
+    if positions.shape != (q.shape[0],) or positions.device != q.device:
+        raise ValueError("positions must be [tokens] on the device of q")
+    return _dev(positions, IDX, "positions")
+
+
+def _into(out, x, name):
+    """A result of its own making, or the caller's: the tensor and its w2v_heads."""
+    n, heads, width = x.shape
+    if out is None:
+        out = x.new_empty(x.shape)
+        return out, _dense(out, heads, width)
+    return out, _heads(out, x, n, heads, name)
+
+
+def rotate(q, turns, k=None, sent_off=None, positions=None, halves=False, gain=1.0, back=False, out=None, k_out=None,
+           stream=None):
+    """w2v_rotate of q [tokens, heads, width] (and k [tokens, kv_heads, width]) by their words' places in the texts sent_off
+    (int64 [n + 1]) or by ``positions`` (int32 [tokens]); turns as of rotary_turns.  Returns the turned q, or (q, k).  out, k_out: where to
+    (q and k themselves will do).  back=True takes gradients by the results to gradients by q and k.  Not differentiable by
+    torch.  Rows of words that no text has are left as they were in out and k_out."""
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise TypeError("q and k must be [tokens, heads, width]")
+    if q.dtype not in TYPES:
+        raise TypeError("q must be float32, float16 or bfloat16")
+    if sent_off is None and positions is None:
+        raise ValueError("sent_off or positions must say where the words stand")
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
+    T, H, d = q.shape
+    with _on(stream, q):
+        st, r = _raw_stream(q.device.index), ctypes.byref
+        at = _positions(positions, q)
+        off, n = (None, 0) if sent_off is None else _texts(sent_off, None, q)[:2]
+        turned = _rotary(turns, halves, gain, q)
+        out, into = _into(out, q, "out")
+        G, y, y_into = 0, None, None
+        if k is not None:
+            G = k.shape[1]
+            y = r(_heads(k, q, T, G, "k"))
+            k_out, y_into = _into(k_out, k, "k_out")
+            y_into = r(y_into)
+        _check(lib().w2v_rotate(TYPES[q.dtype], d, r(turned), 1 if back else 0, r(_heads(q, q, T, H, "q")), H, y, G, off, n, T, at,
+                                r(into), y_into, st))
+    return out if k is None else (out, k_out)
+
+
+def _pages(t, like, heads, name):
+    """A pool [pages, words of a page, heads, width]."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == like.dtype and t.device == like.device and t.dim() == 4 and
+            t.shape[2] == heads and t.shape[3] == like.shape[2]):
+        raise TypeError("%s must be a CUDA tensor [pages, words, %d, %d] of %s" % (name, heads, like.shape[2], like.dtype))
+    a, b, c, e = t.stride()
+    if (e != 1 and t.shape[3] > 1) or min(a, b, c) < 0:
+        raise ValueError("%s: the elements of a head must lie side by side" % name)
+    return Pages(t.data_ptr(), a, b, c)
+
+
+def _table(table, n, k_pages, v_pages, q):
+    if k_pages.shape[:2] != v_pages.shape[:2]:
+        raise ValueError("k_pages and v_pages differ in their pages")
+    if not isinstance(table, torch.Tensor) or table.dtype != IDX or table.dim() != 2 or table.device != q.device:
+        raise TypeError("table must be a CUDA tensor [texts, slots] of int32 on the device of q")
+    if table.stride(1) != 1 and table.shape[1] > 1 or table.stride(0) < 0:
+        raise ValueError("table: the pages of a text must lie side by side")
+    if n.shape != (table.shape[0],) or n.device != q.device:
+        raise ValueError("n must be [texts] on the device of q")
+    return PageTable(table.data_ptr(), table.stride(0), _number(table.shape[1], "slots"), _number(k_pages.shape[1], "words of a page"),
+                     _number(k_pages.shape[0], "pages"))
+
+
+def pages_append(k, v, k_pages, v_pages, table, n, sent_off=None, turns=None, positions=None, halves=False, gain=1.0, q=None,
+                 q_out=None, stream=None):
+    """w2v_pages_append: new words' k and v [tokens, kv_heads, width] behind what their texts have in the pools k_pages and v_pages
+    [pages, words of a page, kv_heads, width], table int32 [texts, slots], n int32 [texts] counting the new words too.  The new words are those
+    of texts sent_off (int64 [texts + 1]), or one of each text.  With turns (rotary_turns) k is turned on the way by its place in its text, or
+    by ``positions`` (int32 [tokens]); q [tokens, heads, width] is turned alike and returned (into q_out, which may be q)."""
+    if k.dim() != 3 or (q is not None and q.dim() != 3):
+        raise TypeError("q, k and v must be [tokens, heads, width]")
+    if k.dtype not in TYPES:
+        raise TypeError("k must be float32, float16 or bfloat16")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    if turns is None and (q is not None or positions is not None):
+        raise ValueError("q or positions without turns")
+    T, G, d = k.shape
+    with _on(stream, k):
+        st, r = _raw_stream(k.device.index), ctypes.byref
+        spec = _table(table, n, k_pages, v_pages, k)
+        if sent_off is not None and sent_off.numel() != table.shape[0] + 1:
+            raise ValueError("sent_off must have %d entries" % (table.shape[0] + 1))
+        off = None if sent_off is None else _texts(sent_off, None, k)[0]
+        turned = None if turns is None else r(_rotary(turns, halves, gain, k))
+        at = _positions(positions, k)
+        H, x, into = 0, None, None
+        if q is not None:
+            H = q.shape[1]
+            x = r(_heads(q, k, T, H, "q"))
+            q_out, into = _into(q_out, q, "q_out")
+            into = r(into)
+        _check(lib().w2v_pages_append(TYPES[k.dtype], d, turned, r(_heads(k, k, T, G, "k")), r(_heads(v, k, T, G, "v")), G, x, H, into,
+                                      off, table.shape[0], T, _dev(n, IDX, "n"), at, r(spec), r(_pages(k_pages, k, G, "k_pages")),
+                                      r(_pages(v_pages, k, G, "v_pages")), st))
+    return q_out
+
+
+def attend_pages(q, k_pages, v_pages, table, n, shared=0, left=None, sinks=0, skip_self=False, scale=None, keep=None, bias=None,
+                 buckets=None, out=None, workspace=None, stream=None):
+    """out [texts, heads, width] of w2v_attend_pages: the newest word's q [texts, heads, width] over the pages of its text, table
+    int32 [texts, slots], n int32 [texts] words each (the newest among them).  The first ``shared`` words of all texts lie in the pages of
+    the table's row 0.  keep: uint8 [texts, slots * words of a page].  ``workspace``: optional uint8 device tensor to reuse.  Other
+    arguments as for ``attend_step``."""
+    if q.dim() != 3 or k_pages.dim() != 4 or v_pages.dim() != 4:
+        raise TypeError("q must be [texts, heads, width], k_pages and v_pages [pages, words, heads, width]")
+    B, H, d = q.shape
+    G = k_pages.shape[2]
+    with _on(stream, q):
+        st, r = _raw_stream(q.device.index), ctypes.byref
+        pages = _table(table, n, k_pages, v_pages, q)
+        if table.shape[0] != B:
+            raise ValueError("table must have a row for each of %d texts" % B)
+        if keep is not None and (keep.shape != (B, table.shape[1] * k_pages.shape[1]) or keep.device != q.device):
+            raise ValueError("keep must be [texts, slots * words of a page] on the device of q")
+        spec = _spec(q, G, left, 0, sinks, skip_self, scale, bias, buckets)
+        shared = _number(shared, "shared")
+        out, into = _into(out, q, "out")
+        if workspace is None:
+            need = int(lib().w2v_attend_pages_workspace(r(spec), B, r(pages), shared))
+            workspace = q.new_empty(max(need, 256), dtype=torch.uint8)
+        at, size = _room(workspace, q.device)
+        _check(lib().w2v_attend_pages(r(spec), r(_heads(q, q, B, H, "q")), r(_pages(k_pages, q, G, "k_pages")),
+                                      r(_pages(v_pages, q, G, "v_pages")), r(pages), shared, _dev(n, IDX, "n"), B,
+                                      _dev(keep, torch.uint8, "keep"), r(into), at, size, st))
     return out

@@ -1,0 +1,261 @@
+"""Positions that turn: against the definition in 64 bits, the gradients, strides, streams, graphs, and what is refused."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_1606_08495_amd import w2v
+from rotary_reference import places, rotate_reference, within
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+def run(offsets, H, G, d, r, ty, halves=False, gain=1.0, back=False, seed=0, **turned):
+    T = offsets[-1]
+    g = torch.Generator().manual_seed(seed)
+    q, k = torch.randn(T, H, d, generator=g).to(ty), torch.randn(T, G, d, generator=g).to(ty)
+    turns = w2v.rotary_turns(r, device="cpu", **turned)
+    at = places(offsets, T)
+    got = w2v.rotate(q.cuda(), turns.cuda(), k=k.cuda(), sent_off=torch.tensor(offsets).cuda(), halves=halves, gain=gain, back=back)
+    for x, y in zip((q, k), got):
+        want, bound = rotate_reference(x, at, turns, halves, gain, back)
+        within(y, want, bound)
+        assert torch.equal(y[..., r:].cpu(), x[..., r:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("H,G,d,r", [(1, 1, 2, 2), (5, 5, 60, 60), (4, 2, 128, 128), (4, 1, 128, 64), (6, 2, 37, 36), (3, 3, 37, 2),
+                                     (2, 1, 33, 30), (8, 8, 100, 50), (40, 5, 127, 126), (1, 1, 3, 2), (7, 7, 15, 14), (9, 3, 72, 72)])
+def test_heads_widths_and_layouts(H, G, d, r, ty):
+    print("rotate", H, G, d, r, ty, flush=True)
+    offsets = [0, 1, 1, 4, 90, 91, 200, 517]
+    for halves in (False, True):
+        run(offsets, H, G, d, r, ty, halves)
+        run(offsets, H, G, d, r, ty, halves, gain=1.25, back=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [1, 2, 15, 16, 17, 2048, 2049, 4097, 40000])
+def test_numbers_of_words(tokens):
+    """Blocks of 1 to 16 words, the last one not full; texts of every length up to all words, and many without any."""
+    print("rotate", tokens, flush=True)
+    run([0, tokens], 2, 1, 20, 20, F32, halves=True)
+    g = torch.Generator().manual_seed(tokens)
+    cuts = torch.randint(0, tokens + 1, (300,), generator=g).sort().values.tolist()
+    run([0] + cuts + [tokens], 2, 1, 20, 12, F16, gain=0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("halves", [False, True])
+def test_far_and_negative_positions(halves):
+    at = torch.tensor([0, 1, -1, 100_003, -100_003, 2 ** 30, 2 ** 31 - 1, -2 ** 31, 12_345_678] * 5, dtype=torch.int32)
+    turns = w2v.rotary_turns(64, device="cpu")
+    turns[3] = -2 ** 63                          # half a turn
+    turns[4] = -1                                # a little less than a whole one
+    q = torch.randn(at.numel(), 3, 70)
+    got = w2v.rotate(q.cuda(), turns.cuda(), positions=at.cuda(), halves=halves)
+    within(got, *rotate_reference(q, at, turns, halves))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("halves", [False, True])
+def test_gradients(halves, ty):
+    """Back against the transpose by the formula (test_heads_widths_and_layouts) and here against differences of the call itself: it is
+    linear, so that a step of any size will do."""
+    T, H, d, r = 9, 2, 12, 8
+    turns = w2v.rotary_turns(r)
+    off = torch.tensor([0, 4, 9]).cuda()
+    turned = dict(sent_off=off, halves=halves, gain=1.5)
+    g = torch.randint(-3, 4, (T, H, d)).cuda().to(ty)
+    back = w2v.rotate(g, turns, back=True, **turned).double().cpu()
+    for c in range(d):
+        one = torch.zeros(T, H, d, device="cuda", dtype=ty)
+        one[..., c] = 1
+        diff = (g.double() * w2v.rotate(one, turns, **turned).double()).sum(2).cpu()
+        # a pair's sine and cosine each off by 1.5 (2^-21 + half a step of the type), on both sides; |g| <= 3
+        u = {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}[ty]
+        assert float((diff - back[..., c]).abs().max()) <= 2 * 2 * 3 * 1.5 * (2.0 ** -21 + u)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, BF16])
+def test_in_place_strides_and_another_stream(ty):
+    T, H, G, d = 210, 6, 2, 38
+    off = torch.tensor([0, 100, 210]).cuda()
+    turns = w2v.rotary_turns(24)
+    for halves in (False, True):
+        packed = torch.randn(T, H + 2 * G, d, device="cuda").to(ty)
+        q, k, v = packed[:, :H], packed[:, H:H + G], packed[:, H + G:]
+        before = v.clone()
+        want = w2v.rotate(q.contiguous(), turns, k=k.contiguous(), sent_off=off, halves=halves)
+        odd = torch.empty(T * (H + 1) * d + 3, device="cuda", dtype=ty)[3:].view(T, H + 1, d)
+        got = w2v.rotate(q, turns, sent_off=off, halves=halves, out=odd[:, 1:])
+        assert torch.equal(got, want[0])
+        heads_first = torch.empty(G, T, d + 5, device="cuda", dtype=ty).transpose(0, 1)[..., :d]
+        w2v.rotate(q, turns, k=k, sent_off=off, halves=halves, k_out=heads_first)
+        assert torch.equal(heads_first, want[1])
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        w2v.rotate(q, turns, k=k, sent_off=off, halves=halves, out=q, k_out=k, stream=st)
+        st.synchronize()
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, before)
+    one = torch.randn(T, 4, d, device="cuda").to(ty)             # a single key head beside the queries, in place
+    q, k = one[:, :3], one[:, 3:]
+    want = w2v.rotate(q.contiguous(), turns, k=k.contiguous(), sent_off=off)
+    w2v.rotate(q, turns, k=k, sent_off=off, out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+@pytest.mark.gpu
+def test_words_that_no_text_has():
+    """Rows in front of the first text, behind the last, and none at all: what they hold stays."""
+    T, turns = 50, w2v.rotary_turns(10)
+    x = torch.randn(T, 2, 10, device="cuda")
+    for off in ([0, 30, 40], [7, 20, 50], [0, 0], [5, 5, 5]):
+        out = torch.full_like(x, 7.5)
+        w2v.rotate(x, turns, sent_off=torch.tensor(off).cuda(), out=out)
+        at = places(off, T)
+        assert torch.equal(out[at.cuda() < 0], torch.full_like(out[at.cuda() < 0], 7.5))
+        if (at >= 0).any():
+            want, bound = rotate_reference(x.cpu()[at >= 0], at[at >= 0], turns.cpu())
+            within(out[at.cuda() >= 0], want, bound)
+    empty = torch.empty(0, 2, 10, device="cuda")
+    assert w2v.rotate(empty, turns, sent_off=torch.tensor([0]).cuda()).shape == (0, 2, 10)
+
+
+@pytest.mark.gpu
+def test_offsets_that_break_their_rules():
+    """Offsets that fall, and lie far outside: nothing but the outputs is written, words that some text has are finite."""
+    T, turns = 100, w2v.rotary_turns(16)
+    x = torch.randn(T, 2, 16, device="cuda")
+    for off in ([50, 20, 100], [0, 2 ** 62, 5], [-5, 40, 2 ** 40], [99, 98, 97, 96]):
+        room = torch.full((T + 20, 2, 16), 3.0, device="cuda")
+        w2v.rotate(x, turns, sent_off=torch.tensor(off).cuda(), out=room[10:-10])
+        assert torch.isfinite(room).all() and (room[:10] == 3).all() and (room[-10:] == 3).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+def test_infinities_stay_in_their_pair(ty):
+    x = torch.randn(20, 2, 24, device="cuda").to(ty)
+    turns = w2v.rotary_turns(16)
+    off = torch.tensor([0, 20]).cuda()
+    for halves in (False, True):
+        want = w2v.rotate(x, turns, sent_off=off, halves=halves)
+        y = x.clone()
+        y[3, 1, 4], y[5, 0, 20] = float("nan"), float("-inf")
+        got = w2v.rotate(y, turns, sent_off=off, halves=halves)
+        pair = [4, 12] if halves else [4, 5]
+        assert torch.isnan(got[3, 1, pair]).all() and got[5, 0, 20] == float("-inf")
+        mask = torch.ones_like(x, dtype=torch.bool)
+        mask[3, 1, pair] = False
+        mask[5, 0, 20] = False
+        assert torch.equal(got[mask], want[mask])
+
+
+@pytest.mark.gpu
+def test_captured_and_replayed():
+    T, turns = 300, w2v.rotary_turns(32, scaling="parts", factor=4.0, trained=200)
+    q, k = torch.randn(T, 4, 40, device="cuda"), torch.randn(T, 2, 40, device="cuda")
+    off = torch.tensor([0, 20, 300]).cuda()
+    out, k_out = torch.empty_like(q), torch.empty_like(k)
+    call = lambda: w2v.rotate(q, turns, k=k, sent_off=off, halves=True, out=out, k_out=k_out)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        call()
+    torch.cuda.current_stream().wait_stream(st)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for n in range(4):
+        q.normal_()
+        k.normal_()
+        off.copy_(torch.tensor([0, 20 + 60 * n, 300]))
+        graph.replay()
+        got = out.clone(), k_out.clone()
+        want = w2v.rotate(q, turns, k=k, sent_off=off, halves=True)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.gpu
+def test_scores_depend_on_distances_alone():
+    """What it is for: words turned and attended, from the first place and from the 10^6th."""
+    T, turns = 60, w2v.rotary_turns(64)
+    q, k, v = [torch.randn(T, n, 64, device="cuda") for n in (4, 2, 2)]
+    off = torch.tensor([0, T]).cuda()
+    at = torch.arange(T, dtype=torch.int32, device="cuda")
+    out = [w2v.attend(*w2v.rotate(q, turns, k=k, positions=at + s), v, off, right=0)[0] for s in (0, 10 ** 6)]
+    # a turned pair is off by 2^-21 (|a| + |b|), so a row by 2^-20 of its norm; a score by that for q and for k and by its sum's
+    # roundings (128 * 2^-24); a weight by a factor of 1 + 2 E; both runs
+    E = (2 * 2.0 ** -20 + 128 * 2.0 ** -24) * float(q.norm(dim=2).max() * k.norm(dim=2).max()) / 8
+    assert float((out[0] - out[1]).abs().max()) <= 2 * (2 * E + 2e-5) * float(v.abs().max())
+    plain = w2v.rotate(q, turns, k=k, sent_off=off)
+    assert torch.equal(plain[0], w2v.rotate(q, turns, positions=at)) and torch.equal(plain[1], w2v.rotate(k, turns, positions=at))
+
+
+@pytest.mark.parametrize("r", [2, 4, 60, 126, 128])
+@pytest.mark.parametrize("base", [10000.0, 2.0, 5e5])
+def test_turns(r, base):
+    """Frequencies against their formulas; a double's own rounding times the power's condition is below 1e-13."""
+    tau = 2 * math.pi
+    plain = [base ** (-2 * c / r) for c in range(r // 2)]
+
+    def near(turns, want):
+        for a, b in zip(turns.tolist(), want):
+            a = a % 2 ** 64
+            assert abs(a - b / tau * 2.0 ** 64) <= 1e-13 * a + 1
+    near(w2v.rotary_turns(r, base, device="cpu"), plain)
+    near(w2v.rotary_turns(r, base, "linear", 8.0, device="cpu"), [f / 8 for f in plain])
+    near(w2v.rotary_turns(r, base, "base", 8.0, device="cpu"), [f * (8.0 ** (-2 * c / (r - 2)) if c else 1) for c, f in enumerate(plain)])
+    got = w2v.rotary_turns(r, base, "parts", 8.0, trained=4096, low=1.0, high=32.0, device="cpu")
+    want = []
+    for f in plain:
+        w = min(1.0, max(0.0, (4096 * f / tau - 1) / 31))
+        want.append(f * (w + (1 - w) / 8))
+    near(got, want)
+
+
+def test_turns_refused():
+    for kw in (dict(rotated=0), dict(rotated=3), dict(rotated=130), dict(rotated=2 ** 32 + 4), dict(base=1.0), dict(base=math.nan),
+               dict(base=math.inf), dict(scaling="linear", factor=0.5), dict(scaling="base", factor=math.nan),
+               dict(scaling="parts", factor=2.0), dict(scaling="parts", factor=2.0, trained=9, low=3.0, high=3.0),
+               dict(scaling="parts", factor=2.0, trained=9, low=-1.0), dict(scaling="parts", factor=2.0, trained=9, high=math.inf)):
+        with pytest.raises(w2v.W2VError):
+            w2v.rotary_turns(**{**dict(rotated=8), **kw}, device="cpu")
+    for kw in (dict(rotated=-2), dict(scaling="other"), dict(scaling="parts", trained=-1)):
+        with pytest.raises(ValueError):
+            w2v.rotary_turns(**{**dict(rotated=8), **kw}, device="cpu")
+    assert w2v.lib().w2v_rotary_turns(8, 1e4, 0, 1.0, 0, 0.0, 0.0, None) == -1
+
+
+def test_refusals():
+    L, p, r = w2v.lib(), 1 << 20, ctypes.byref
+    T, H, G, d = 10, 4, 2, 64
+
+    def call(type=0, width=d, rotated=64, gain=1.0, turns=p, x=None, heads=H, y=None, y_heads=G, off=p, n_sent=2, tokens=T, position=None,
+             x_out=None, y_out=None, rotary=True, no_y=False):
+        x, y = x or w2v.Heads(p, H * d, d), y or w2v.Heads(2 * p, G * d, d)
+        x_out, y_out = x_out or w2v.Heads(3 * p, H * d, d), y_out or w2v.Heads(4 * p, G * d, d)
+        return L.w2v_rotate(type, width, r(w2v.Rotary(rotated, 0, gain, turns)) if rotary else None, 0, r(x), heads, None if no_y else r(y),
+                            y_heads, off, n_sent, tokens, position, r(x_out), r(y_out), None)
+    assert call(tokens=0) == 0
+    for bad in (dict(type=3), dict(width=0), dict(width=129), dict(rotated=0), dict(rotated=3), dict(rotated=66), dict(gain=math.inf),
+                dict(gain=math.nan), dict(turns=p + 4), dict(heads=0), dict(heads=1025), dict(y_heads=0), dict(n_sent=0), dict(n_sent=2 ** 31),
+                dict(tokens=0x7FFFFFFF), dict(x=w2v.Heads(p + 2, H * d, d)), dict(x_out=w2v.Heads(3 * p, H * d, d - 1)),
+                dict(x_out=w2v.Heads(3 * p, H * d - 1, d)), dict(x=w2v.Heads(p, 1 << 41, d)), dict(x_out=w2v.Heads(p + 4, H * d, d)),
+                dict(x_out=w2v.Heads(p, H * d + 1, d)), dict(x_out=w2v.Heads(2 * p, H * d, d)), dict(y_out=w2v.Heads(3 * p, G * d, d)),
+                dict(y_out=w2v.Heads(p + 4 * H * d * (T - 1), G * d, d))):
+        assert call(**bad) == -2, bad
+    for bad in (dict(rotary=False), dict(turns=None), dict(off=None), dict(x=w2v.Heads(None, 1, 1)), dict(x_out=w2v.Heads(None, 1, 1)),
+                dict(y=w2v.Heads(None, 1, 1)), dict(y_out=w2v.Heads(None, 1, 1))):
+        assert call(**bad) == -1, bad
+    q, turns = torch.zeros(4, 2, 8), torch.zeros(4, dtype=torch.int64)
+    for bad in (dict(), dict(sent_off=torch.zeros(2, dtype=torch.int64)), dict(positions=torch.zeros(4, dtype=torch.int32)),
+                dict(k_out=q, positions=torch.zeros(4, dtype=torch.int32))):
+        with pytest.raises((TypeError, ValueError)):           # no words' places, host memory, a result of no input
+            w2v.rotate(q, turns, **bad)
