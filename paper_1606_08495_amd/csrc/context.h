@@ -72,11 +72,20 @@ struct StepArgs {
     // over pages: k.text and v.text lead from page to page, word j of a text is on page table[text table_stride + (j >> shift)] (row 0
     // for j < shared); room is the table's
     const uint32_t* table; uint64_t table_stride; uint32_t shift, n_pages, shared;
+    // the first `begin` words are the common prefix's blocks' (0: there are none), which leave `front` parts of each row before the others;
+    // parts: [batch][heads][front + splits][width + 2]
+    uint32_t begin, front;
 };
 struct StepSplits { uint32_t splits, per_split; };
 StepSplits step_splits(uint32_t batch, uint32_t kv_heads, uint32_t room, uint32_t left, uint32_t sinks);
 void launch_step(const StepArgs& a, uint32_t type, hipStream_t st);
+
+// Over pages.  What a call splits into, by sizes alone.
+uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t shared);
+struct PageSplits { uint32_t begin, front; StepSplits own; };
+PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t room, uint32_t shared, uint32_t left, uint32_t sinks);
 void launch_step_pages(const StepArgs& a, uint32_t type, hipStream_t st);
+void launch_prefix(const StepArgs& a, uint32_t type, hipStream_t st);
 
 // ---- positions that turn, and words on their way into pages ------------------------------------------
 struct Pages { void* p; uint64_t page, token, head; };

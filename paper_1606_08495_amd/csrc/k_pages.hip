@@ -3,6 +3,18 @@
 
 namespace w2v {
 
+// A prefix that several texts have is taken by its own blocks (k_prefix.hip); what is left of the texts as for a cache of one stride.
+PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t room, uint32_t shared, uint32_t left, uint32_t sinks) {
+    PageSplits p{};
+    if (shared && batch > 1) {
+        p.begin = shared;
+        p.front = prefix_splits(type, batch, heads, kv_heads, shared);
+    }
+    const uint32_t rest = room > p.begin ? room - p.begin : 1;
+    p.own = step_splits(batch, kv_heads, rest, left, sinks);
+    return p;
+}
+
 void launch_step_pages(const StepArgs& a, uint32_t type, hipStream_t st) {
     if (type == ELEM_F32) step_any<float, true>(a, st);
     else if (type == ELEM_F16) step_any<_Float16, true>(a, st);

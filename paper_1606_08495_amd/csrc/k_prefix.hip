@@ -1,0 +1,381 @@
+// Attention of the newest words of many texts over the words that all texts begin with, which lie in pages once.
+//
+// For a key head the queries of all texts and of the heads that share it are the rows of one product with the prefix's keys,
+// and their weights those of one with its values: the prefix is read once for 32 WR rows and not once for each.  Pages are looked up
+// and rows staged in LDS by tiles of 64 words, as in attention over texts: scores transposed (keys are rows, a query is a lane), the maximum
+// and sum of a query in its two lanes, weights fed to the second product from the registers they are in.  WR wavefronts have 32
+// queries each; with WK = 2 two of them share queries and take a half of every tile each.  A block has a part of the prefix and leaves
+// (maximum, sum, output) of its queries over it in the workspace, where the join finds them beside those of the texts' own words.
+//
+// Scores, maxima, sums and outputs are fp32; weights are rounded to the type of v for the second product, relative to the row's maximum
+// (fp16: lifted by a power of two, so that small ones keep their bits), and summed before that.
+#include <type_traits>
+
+#include "attend.h"
+#include "tiles.h"
+
+namespace w2v {
+namespace {
+
+constexpr int KEYS = 64;
+template <typename T> constexpr float RISE = std::is_same<T, _Float16>::value ? 2.f : 8.f;
+template <typename T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 13.f : 0.f;
+
+__device__ __forceinline__ uint32_t lanes_least(uint32_t x) {
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t y = (uint32_t)__shfl_xor((int)x, d, 64);
+        x = y < x ? y : x;
+    }
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// A query: its text, head, and the words it is shown, lo .. hi and those before `sinks`.
+struct Query { uint32_t text, head, lo, hi; };
+__device__ __forceinline__ Query query_of(const StepArgs& a, uint32_t kv_head, uint32_t row) {
+    Query q;
+    q.text = row / a.group;
+    q.head = kv_head * a.group + row % a.group;
+    const uint32_t n = a.n[q.text];
+    q.hi = n < a.room ? n : a.room;
+    q.lo = q.hi && q.hi - 1 > a.left ? q.hi - 1 - a.left : 0;
+    return q;
+}
+__device__ __forceinline__ bool shows(const StepArgs& a, const Query& q, uint32_t j) {
+    return j < q.hi && (j >= q.lo || j < a.sinks) && !(a.skip_self && j + 1 == q.hi) && (!a.keep || a.keep[(uint64_t)q.text * a.room + j]);
+}
+// Of the prefix, what a block's queries are shown between them: `sunk` first words, then those from lo on.
+struct Axis {
+    uint32_t sunk, lo, count;
+    __device__ __forceinline__ uint32_t word(uint32_t at) const { return at < sunk ? at : lo + at - sunk; }
+};
+__device__ __forceinline__ uint32_t prefix_page(const StepArgs& a, uint32_t j) { return a.table[j >> a.shift]; }
+
+__device__ __forceinline__ float query_bias(const StepArgs& a, const Query& q, uint32_t j) {
+    const uint32_t back = q.hi - 1 - j < a.span ? q.hi - 1 - j : a.span;
+    return scaled_bias(a.bias, a.buckets, a.n_buckets, a.span, q.head, -(int32_t)back);
+}
+
+// A query's part [from, to) of the axis, word by word and nothing touched that it is not shown: for rows whose result is not finite.
+template <typename T>
+__device__ void careful_row(const StepArgs& a, const Axis& x, uint32_t kv_head, const Query& q, uint32_t from, uint32_t to, uint32_t lane,
+                            float& m, float& total, float (&o)[2]) {
+    const T* row = head_row<T>(a.q, q.text, q.head);
+    const auto place = [&](const Cache& c, uint32_t j) {
+        return (const T*)c.p + (uint64_t)prefix_page(a, j) * c.text + (uint64_t)(j & ((1u << a.shift) - 1)) * c.token + (uint64_t)kv_head * c.head;
+    };
+    const auto score = [&](uint32_t j) {
+        const float s = dot_rows(row, place(a.k, j), a.width) * a.scale2;
+        return a.bias ? s + query_bias(a, q, j) : s;
+    };
+    const auto in = [&](uint32_t at) {
+        const uint32_t j = x.word(at < to ? at : to - 1);
+        return at < to && shows(a, q, j) && prefix_page(a, j) < a.n_pages;
+    };
+    m = -__builtin_inff();
+    bool nan = false;
+    for (uint32_t at = from + lane; at < to; at += WAVE) {
+        if (!in(at)) continue;
+        const float s = score(x.word(at));
+        nan |= s != s;
+        m = fmaxf(m, s);
+    }
+    m = wave_max(m);
+    o[0] = o[1] = total = 0.f;
+    if (__any(nan) || m == __builtin_inff()) {        // every weight is not a number, and so is every column
+        o[0] = o[1] = total = __builtin_nanf("");
+        m = -__builtin_inff();
+        return;
+    }
+    if (m == -__builtin_inff()) return;
+    for (uint32_t at0 = from; at0 < to; at0 += WAVE) {
+        const uint32_t at = at0 + lane, j = x.word(at < to ? at : to - 1);
+        const float p = in(at) ? exp2f(score(j) - m) : 0.f;
+        total += p;
+        for (uint64_t left = __ballot(p != 0.f); left; left &= left - 1) {
+            const int l = __builtin_ctzll(left);
+            const T* v = place(a.v, (uint32_t)__shfl((int)j, l, 64));
+            const float pl = __shfl(p, l, 64);
+            if (lane < a.width) o[0] = fmaf(pl, (float)v[lane], o[0]);
+            if (lane + WAVE < a.width) o[1] = fmaf(pl, (float)v[lane + WAVE], o[1]);
+        }
+    }
+    total = lanes_sum<64>(total);
+}
+
+template <typename T, int DB, int WR, int WK, bool BIAS>
+__global__ __launch_bounds__(64 * WR * WK, (sizeof(T) == 2 || DB <= 2 ? 2 : 1)) void prefix_kernel(const StepArgs a) {
+    typedef Tile<T, DB, KEYS> Tl;
+    constexpr int THREADS = 64 * WR * WK, PIECES = 2 / WK, KEEP = DB * 16 + 2;
+    __shared__ __align__(16) char tiles[2][Tl::BYTES];
+    __shared__ uint32_t bounds[2][WR];
+    extern __shared__ float dynamic[];                // bias: the buckets of distances 0 .. -span
+    static_assert(WK == 1 || WR * KEEP * 64 * 4 <= (int)sizeof(tiles), "room to join the halves");
+    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const uint32_t wr = wave % WR, wk = wave / WR;
+    // blocks of the same words and key head lie eight apart: they run on one die and share its cache
+    const uint32_t rows = a.batch * a.group, row_tiles = (rows + 32 * WR - 1) / (32 * WR), units = a.kv_heads * a.front;
+    const uint32_t unit = blockIdx.x / (8 * row_tiles) * 8 + blockIdx.x % 8, row_tile = blockIdx.x / 8 % row_tiles;
+    if (unit >= units) return;
+    const uint32_t kv_head = unit % a.kv_heads, split = unit / a.kv_heads;
+    const uint32_t first = row_tile * 32 * WR + wr * 32;
+    const bool some = first < rows, real = first + lane % 32 < rows;
+    const Query own = query_of(a, kv_head, real ? first + lane % 32 : rows - 1);
+
+    typename Frag<T>::vec q[2 * DB];
+#pragma unroll
+    for (int s = 0; s < 2 * DB; ++s) q[s] = load_operand<T, DB>(head_row<T>(a.q, own.text, own.head), s, h, a.width);
+    const uint32_t lo_least = lanes_least(own.lo), lo_most = ~lanes_least(~own.lo), hi_least = lanes_least(own.hi), hi_most = ~lanes_least(~own.hi);
+    if (lane == 0) {
+        bounds[0][wr] = lo_least;
+        bounds[1][wr] = hi_most;
+    }
+    uint32_t* const buckets = (uint32_t*)dynamic;
+    if constexpr (BIAS)
+        for (uint32_t c = threadIdx.x; c <= a.span; c += THREADS) buckets[c] = a.buckets[a.span - c];
+    __syncthreads();
+    Axis x;
+    uint32_t end = 0;
+    x.lo = ~0u;
+#pragma unroll
+    for (int w = 0; w < WR; ++w) {
+        x.lo = bounds[0][w] < x.lo ? bounds[0][w] : x.lo;
+        end = bounds[1][w] > end ? bounds[1][w] : end;
+    }
+    end = __builtin_amdgcn_readfirstlane(end < a.begin ? end : a.begin);
+    x.lo = __builtin_amdgcn_readfirstlane(x.lo < end ? x.lo : end);
+    x.sunk = x.lo < a.sinks ? x.lo : a.sinks;
+    x.count = x.sunk + end - x.lo;
+    const uint32_t per = ((x.count + KEYS - 1) / KEYS + a.front - 1) / a.front * KEYS;
+    const uint32_t from = split * per < x.count ? split * per : x.count, to = x.count - from < per ? x.count : from + per;
+    const uint32_t shift = x.lo - x.sunk;             // word of key n >= sunk: n + shift
+
+    Acc o[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) o[b] = Acc{};
+    float m = -__builtin_inff(), total = 0.f;
+    const float unit_scale = BIAS ? 1.f : a.scale2;   // of the scores once masked
+    float far = 0.f;
+    if constexpr (BIAS) far = scaled_bias(a.bias, a.buckets, a.n_buckets, a.span, own.head, -(int32_t)a.span);
+    const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
+
+    Transit<T, DB, KEYS, THREADS> k, v;
+    k.start(Heads{a.k.p, a.k.token, a.k.head}, kv_head, 0);
+    v.start(Heads{a.v.p, a.v.token, a.v.head}, kv_head, 0);
+    uint32_t page = 0;                                // of the key n0 + lane of the tile to be fetched next
+    const auto look = [&](uint32_t n0) __attribute__((always_inline)) { page = prefix_page(a, x.word(n0 + lane < to ? n0 + lane : to - 1)); };
+    const auto fetch = [&](uint32_t n0) __attribute__((always_inline)) {
+#pragma unroll
+        for (uint32_t n = 0; n < decltype(k)::PER; ++n) {
+            const uint32_t r = k.r0 + n * decltype(k)::RS, j = x.word(n0 + r < to ? n0 + r : to - 1);
+            const uint32_t there = (uint32_t)__shfl((int)page, (int)r, 64), g = there < a.n_pages ? there : 0, place = j & ((1u << a.shift) - 1);
+            k.at[n] = k.base + g * a.k.text + place * a.k.token;
+            v.at[n] = v.base + g * a.v.text + place * a.v.token;
+        }
+        k.load(a.width);
+        v.load(a.width);
+        return (uint64_t)__ballot(n0 + lane < to && page < a.n_pages);
+    };
+    uint64_t kept = 0, kept_next = 0;
+    if (from < to) {
+        look(from);
+        kept = fetch(from);
+        if (from + KEYS < to) look(from + KEYS);
+        k.store(tiles[0], a.width);
+        v.store(tiles[1], a.width, kept);
+    }
+    __syncthreads();
+    for (uint32_t n0 = from; n0 < to; n0 += KEYS) {
+        const bool more = n0 + KEYS < to;
+        if (more) {
+            kept_next = fetch(n0 + KEYS);
+            if (n0 + 2 * KEYS < to) look(n0 + 2 * KEYS);
+        }
+        const char *kt = tiles[0], *vt = tiles[1];
+#pragma unroll
+        for (int p0 = 0; p0 < PIECES; ++p0) {
+            const int p = WK == 2 ? (int)wk : p0;
+            const uint32_t n = n0 + p * 32, j0 = n + shift, kept32 = (uint32_t)(kept >> (p * 32));
+            const bool linear = n >= x.sunk;
+            // pieces that none of the wavefront's queries is shown
+            if (!some || n >= to || (linear && !(j0 < hi_most && (j0 + 32 > lo_least || j0 < a.sinks)))) continue;
+            Acc s = {};
+#pragma unroll
+            for (int c = 0; c < 2 * DB; ++c) mma(Tl::along(kt, at_along + p * (32 / 4 * Tl::STRIDE), 0, c), q[c], s);
+            const auto word = [&](int r) __attribute__((always_inline)) { return x.word(n + 4 * h + acc_row(r, 0)); };
+            if constexpr (BIAS) {
+                if (linear && hi_least > a.span && j0 + 31 <= hi_least - 1 - a.span) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, far);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t back = own.hi - 1 - word(r), b = buckets[back < a.span ? back : a.span];      // (words behind the text: masked)
+                        const float w = b < a.n_buckets ? a.bias[(uint64_t)own.head * a.n_buckets + b] : 0.f;
+                        s[r] = fmaf(s[r], a.scale2, fabsf(w) < __builtin_inff() ? fminf(fmaxf(w, -BIAS_HELD), BIAS_HELD) * LOG2E : w);
+                    }
+                }
+            }
+            const bool all = linear && j0 >= lo_most && j0 + 32 <= hi_least && kept32 == 0xFFFFFFFFu && !a.keep && !(a.skip_self && j0 + 32 >= hi_least);
+            if (!all)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const bool in = (kept32 >> acc_row(r, h) & 1) != 0 && shows(a, own, word(r));
+                    s[r] = in ? s[r] : -__builtin_inff();
+                }
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[r]);
+            most = halves_max(most) * unit_scale;
+            if (__any(most > m + RISE<T>)) {
+                const float up = fmaxf(m, most);
+                const float factor = up == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - up);
+                m = up;
+                total *= factor;
+#pragma unroll
+                for (int b = 0; b < DB; ++b) o[b] *= factor;
+            }
+            const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit_scale, -base));
+                sum += s[r];
+            }
+            total += sum;
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+                if constexpr (sizeof(T) == 4) {       // a piece's sum first, then the whole's: one long chain would lose bits
+                    Acc part = {};
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) mma(Tl::across(vt, at_across + p * (32 / 4 * Tl::STRIDE), 0, g, b), acc_operand<T>(s, g), part);
+                    o[b] += part;
+                } else {
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) mma(Tl::across(vt, at_across + p * (32 / 4 * Tl::STRIDE), 0, g, b), acc_operand<T>(s, g), o[b]);
+                }
+            }
+        }
+        if (more) {
+            __syncthreads();
+            kept = kept_next;
+            k.store(tiles[0], a.width);
+            v.store(tiles[1], a.width, kept);
+            __syncthreads();
+        }
+    }
+    if constexpr (WK == 2) {                          // the second half's sums through LDS to the first
+        float* const other = (float*)&tiles[0][0] + wr * KEEP * WAVE + lane;
+        __syncthreads();
+        if (wk) {
+            other[0] = m;
+            other[WAVE] = total;
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) other[(2 + b * 16 + r) * WAVE] = o[b][r];
+        }
+        __syncthreads();
+        if (wk) return;
+        const float m1 = other[0], up = fmaxf(m, m1);
+        const float f0 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - up);
+        const float f1 = m1 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m1 - up);
+        // (a maximum is -infinity where a half has seen nothing: its sums are zero; not a number stays where it is)
+        total = total * (total == 0.f ? 1.f : f0) + other[WAVE] * (other[WAVE] == 0.f ? 1.f : f1);
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[b][r] = o[b][r] * f0 + other[(2 + b * 16 + r) * WAVE] * f1;
+        m = up;
+    }
+    if (!some) return;
+    total = halves_sum(total);
+    float worst = total * 0.f;                        // not a number, if any sum is not finite
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) worst = fmaf(o[b][r], 0.f, worst);
+    worst = halves_sum(worst);
+    const bool redo = worst != 0.f;
+    const auto part_of = [&](uint32_t text, uint32_t head) __attribute__((always_inline)) {
+        return a.parts + (((uint64_t)text * a.heads + head) * (a.front + a.splits) + split) * (a.width + 2);
+    };
+    if (real && !redo) {
+        float* p = part_of(own.text, own.head);
+        if (h == 0) {
+            p[0] = total == 0.f ? -__builtin_inff() : m - LIFT<T>;
+            p[1] = total;
+        }
+        p += 2;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const uint32_t c = 32 * b + acc_row(r, h);
+                if (c + 4 <= a.width) *(Pack<float, 4>::mem*)(p + c) = Pack<float, 4>::vec{o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]};
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) if (c + e < a.width) p[c + e] = o[b][r + e];
+            }
+    }
+    // what a query is not shown must not show: rows that are not finite are formed from their words alone
+    uint64_t again = __ballot(redo && real && h == 0);
+    if (rare(again)) for (; again; again &= again - 1) {
+        const int l = __builtin_ctzll(again);
+        const Query one{(uint32_t)__shfl((int)own.text, l, 64), (uint32_t)__shfl((int)own.head, l, 64), (uint32_t)__shfl((int)own.lo, l, 64),
+                        (uint32_t)__shfl((int)own.hi, l, 64)};
+        float most, sum, row[2];
+        careful_row<T>(a, x, kv_head, one, from, to, lane, most, sum, row);
+        float* p = part_of(one.text, one.head);
+        if (lane == 0) {
+            p[0] = most;
+            p[1] = sum;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) p[2 + lane + c * WAVE] = row[c];
+    }
+}
+
+// Queries of a block: as many as there are for one key head, up to 128.  (32 bits: always four wavefronts, whose loads the
+// registers of two would not hold.)
+uint32_t prefix_rows(uint32_t type, uint32_t rows) { return rows <= 32 && type != ELEM_F32 ? 32 : rows <= 64 ? 64 : 128; }
+
+template <typename T, int DB, int WR, int WK> void prefix_bias(const StepArgs& a, hipStream_t st) {
+    const uint32_t rows = a.batch * a.group, row_tiles = (rows + 32 * WR - 1) / (32 * WR), units = a.kv_heads * a.front;
+    const uint32_t blocks = (units + 7) / 8 * 8 * row_tiles;
+    if (a.bias) prefix_kernel<T, DB, WR, WK, true><<<blocks, 64 * WR * WK, (a.span + 1) * sizeof(uint32_t), st>>>(a);
+    else prefix_kernel<T, DB, WR, WK, false><<<blocks, 64 * WR * WK, 0, st>>>(a);
+}
+template <typename T, int DB> void prefix_run(const StepArgs& a, uint32_t type, hipStream_t st) {
+    switch (prefix_rows(type, a.batch * a.group)) {
+        case 128: return prefix_bias<T, DB, 4, 1>(a, st);
+        case 64: return prefix_bias<T, DB, 2, 2>(a, st);
+    }
+    if constexpr (sizeof(T) == 2) prefix_bias<T, DB, 1, 2>(a, st);
+}
+template <typename T> void prefix_any(const StepArgs& a, uint32_t type, hipStream_t st) {
+    switch ((a.width + 31) / 32) {
+        case 1: return prefix_run<T, 1>(a, type, st);
+        case 2: return prefix_run<T, 2>(a, type, st);
+        case 3: return prefix_run<T, 3>(a, type, st);
+        default: return prefix_run<T, 4>(a, type, st);
+    }
+}
+
+}  // namespace
+
+// Blocks enough to fill the device twice over, of at least two tiles each.
+uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t shared) {
+    const uint32_t rows = batch * (heads / kv_heads), per_block = prefix_rows(type, rows);
+    const uint32_t blocks = (rows + per_block - 1) / per_block * kv_heads, most = (shared + 2 * KEYS - 1) / (2 * KEYS);
+    const uint32_t want = blocks < 512 ? (512 + blocks - 1) / blocks : 1;
+    return want < most ? want : most;
+}
+
+void launch_prefix(const StepArgs& a, uint32_t type, hipStream_t st) {
+    if (type == ELEM_F32) prefix_any<float>(a, type, st);
+    else if (type == ELEM_F16) prefix_any<_Float16>(a, type, st);
+    else prefix_any<__bf16>(a, type, st);
+}
+
+}  // namespace w2v

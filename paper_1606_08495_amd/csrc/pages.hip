@@ -265,8 +265,12 @@ int check_attend_pages(const w2v_attend_spec* s, uint32_t batch, const w2v_page_
 }
 
 // The workspace: partial results where a text's words are read by several blocks.
-size_t pages_bytes(const w2v_attend_spec* s, uint32_t batch, const StepSplits& p) {
-    return p.splits > 1 ? (size_t)batch * s->heads * p.splits * (s->width + 2) * sizeof(float) : 0;
+PageSplits pages_splits(const w2v_attend_spec* s, uint32_t batch, const w2v_page_table* t, uint32_t shared) {
+    return page_splits((uint32_t)s->type, batch, s->heads, s->kv_heads, t->slots * t->page_words, shared, s->left, s->sinks);
+}
+size_t pages_bytes(const w2v_attend_spec* s, uint32_t batch, const PageSplits& p) {
+    const uint32_t parts = p.front + p.own.splits;
+    return parts > 1 ? (size_t)batch * s->heads * parts * (s->width + 2) * sizeof(float) : 0;
 }
 
 }  // namespace
@@ -274,7 +278,7 @@ size_t pages_bytes(const w2v_attend_spec* s, uint32_t batch, const StepSplits& p
 extern "C" size_t w2v_attend_pages_workspace(const w2v_attend_spec* spec, uint32_t batch, const w2v_page_table* table,
                                              uint32_t shared) {
     if (batch == 0 || check_attend_pages(spec, batch, table, shared)) return 0;
-    return pages_bytes(spec, batch, step_splits(batch, spec->kv_heads, table->slots * table->page_words, spec->left, spec->sinks));
+    return pages_bytes(spec, batch, pages_splits(spec, batch, table, shared));
 }
 
 extern "C" int w2v_attend_pages(const w2v_attend_spec* spec, const w2v_heads* q, const w2v_pages* k, const w2v_pages* v,
@@ -294,8 +298,7 @@ extern "C" int w2v_attend_pages(const w2v_attend_spec* spec, const w2v_heads* q,
         return fail(W2V_ERR_ARG, "out overlaps q");
     if (touch(to, lattice_of(k, spec, table)) || touch(to, lattice_of(v, spec, table)))
         return fail(W2V_ERR_ARG, "out overlaps a pool");
-    const uint32_t room = table->slots * table->page_words;
-    const StepSplits p = step_splits(batch, spec->kv_heads, room, spec->left, spec->sinks);
+    const PageSplits p = pages_splits(spec, batch, table, shared);
     const size_t need = pages_bytes(spec, batch, p);
     if (need) {
         if (!workspace) return fail(W2V_ERR_NULL, "workspace is NULL");
@@ -307,15 +310,17 @@ extern "C" int w2v_attend_pages(const w2v_attend_spec* spec, const w2v_heads* q,
     a.q = heads_of(q); a.o = heads_out(out);
     a.k = Cache{k->p, k->page_stride, k->token_stride, k->head_stride};
     a.v = Cache{v->p, v->page_stride, v->token_stride, v->head_stride};
-    a.n = n; a.batch = batch; a.room = room;
+    a.n = n; a.batch = batch; a.room = table->slots * table->page_words;
     a.heads = spec->heads; a.kv_heads = spec->kv_heads; a.group = spec->heads / spec->kv_heads; a.width = spec->width;
     a.left = spec->left; a.sinks = spec->sinks; a.skip_self = spec->skip_self != 0;
     a.scale2 = spec->scale * 1.4426950408889634f;
     a.keep = keep;
     a.bias = spec->bias_dev; a.buckets = spec->bucket_dev; a.n_buckets = spec->n_buckets; a.span = spec->span;
-    a.splits = p.splits; a.per_split = p.per_split; a.parts = (float*)workspace;
+    a.splits = p.own.splits; a.per_split = p.own.per_split; a.parts = (float*)workspace;
+    a.begin = p.begin; a.front = p.front;
     a.table = table->page_dev; a.table_stride = table->stride; a.shift = shift_of(table); a.n_pages = table->n_pages;
     a.shared = shared;
+    if (p.front) launch_prefix(a, (uint32_t)spec->type, (hipStream_t)stream);
     launch_step_pages(a, (uint32_t)spec->type, (hipStream_t)stream);
     return launched();
 }

@@ -17,16 +17,26 @@ namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / (int)WAVE, AHEAD = 4;
 
-// The keys of a text on one axis: `sunk` first words, then the window up to the new word.
-struct Keys { uint32_t sunk, lo, count, last; };
-__device__ inline Keys step_keys(const StepArgs& a, uint32_t text) {
+// The keys of a text on one axis: `sunk` first words, then the window up to the new word.  Over pages those from `begin` on.
+struct Keys {
+    uint32_t first, sunk, lo, count, last;
+    __device__ __forceinline__ uint32_t word(uint32_t at) const { return at < sunk ? first + at : lo + at - sunk; }
+};
+template <bool PAGED> __device__ inline Keys step_keys(const StepArgs& a, uint32_t text) {
     const uint32_t n = a.n[text] < a.room ? a.n[text] : a.room;
-    Keys k{0, 0, 0, 0};
+    Keys k{0, 0, 0, 0, 0};
     if (n == 0) return k;
     k.last = n - 1;
     k.lo = k.last > a.left ? k.last - a.left : 0;
     k.sunk = k.lo < a.sinks ? k.lo : a.sinks;
-    k.count = k.sunk + n - k.lo;
+    if constexpr (PAGED) {
+        k.first = k.sunk < a.begin ? k.sunk : a.begin;
+        k.sunk -= k.first;
+        k.lo = k.lo < a.begin ? a.begin : k.lo;
+        k.count = k.sunk + (n > k.lo ? n - k.lo : 0);
+    } else {
+        k.count = k.sunk + n - k.lo;
+    }
     return k;
 }
 
@@ -48,9 +58,10 @@ __global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(c
     const uint32_t kv_head = at % a.kv_heads, text = at / a.kv_heads;
     const uint32_t head0 = kv_head * a.group + round * HEADS;
     const uint32_t heads = a.group - round * HEADS < HEADS ? a.group - round * HEADS : HEADS;
-    const Keys keys = step_keys(a, text);
+    const Keys keys = step_keys<PAGED>(a, text);
     const uint32_t from = split * a.per_split, to = keys.count < from + a.per_split ? keys.count : from + a.per_split;
-    if (from >= to && !(split == 0 && a.splits == 1)) return;
+    const bool whole = a.splits == 1 && !(PAGED && a.front);
+    if (from >= to && !(split == 0 && whole)) return;
 
     if (a.bias) {
         for (uint32_t c = threadIdx.x; c < (a.span + 1) * heads; c += THREADS)
@@ -81,7 +92,7 @@ __global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(c
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const uint32_t n = n0 + u * GROUPS + group, at = n < to ? n : to - 1;
-            const uint32_t word = at < keys.sunk ? at : keys.lo + at - keys.sunk;
+            const uint32_t word = keys.word(at);
             next_page[u] = a.table[(word < a.shared ? 0 : (uint64_t)text * a.table_stride) + (word >> a.shift)];
         }
     };
@@ -89,7 +100,7 @@ __global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(c
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const uint32_t n = n0 + u * GROUPS + group, at = n < to ? n : to - 1;
-            j[u] = at < keys.sunk ? at : keys.lo + at - keys.sunk;
+            j[u] = PAGED ? keys.word(at) : at < keys.sunk ? at : keys.lo + at - keys.sunk;
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
@@ -216,10 +227,11 @@ __global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(c
             o = fmaf(f, joined[w][g][2 + col], o);
         }
         const uint32_t head = head0 + g;
-        if (a.splits == 1) {
+        if (whole) {
             head_row<T>(a.o, text, head)[col] = (T)(sum == 0.f ? 0.f : o / sum);
         } else {
-            float* p = a.parts + (((uint64_t)text * a.heads + head) * a.splits + split) * (a.width + 2);
+            const uint64_t row = (uint64_t)text * a.heads + head;
+            float* p = a.parts + (PAGED ? row * (a.front + a.splits) + a.front + split : row * a.splits + split) * (a.width + 2);
             p[2 + col] = o;
             if (col == 0) { p[0] = most; p[1] = sum; }
         }
@@ -227,15 +239,15 @@ __global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(c
 }
 
 // Joins the splits of a text's cache: one wavefront per text and head.
-template <typename T> __global__ __launch_bounds__(THREADS) void step_join_kernel(const StepArgs a) {
+template <typename T, bool PAGED> __global__ __launch_bounds__(THREADS) void step_join_kernel(const StepArgs a) {
     const uint32_t lane = threadIdx.x % WAVE;
     const uint64_t at = (uint64_t)blockIdx.x * WAVES + threadIdx.x / WAVE;
     if (at >= (uint64_t)a.batch * a.heads) return;
     const uint32_t text = (uint32_t)(at / a.heads), head = (uint32_t)(at % a.heads);
-    const Keys keys = step_keys(a, text);
-    const uint32_t count = (keys.count + a.per_split - 1) / a.per_split;
+    const Keys keys = step_keys<PAGED>(a, text);
+    const uint32_t count = (keys.count + a.per_split - 1) / a.per_split + (PAGED ? a.front : 0);
     const uint32_t row = a.width + 2;
-    const float* p = a.parts + at * a.splits * row;
+    const float* p = a.parts + at * (PAGED ? a.front + a.splits : a.splits) * row;
     float most = -__builtin_inff(), sum = 0.f, o[2] = {0.f, 0.f};
     for (uint32_t s = lane; s < count; s += WAVE) most = fmaxf(most, p[(uint64_t)s * row]);
     most = wave_max(most);
@@ -248,6 +260,7 @@ template <typename T> __global__ __launch_bounds__(THREADS) void step_join_kerne
 #pragma unroll 8
         for (uint32_t l = 0; l < here; ++l) {
             const float fl = __shfl(f, (int)l, 64);
+            if (PAGED && fl == 0.f) continue;         // a part of no weight, whatever it holds
             const float* x = p + (uint64_t)(s0 + l) * row + 2;
 #pragma unroll
             for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) o[c] = fmaf(fl, x[lane + c * WAVE], o[c]);
@@ -275,7 +288,7 @@ template <typename T, bool PAGED> void step_any(const StepArgs& a, hipStream_t s
     if (chunks <= 8) step_heads<T, 8, PAGED>(a, st);
     else if (chunks <= 16) step_heads<T, 16, PAGED>(a, st);
     else if constexpr (sizeof(T) == 4) step_heads<T, 32, PAGED>(a, st);
-    if (a.splits > 1) step_join_kernel<T><<<(uint32_t)(((uint64_t)a.batch * a.heads + WAVES - 1) / WAVES), THREADS, 0, st>>>(a);
+    if (a.splits > 1 || (PAGED && a.front)) step_join_kernel<T, PAGED><<<(uint32_t)(((uint64_t)a.batch * a.heads + WAVES - 1) / WAVES), THREADS, 0, st>>>(a);
 }
 
 }  // namespace
