@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libw2v_shard.so")
 
 HIP_SOURCES = ["api.hip", "k_gather.hip", "k_sort.hip", "k_adjust.hip", "k_pairs.hip", "k_cbow.hip", "k_topk.hip",
                "context.hip", "k_norm.hip", "k_attend.hip", "k_attend_back.hip", "k_step.hip", "pages.hip",
-               "k_rotate.hip", "k_pages.hip", "k_prefix.hip"]
+               "k_rotate.hip", "k_pages.hip", "k_page_tiles.hip"]
 CPP_SOURCES = ["tables.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

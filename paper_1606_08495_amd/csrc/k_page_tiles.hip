@@ -1,0 +1,479 @@
+// Attention of the newest words of many texts over the words that all texts begin with, which lie in pages once.
+//
+// For a key head the queries of all texts and of the heads that share it are the rows of one product with the prefix's keys,
+// and their weights those of one with its values: the prefix is read once for 32 WR rows and not once for each.  Pages are looked up
+// and rows staged in LDS by tiles of 64 words, as in attention over texts: scores transposed (keys are rows, a query is a lane), the maximum
+// and sum of a query in its two lanes, weights fed to the second product from the registers they are in.  WR wavefronts have 32
+// queries each; with WK = 2 two of them share queries and take a half of every tile each.  A block has a part of the prefix and leaves
+// (maximum, sum, output) of its queries over it in the workspace, where the join finds them beside those of the texts' own words.
+//
+// Scores, maxima, sums and outputs are fp32; weights are rounded to the type of v for the second product, relative to the row's maximum
+// (fp16: lifted by a power of two, so that small ones keep their bits), and summed before that.
+#include <type_traits>
+
+#include "attend.h"
+#include "tiles.h"
+
+namespace w2v {
+namespace {
+
+template <typename T> constexpr float RISE = std::is_same<T, _Float16>::value ? 2.f : 8.f;
+template <typename T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 13.f : 0.f;
+
+__device__ __forceinline__ uint32_t lanes_least(uint32_t x) {
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t y = (uint32_t)__shfl_xor((int)x, d, 64);
+        x = y < x ? y : x;
+    }
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// A query: its text, head, and the words it is shown, lo .. hi and those before `sinks`.
+struct Query { uint32_t text, head, lo, hi; };
+__device__ __forceinline__ Query query_of(const StepArgs& a, uint32_t text, uint32_t head) {
+    Query q;
+    q.text = text;
+    q.head = head;
+    const uint32_t n = a.n[text];
+    q.hi = n < a.room ? n : a.room;
+    q.lo = q.hi && q.hi - 1 > a.left ? q.hi - 1 - a.left : 0;
+    return q;
+}
+__device__ __forceinline__ bool shows(const StepArgs& a, const Query& q, uint32_t j) {
+    return j < q.hi && (j >= q.lo || j < a.sinks) && !(a.skip_self && j + 1 == q.hi) && (!a.keep || a.keep[(uint64_t)q.text * a.room + j]);
+}
+// What a block's queries are shown between them, of the prefix or of their text's own words: `sunk` words from `first` on, then those
+// from lo on.  Words lie in the pages of row `pages` of the table (those before `shared` in row 0's).
+struct Axis {
+    uint32_t first, sunk, lo, count, shared;
+    const uint32_t *row0, *pages;
+    __device__ __forceinline__ uint32_t word(uint32_t at) const { return at < sunk ? first + at : lo + at - sunk; }
+    __device__ __forceinline__ uint32_t page(uint32_t j, uint32_t shift) const { return (j < shared ? row0 : pages)[j >> shift]; }
+};
+
+__device__ __forceinline__ float query_bias(const StepArgs& a, const Query& q, uint32_t j) {
+    const uint32_t back = q.hi - 1 - j < a.span ? q.hi - 1 - j : a.span;
+    return scaled_bias(a.bias, a.buckets, a.n_buckets, a.span, q.head, -(int32_t)back);
+}
+
+// A query's part [from, to) of the axis, word by word and nothing touched that it is not shown: for rows whose result is not finite.
+template <typename T>
+__device__ void careful_row(const StepArgs& a, const Axis& x, uint32_t kv_head, const Query& q, uint32_t from, uint32_t to, uint32_t lane,
+                            float& m, float& total, float (&o)[2]) {
+    const T* row = head_row<T>(a.q, q.text, q.head);
+    const auto place = [&](const Cache& c, uint32_t j) {
+        return (const T*)c.p + (uint64_t)x.page(j, a.shift) * c.text + (uint64_t)(j & ((1u << a.shift) - 1)) * c.token + (uint64_t)kv_head * c.head;
+    };
+    const auto score = [&](uint32_t j) {
+        const float s = dot_rows(row, place(a.k, j), a.width) * a.scale2;
+        return a.bias ? s + query_bias(a, q, j) : s;
+    };
+    const auto in = [&](uint32_t at) {
+        const uint32_t j = x.word(at < to ? at : to - 1);
+        return at < to && shows(a, q, j) && x.page(j, a.shift) < a.n_pages;
+    };
+    m = -__builtin_inff();
+    bool nan = false;
+    for (uint32_t at = from + lane; at < to; at += WAVE) {
+        if (!in(at)) continue;
+        const float s = score(x.word(at));
+        nan |= s != s;
+        m = fmaxf(m, s);
+    }
+    m = wave_max(m);
+    o[0] = o[1] = total = 0.f;
+    if (__any(nan) || m == __builtin_inff()) {        // every weight is not a number, and so is every column
+        o[0] = o[1] = total = __builtin_nanf("");
+        m = -__builtin_inff();
+        return;
+    }
+    if (m == -__builtin_inff()) return;
+    for (uint32_t at0 = from; at0 < to; at0 += WAVE) {
+        const uint32_t at = at0 + lane, j = x.word(at < to ? at : to - 1);
+        const float p = in(at) ? exp2f(score(j) - m) : 0.f;
+        total += p;
+        for (uint64_t left = __ballot(p != 0.f); left; left &= left - 1) {
+            const int l = __builtin_ctzll(left);
+            const T* v = place(a.v, (uint32_t)__shfl((int)j, l, 64));
+            const float pl = __shfl(p, l, 64);
+            if (lane < a.width) o[0] = fmaf(pl, (float)v[lane], o[0]);
+            if (lane + WAVE < a.width) o[1] = fmaf(pl, (float)v[lane + WAVE], o[1]);
+        }
+    }
+    total = lanes_sum<64>(total);
+}
+
+// The keys of a tile: with four wavefronts on it 128, a piece of 32 for each.
+template <int WK> constexpr int KEYS = WK == 4 ? 128 : 64;
+template <typename T, int DB, int WK> constexpr int TILES_BYTES = 2 * Tile<T, DB, KEYS<WK>>::BYTES;
+
+// One block, of the prefix (PREFIX) or of one text's own words.
+template <typename T, int DB, int WR, int WK, bool BIAS, bool PREFIX>
+__device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block, char* tiles, uint32_t* bounds, uint32_t* buckets) {
+    constexpr int K = KEYS<WK>, THREADS = 64 * WR * WK, PIECES = K / 32 / WK, KEEP = DB * 16 + 2, MASKS = K / 64;
+    typedef Tile<T, DB, K> Tl;
+    static_assert(WK == 1 || WR * KEEP * 64 * 4 <= 2 * Tl::BYTES, "room to join the parts");
+    const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const uint32_t wr = wave % WR, wk = wave / WR;
+    uint32_t kv_head, split, row_tile, text = 0;
+    const uint32_t rows = PREFIX ? a.batch * a.group : a.group, row_tiles = (rows + 32 * WR - 1) / (32 * WR);
+    if constexpr (PREFIX) {
+        // blocks of the same words and key head lie eight apart: they run on one die and share its cache
+        const uint32_t unit = block / (8 * row_tiles) * 8 + block % 8;
+        row_tile = block / 8 % row_tiles;
+        if (unit >= a.kv_heads * a.front) return;
+        kv_head = unit % a.kv_heads;
+        split = unit / a.kv_heads;
+    } else {
+        split = block % a.splits; block /= a.splits;
+        row_tile = block % row_tiles; block /= row_tiles;
+        kv_head = block % a.kv_heads;
+        text = block / a.kv_heads;
+    }
+    const bool whole = !PREFIX && a.front + a.splits == 1;
+    const uint32_t first = row_tile * 32 * WR + wr * 32;
+    const bool some = first < rows, real = first + lane % 32 < rows;
+    const uint32_t row = real ? first + lane % 32 : rows - 1;
+    const Query own = PREFIX ? query_of(a, row / a.group, kv_head * a.group + row % a.group) : query_of(a, text, kv_head * a.group + row);
+    Axis x;
+    x.row0 = a.table;
+    x.shared = PREFIX ? ~0u : a.shared;
+    x.pages = a.table + (uint64_t)text * a.table_stride;
+    uint32_t from, to;
+    if constexpr (!PREFIX) {
+        x.sunk = own.lo < a.sinks ? own.lo : a.sinks;
+        x.first = x.sunk < a.begin ? x.sunk : a.begin;
+        x.sunk -= x.first;
+        x.lo = own.lo < a.begin ? a.begin : own.lo;
+        x.count = x.sunk + (own.hi > x.lo ? own.hi - x.lo : 0);
+        x.first = __builtin_amdgcn_readfirstlane(x.first);
+        x.sunk = __builtin_amdgcn_readfirstlane(x.sunk);
+        x.lo = __builtin_amdgcn_readfirstlane(x.lo);
+        x.count = __builtin_amdgcn_readfirstlane(x.count);
+        from = split * a.per_split;
+        to = x.count < from + a.per_split ? x.count : from + a.per_split;
+        if (from >= to && !whole) return;
+    }
+
+    typename Frag<T>::vec q[2 * DB];
+#pragma unroll
+    for (int s = 0; s < 2 * DB; ++s) q[s] = load_operand<T, DB>(head_row<T>(a.q, own.text, own.head), s, h, a.width);
+    uint32_t lo_least = 0, lo_most = 0, hi_least = own.hi, hi_most = own.hi;
+    if constexpr (BIAS)
+        for (uint32_t c = threadIdx.x; c <= a.span; c += THREADS) buckets[c] = a.buckets[a.span - c];
+    if constexpr (PREFIX) {
+        lo_least = lanes_least(own.lo), lo_most = ~lanes_least(~own.lo), hi_least = lanes_least(own.hi), hi_most = ~lanes_least(~own.hi);
+        if (lane == 0) {
+            bounds[wr] = lo_least;
+            bounds[WR + wr] = hi_most;
+        }
+        __syncthreads();
+        uint32_t end = 0;
+        x.lo = ~0u;
+#pragma unroll
+        for (int w = 0; w < WR; ++w) {
+            x.lo = bounds[w] < x.lo ? bounds[w] : x.lo;
+            end = bounds[WR + w] > end ? bounds[WR + w] : end;
+        }
+        end = __builtin_amdgcn_readfirstlane(end < a.begin ? end : a.begin);
+        x.first = 0;
+        x.lo = __builtin_amdgcn_readfirstlane(x.lo < end ? x.lo : end);
+        x.sunk = x.lo < a.sinks ? x.lo : a.sinks;
+        x.count = x.sunk + end - x.lo;
+        const uint32_t per = ((x.count + K - 1) / K + a.front - 1) / a.front * K;
+        from = split * per < x.count ? split * per : x.count;
+        to = x.count - from < per ? x.count : from + per;
+    }
+    const uint32_t shift = x.lo - x.sunk;             // word of key n >= sunk: n + shift
+
+    Acc o[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b) o[b] = Acc{};
+    float m = -__builtin_inff(), total = 0.f;
+    const float unit_scale = BIAS ? 1.f : a.scale2;   // of the scores once masked
+    float far = 0.f;
+    if constexpr (BIAS) far = scaled_bias(a.bias, a.buckets, a.n_buckets, a.span, own.head, -(int32_t)a.span);
+    const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
+
+
+    Transit<T, DB, K, THREADS> k, v;
+    k.start(Heads{a.k.p, a.k.token, a.k.head}, kv_head, 0);
+    v.start(Heads{a.v.p, a.v.token, a.v.head}, kv_head, 0);
+    uint32_t page[MASKS];                             // of keys n0 + lane (and 64 on) of the tile to be fetched next
+    bool in[MASKS];                                   // whether they are there to be shown
+    const auto look = [&](uint32_t n0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < MASKS; ++i) {
+            const uint32_t at = n0 + i * 64 + lane, j = x.word(at < to ? at : to - 1);
+            page[i] = x.page(j, a.shift);
+            in[i] = at < to;
+            if (!PREFIX) in[i] &= !(a.skip_self && j + 1 == own.hi) && (!a.keep || a.keep[(uint64_t)text * a.room + j]);
+        }
+    };
+    struct Kept { uint64_t mask[MASKS]; };
+    const auto fetch = [&](uint32_t n0) __attribute__((always_inline)) {
+#pragma unroll
+        for (uint32_t n = 0; n < decltype(k)::PER; ++n) {
+            const uint32_t r = k.r0 + n * decltype(k)::RS, j = x.word(n0 + r < to ? n0 + r : to - 1);
+            const uint32_t there = (uint32_t)__shfl((int)page[n * decltype(k)::RS / 64], (int)(r % 64), 64);
+            const uint32_t g = there < a.n_pages ? there : 0, place = j & ((1u << a.shift) - 1);
+            k.at[n] = k.base + g * a.k.text + place * a.k.token;
+            v.at[n] = v.base + g * a.v.text + place * a.v.token;
+        }
+        k.load(a.width);
+        v.load(a.width);
+        Kept kept;
+#pragma unroll
+        for (int i = 0; i < MASKS; ++i) kept.mask[i] = __ballot(in[i] && page[i] < a.n_pages);
+        return kept;
+    };
+    Kept kept, kept_next;
+    char *const k_tile = tiles, *const v_tile = tiles + Tl::BYTES;
+    const auto store = [&]() __attribute__((always_inline)) {
+        k.store(k_tile, a.width);
+        uint64_t every = ~0ull;
+#pragma unroll
+        for (int i = 0; i < MASKS; ++i) every &= kept.mask[i];
+        if (!rare(~every)) v.store(v_tile, a.width);
+        else v.store_rows(v_tile, a.width, [&](uint32_t r0, uint32_t r) __attribute__((always_inline)) { return !(kept.mask[r / 64] >> (r % 64 + r0) & 1); });
+    };
+    if (from < to) {
+        look(from);
+        kept = fetch(from);
+        if (from + K < to) look(from + K);
+        store();
+    }
+    __syncthreads();
+    for (uint32_t n0 = from; n0 < to; n0 += K) {
+        const bool more = n0 + K < to;
+        if (more) {
+            kept_next = fetch(n0 + K);
+            if (n0 + 2 * K < to) look(n0 + 2 * K);
+        }
+#pragma unroll
+        for (int p0 = 0; p0 < PIECES; ++p0) {
+            const int p = WK > 1 ? (int)wk : p0;
+            uint64_t mask = kept.mask[0];
+            if constexpr (MASKS > 1) mask = wk < 2 ? mask : kept.mask[1];
+            const uint32_t n = n0 + p * 32, j0 = n + shift, kept32 = (uint32_t)(mask >> (p % 2 * 32));
+            const bool linear = n >= x.sunk;
+            // pieces that none of the wavefront's queries is shown
+            if (!some || n >= to || (PREFIX && linear && !(j0 < hi_most && (j0 + 32 > lo_least || j0 < a.sinks)))) continue;
+            Acc s = {};
+#pragma unroll
+            for (int c = 0; c < 2 * DB; ++c) mma(Tl::along(k_tile, at_along + p * (32 / 4 * Tl::STRIDE), 0, c), q[c], s);
+            const auto word = [&](int r) __attribute__((always_inline)) { return x.word(n + 4 * h + acc_row(r, 0)); };
+            if constexpr (BIAS) {
+                if (linear && hi_least > a.span && j0 + 31 <= hi_least - 1 - a.span) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, far);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t back = own.hi - 1 - word(r), b = buckets[back < a.span ? back : a.span];      // (words behind the text: masked)
+                        const float w = b < a.n_buckets ? a.bias[(uint64_t)own.head * a.n_buckets + b] : 0.f;
+                        s[r] = fmaf(s[r], a.scale2, fabsf(w) < __builtin_inff() ? fminf(fmaxf(w, -BIAS_HELD), BIAS_HELD) * LOG2E : w);
+                    }
+                }
+            }
+            bool all = kept32 == 0xFFFFFFFFu;
+            if (PREFIX) all &= linear && j0 >= lo_most && j0 + 32 <= hi_least && !a.keep && !(a.skip_self && j0 + 32 >= hi_least);
+            if (!all)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const bool in = (kept32 >> acc_row(r, h) & 1) != 0 && (!PREFIX || shows(a, own, word(r)));
+                    s[r] = in ? s[r] : -__builtin_inff();
+                }
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[r]);
+            most = halves_max(most) * unit_scale;
+            if (__any(most > m + RISE<T>)) {
+                const float up = fmaxf(m, most);
+                const float factor = up == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - up);
+                m = up;
+                total *= factor;
+#pragma unroll
+                for (int b = 0; b < DB; ++b) o[b] *= factor;
+            }
+            const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit_scale, -base));
+                sum += s[r];
+            }
+            total += sum;
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+                if constexpr (sizeof(T) == 4) {       // a piece's sum first, then the whole's: one long chain would lose bits
+                    Acc part = {};
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) mma(Tl::across(v_tile, at_across + p * (32 / 4 * Tl::STRIDE), 0, g, b), acc_operand<T>(s, g), part);
+                    o[b] += part;
+                } else {
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) mma(Tl::across(v_tile, at_across + p * (32 / 4 * Tl::STRIDE), 0, g, b), acc_operand<T>(s, g), o[b]);
+                }
+            }
+        }
+        if (more) {
+            __syncthreads();
+            kept = kept_next;
+            store();
+            __syncthreads();
+        }
+    }
+    if constexpr (WK > 1) {                           // the other parts' sums through LDS to the first, one part after the other
+        float* const other = (float*)tiles + wr * KEEP * WAVE + lane;
+#pragma unroll
+        for (int part = 1; part < WK; ++part) {
+            __syncthreads();
+            if ((int)wk == part) {
+                other[0] = m;
+                other[WAVE] = total;
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) other[(2 + b * 16 + r) * WAVE] = o[b][r];
+            }
+            __syncthreads();
+            if (wk == 0) {
+                const float m1 = other[0], up = fmaxf(m, m1);
+                const float f0 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - up);
+                const float f1 = m1 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m1 - up);
+                // (a maximum is -infinity where a part has seen nothing: its sums are zero; not a number stays where it is)
+                total = total * (total == 0.f ? 1.f : f0) + other[WAVE] * (other[WAVE] == 0.f ? 1.f : f1);
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[b][r] = o[b][r] * f0 + other[(2 + b * 16 + r) * WAVE] * f1;
+                m = up;
+            }
+        }
+        if (wk) return;
+    }
+    if (!some) return;
+    total = halves_sum(total);
+    float worst = total * 0.f;                        // not a number, if any sum is not finite
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) worst = fmaf(o[b][r], 0.f, worst);
+    worst = halves_sum(worst);
+    const bool redo = worst != 0.f;
+    const uint32_t place = PREFIX ? split : a.front + split;
+    const auto part_of = [&](uint32_t text, uint32_t head) __attribute__((always_inline)) {
+        return a.parts + (((uint64_t)text * a.heads + head) * (a.front + a.splits) + place) * (a.width + 2);
+    };
+    if (real && !redo) {
+        const float inv = !whole ? 1.f : total == 0.f ? 0.f : 1.f / total;
+        float* p = whole ? nullptr : part_of(own.text, own.head);
+        T* out = head_row<T>(a.o, own.text, own.head);
+        if (!whole && h == 0) {
+            p[0] = total == 0.f ? -__builtin_inff() : m - LIFT<T>;
+            p[1] = total;
+        }
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const uint32_t c = 32 * b + acc_row(r, h);
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) if (c + e < a.width) out[c + e] = (T)(o[b][r + e] * inv);
+                } else if (c + 4 <= a.width) {
+                    *(Pack<float, 4>::mem*)(p + 2 + c) = Pack<float, 4>::vec{o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) if (c + e < a.width) p[2 + c + e] = o[b][r + e];
+                }
+            }
+    }
+    // what a query is not shown must not show: rows that are not finite are formed from their words alone
+    uint64_t again = __ballot(redo && real && h == 0);
+    if (rare(again)) for (; again; again &= again - 1) {
+        const int l = __builtin_ctzll(again);
+        const Query one{(uint32_t)__shfl((int)own.text, l, 64), (uint32_t)__shfl((int)own.head, l, 64), (uint32_t)__shfl((int)own.lo, l, 64),
+                        (uint32_t)__shfl((int)own.hi, l, 64)};
+        float most, sum, row[2];
+        careful_row<T>(a, x, kv_head, one, from, to, lane, most, sum, row);
+        if (whole) {
+            T* out = head_row<T>(a.o, one.text, one.head);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) out[lane + c * WAVE] = (T)(sum == 0.f ? 0.f : row[c] / sum);
+            continue;
+        }
+        float* p = part_of(one.text, one.head);
+        if (lane == 0) {
+            p[0] = most;
+            p[1] = sum;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) p[2 + lane + c * WAVE] = row[c];
+    }
+}
+
+// PW: wavefronts of queries in the prefix's blocks, which come first (0: there are none).  OWN: the texts' own words are taken here too.
+template <typename T, int DB, int PW, bool OWN, bool BIAS>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 || DB <= 2 ? 2 : 1)) void tiles_kernel(const StepArgs a, uint32_t prefix_blocks) {
+    constexpr int PK = PW ? 4 / PW : 4, P = PW ? TILES_BYTES<T, DB, PK> : 0, O = OWN ? TILES_BYTES<T, DB, 4> : 0;
+    __shared__ __align__(16) char tiles[P > O ? P : O];
+    __shared__ uint32_t bounds[8];
+    extern __shared__ uint32_t buckets[];             // of distances 0 .. -span
+    if constexpr (PW > 0) {
+        if (!OWN || blockIdx.x < prefix_blocks) {
+            tile_block<T, DB, PW, PK, BIAS, true>(a, blockIdx.x, tiles, bounds, buckets);
+            return;
+        }
+    }
+    if constexpr (OWN) tile_block<T, DB, 1, 4, BIAS, false>(a, blockIdx.x - prefix_blocks, tiles, bounds, buckets);
+}
+
+// Queries of a prefix's block: as many as there are for one key head, up to 128.  (32 bits: 64 at least, the tiles of 32 would not fit.)
+uint32_t prefix_rows(uint32_t type, uint32_t rows) { return rows <= 32 && type != ELEM_F32 ? 32 : rows <= 64 ? 64 : 128; }
+
+template <typename T, int DB, int PW, bool OWN> void tiles_bias(const StepArgs& a, hipStream_t st) {
+    const uint32_t rows = a.batch * a.group, row_tiles = PW ? (rows + 32 * PW - 1) / (32 * PW) : 0, units = a.kv_heads * a.front;
+    const uint32_t prefix = (units + 7) / 8 * 8 * row_tiles, own = OWN ? a.batch * a.kv_heads * ((a.group + 31) / 32) * a.splits : 0;
+    if (a.bias) tiles_kernel<T, DB, PW, OWN, true><<<prefix + own, 256, (a.span + 1) * sizeof(uint32_t), st>>>(a, prefix);
+    else tiles_kernel<T, DB, PW, OWN, false><<<prefix + own, 256, 0, st>>>(a, prefix);
+}
+template <typename T, int DB> void tiles_run(const StepArgs& a, uint32_t type, hipStream_t st) {
+    constexpr bool OWN = sizeof(T) == 2;
+    if (a.front) {
+        switch (prefix_rows(type, a.batch * a.group)) {
+            case 128: return tiles_bias<T, DB, 4, OWN>(a, st);
+            case 64: return tiles_bias<T, DB, 2, OWN>(a, st);
+        }
+        if constexpr (OWN) return tiles_bias<T, DB, 1, true>(a, st);
+    }
+    if constexpr (OWN) tiles_bias<T, DB, 0, true>(a, st);
+}
+template <typename T> void tiles_any(const StepArgs& a, uint32_t type, hipStream_t st) {
+    switch ((a.width + 31) / 32) {
+        case 1: return tiles_run<T, 1>(a, type, st);
+        case 2: return tiles_run<T, 2>(a, type, st);
+        case 3: return tiles_run<T, 3>(a, type, st);
+        default: return tiles_run<T, 4>(a, type, st);
+    }
+}
+
+}  // namespace
+
+// Blocks enough to fill the device twice over, of at least 128 words each.
+uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t shared) {
+    const uint32_t rows = batch * (heads / kv_heads), per_block = prefix_rows(type, rows);
+    const uint32_t blocks = (rows + per_block - 1) / per_block * kv_heads, most = (shared + 127) / 128;
+    const uint32_t want = blocks < 512 ? (512 + blocks - 1) / blocks : 1;
+    return want < most ? want : most;
+}
+
+void launch_tiles(const StepArgs& a, uint32_t type, hipStream_t st) {
+    if (type == ELEM_F32) tiles_any<float>(a, type, st);
+    else if (type == ELEM_F16) tiles_any<_Float16>(a, type, st);
+    else tiles_any<__bf16>(a, type, st);
+}
+
+}  // namespace w2v

@@ -15,10 +15,20 @@ PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t k
     return p;
 }
 
-void launch_step_pages(const StepArgs& a, uint32_t type, hipStream_t st) {
-    if (type == ELEM_F32) step_any<float, true>(a, st);
-    else if (type == ELEM_F16) step_any<_Float16, true>(a, st);
-    else step_any<__bf16, true>(a, st);
+namespace {
+// 16 bits: the texts' own words on the matrix cores too, whose 32 rows of queries cost less than converting every element on the
+// vector units.
+template <typename T> void pages_any(const StepArgs& a, uint32_t type, hipStream_t st) {
+    if (a.front || sizeof(T) == 2) launch_tiles(a, type, st);
+    if constexpr (sizeof(T) == 4) step_any<T, true>(a, st);
+    pages_join<T>(a, st);
+}
+}  // namespace
+
+void launch_pages(const StepArgs& a, uint32_t type, hipStream_t st) {
+    if (type == ELEM_F32) pages_any<float>(a, type, st);
+    else if (type == ELEM_F16) pages_any<_Float16>(a, type, st);
+    else pages_any<__bf16>(a, type, st);
 }
 
 }  // namespace w2v

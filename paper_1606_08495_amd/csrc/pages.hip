@@ -320,7 +320,6 @@ extern "C" int w2v_attend_pages(const w2v_attend_spec* spec, const w2v_heads* q,
     a.begin = p.begin; a.front = p.front;
     a.table = table->page_dev; a.table_stride = table->stride; a.shift = shift_of(table); a.n_pages = table->n_pages;
     a.shared = shared;
-    if (p.front) launch_prefix(a, (uint32_t)spec->type, (hipStream_t)stream);
-    launch_step_pages(a, (uint32_t)spec->type, (hipStream_t)stream);
+    launch_pages(a, (uint32_t)spec->type, (hipStream_t)stream);
     return launched();
 }

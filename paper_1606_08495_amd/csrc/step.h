@@ -239,15 +239,15 @@ __global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(c
 }
 
 // Joins the splits of a text's cache: one wavefront per text and head.
-template <typename T, bool PAGED> __global__ __launch_bounds__(THREADS) void step_join_kernel(const StepArgs a) {
+template <typename T> __global__ __launch_bounds__(THREADS) void step_join_kernel(const StepArgs a) {
     const uint32_t lane = threadIdx.x % WAVE;
     const uint64_t at = (uint64_t)blockIdx.x * WAVES + threadIdx.x / WAVE;
     if (at >= (uint64_t)a.batch * a.heads) return;
     const uint32_t text = (uint32_t)(at / a.heads), head = (uint32_t)(at % a.heads);
-    const Keys keys = step_keys<PAGED>(a, text);
-    const uint32_t count = (keys.count + a.per_split - 1) / a.per_split + (PAGED ? a.front : 0);
+    const Keys keys = step_keys<false>(a, text);
+    const uint32_t count = (keys.count + a.per_split - 1) / a.per_split;
     const uint32_t row = a.width + 2;
-    const float* p = a.parts + at * (PAGED ? a.front + a.splits : a.splits) * row;
+    const float* p = a.parts + at * a.splits * row;
     float most = -__builtin_inff(), sum = 0.f, o[2] = {0.f, 0.f};
     for (uint32_t s = lane; s < count; s += WAVE) most = fmaxf(most, p[(uint64_t)s * row]);
     most = wave_max(most);
@@ -260,7 +260,6 @@ template <typename T, bool PAGED> __global__ __launch_bounds__(THREADS) void ste
 #pragma unroll 8
         for (uint32_t l = 0; l < here; ++l) {
             const float fl = __shfl(f, (int)l, 64);
-            if (PAGED && fl == 0.f) continue;         // a part of no weight, whatever it holds
             const float* x = p + (uint64_t)(s0 + l) * row + 2;
 #pragma unroll
             for (int c = 0; c < 2; ++c) if (lane + c * WAVE < a.width) o[c] = fmaf(fl, x[lane + c * WAVE], o[c]);
@@ -270,6 +269,62 @@ template <typename T, bool PAGED> __global__ __launch_bounds__(THREADS) void ste
 #pragma unroll
     for (int c = 0; c < 2; ++c)
         if (lane + c * WAVE < a.width) to[lane + c * WAVE] = (T)(sum == 0.f ? 0.f : o[c] / sum);
+}
+
+// The same over pages, where a row may have many parts: a block per text and head.  A part's columns lie in L lanes, four each, so
+// the block reads 256 / L parts at a time; what the groups of lanes have summed is added in their order.
+template <typename T> __global__ __launch_bounds__(THREADS) void pages_join_kernel(const StepArgs a, uint32_t L) {
+    extern __shared__ float factors[];                // of each part
+    __shared__ float waves[2][WAVES], sums[THREADS][4];
+    const uint32_t tid = threadIdx.x, text = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
+    const Keys keys = step_keys<true>(a, text);
+    const uint32_t count = (keys.count + a.per_split - 1) / a.per_split + a.front, row = a.width + 2;
+    const float* p = a.parts + (uint64_t)blockIdx.x * (a.front + a.splits) * row;
+    float most = -__builtin_inff();
+    for (uint32_t s = tid; s < count; s += THREADS) most = fmaxf(most, p[(uint64_t)s * row]);
+    most = wave_max(most);
+    if (tid % WAVE == 0) waves[0][tid / WAVE] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) most = fmaxf(most, waves[0][w]);
+    float total = 0.f;
+    for (uint32_t s = tid; s < count; s += THREADS) {
+        const float m = p[(uint64_t)s * row], part = p[(uint64_t)s * row + 1];
+        const float f = m == -__builtin_inff() ? (part == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - most);
+        factors[s] = f;
+        total += f == 0.f ? 0.f : f * part;           // (a part of no weight does not show, whatever it holds)
+    }
+    total = lanes_sum<64>(total);
+    if (tid % WAVE == 0) waves[1][tid / WAVE] = total;
+    __syncthreads();
+    total = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) total += waves[1][w];
+    typedef Pack<float, 4>::vec vec;
+    const uint32_t c = tid % L * 4, start = a.width < 4 ? 0 : c < a.width - 4 ? c : a.width - 4, groups = THREADS / L;
+    vec o = {};
+    if (c < a.width) {
+#pragma unroll 4
+        for (uint32_t s = tid / L; s < count; s += groups) {
+            const float* x = p + (uint64_t)s * row + 2;
+            vec four;
+            if (a.width < 4)
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) four[e] = x[e < a.width ? e : 0];
+            else four = *(const Pack<float, 4>::mem*)(x + start);
+            const float f = factors[s];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = f == 0.f ? o[e] : fmaf(f, four[e], o[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[tid][e] = o[e];
+    __syncthreads();
+    if (tid >= a.width) return;
+    const uint32_t lane = tid / 4, e = tid < a.width / 4 * 4 || a.width < 4 ? tid % 4 : tid + 4 - a.width;      // (the last columns lie in a lane that starts earlier)
+    float x = 0.f;
+    for (uint32_t g = 0; g < groups; ++g) x += sums[g * L + lane][e];
+    head_row<T>(a.o, text, head)[tid] = (T)(total == 0.f ? 0.f : x / total);
 }
 
 template <typename T, int L, int HEADS, bool PAGED> void step_run(const StepArgs& a, hipStream_t st) {
@@ -288,7 +343,14 @@ template <typename T, bool PAGED> void step_any(const StepArgs& a, hipStream_t s
     if (chunks <= 8) step_heads<T, 8, PAGED>(a, st);
     else if (chunks <= 16) step_heads<T, 16, PAGED>(a, st);
     else if constexpr (sizeof(T) == 4) step_heads<T, 32, PAGED>(a, st);
-    if (a.splits > 1 || (PAGED && a.front)) step_join_kernel<T, PAGED><<<(uint32_t)(((uint64_t)a.batch * a.heads + WAVES - 1) / WAVES), THREADS, 0, st>>>(a);
+    if constexpr (!PAGED) {
+        if (a.splits > 1) step_join_kernel<T><<<(uint32_t)(((uint64_t)a.batch * a.heads + WAVES - 1) / WAVES), THREADS, 0, st>>>(a);
+    }
+}
+template <typename T> void pages_join(const StepArgs& a, hipStream_t st) {
+    uint32_t L = 1;
+    while (L * 4 < a.width) L *= 2;
+    if (a.front + a.splits > 1) pages_join_kernel<T><<<a.batch * a.heads, THREADS, (a.front + a.splits) * sizeof(float), st>>>(a, L);
 }
 
 }  // namespace
