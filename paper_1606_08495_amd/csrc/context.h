@@ -83,9 +83,12 @@ void launch_step(const StepArgs& a, uint32_t type, hipStream_t st);
 // Over pages.  What a call splits into, by sizes alone.
 uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t shared);
 struct PageSplits { uint32_t begin, front; StepSplits own; };
-PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t room, uint32_t shared, uint32_t left, uint32_t sinks);
+PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t width, uint32_t room, uint32_t shared,
+                       uint32_t left, uint32_t sinks);
 void launch_pages(const StepArgs& a, uint32_t type, hipStream_t st);
-void launch_tiles(const StepArgs& a, uint32_t type, hipStream_t st);      // of k_page_tiles.hip, for k_pages.hip
+// of k_page_tiles.hip, for k_pages.hip
+void launch_prefix(const StepArgs& a, uint32_t type, hipStream_t st);
+void launch_own_tiles(const StepArgs& a, uint32_t type, hipStream_t st);      // (16 bits)
 
 // ---- positions that turn, and words on their way into pages ------------------------------------------
 struct Pages { void* p; uint64_t page, token, head; };

@@ -17,6 +17,7 @@
 namespace w2v {
 namespace {
 
+constexpr uint64_t NOWHERE = ~0ull;
 template <typename T> constexpr float RISE = std::is_same<T, _Float16>::value ? 2.f : 8.f;
 template <typename T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 13.f : 0.f;
 
@@ -104,15 +105,18 @@ __device__ void careful_row(const StepArgs& a, const Axis& x, uint32_t kv_head, 
     total = lanes_sum<64>(total);
 }
 
-// The keys of a tile: with four wavefronts on it 128, a piece of 32 for each.
-template <int WK> constexpr int KEYS = WK == 4 ? 128 : 64;
-template <typename T, int DB, int WK> constexpr int TILES_BYTES = 2 * Tile<T, DB, KEYS<WK>>::BYTES;
+constexpr int KEYS = 64;                              // of a tile
 
 // One block, of the prefix (PREFIX) or of one text's own words.
 template <typename T, int DB, int WR, int WK, bool BIAS, bool PREFIX>
-__device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block, char* tiles, uint32_t* bounds, uint32_t* buckets) {
-    constexpr int K = KEYS<WK>, THREADS = 64 * WR * WK, PIECES = K / 32 / WK, KEEP = DB * 16 + 2, MASKS = K / 64;
-    typedef Tile<T, DB, K> Tl;
+__device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
+    constexpr int THREADS = 64 * WR * WK, KEEP = DB * 16 + 2;
+    constexpr bool JOINT = DB <= (sizeof(T) == 2 ? 2 : 1);      // both pieces of a tile at a time, where registers allow
+    typedef Tile<T, DB, KEYS> Tl;
+    __shared__ __align__(16) char tiles[2 * Tl::BYTES];
+    __shared__ uint64_t places[2][2][KEYS];
+    __shared__ uint32_t bounds[2 * WR];
+    extern __shared__ uint32_t buckets[];             // of distances 0 .. -span
     static_assert(WK == 1 || WR * KEEP * 64 * 4 <= 2 * Tl::BYTES, "room to join the parts");
     const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const uint32_t wr = wave % WR, wk = wave / WR;
@@ -126,10 +130,11 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block, ch
         kv_head = unit % a.kv_heads;
         split = unit / a.kv_heads;
     } else {
-        split = block % a.splits; block /= a.splits;
+        // the heads of the same words, which lie side by side in memory, follow each other
+        kv_head = block % a.kv_heads; block /= a.kv_heads;
         row_tile = block % row_tiles; block /= row_tiles;
-        kv_head = block % a.kv_heads;
-        text = block / a.kv_heads;
+        split = block % a.splits;
+        text = block / a.splits;
     }
     const bool whole = !PREFIX && a.front + a.splits == 1;
     const uint32_t first = row_tile * 32 * WR + wr * 32;
@@ -181,7 +186,7 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block, ch
         x.lo = __builtin_amdgcn_readfirstlane(x.lo < end ? x.lo : end);
         x.sunk = x.lo < a.sinks ? x.lo : a.sinks;
         x.count = x.sunk + end - x.lo;
-        const uint32_t per = ((x.count + K - 1) / K + a.front - 1) / a.front * K;
+        const uint32_t per = ((x.count + KEYS - 1) / KEYS + a.front - 1) / a.front * KEYS;
         from = split * per < x.count ? split * per : x.count;
         to = x.count - from < per ? x.count : from + per;
     }
@@ -197,97 +202,105 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block, ch
     const uint32_t at_along = Tl::base_along(lane), at_across = Tl::base_across(lane);
 
 
-    Transit<T, DB, K, THREADS> k, v;
+    Transit<T, DB, KEYS, THREADS> k, v;
     k.start(Heads{a.k.p, a.k.token, a.k.head}, kv_head, 0);
     v.start(Heads{a.v.p, a.v.token, a.v.head}, kv_head, 0);
-    uint32_t page[MASKS];                             // of keys n0 + lane (and 64 on) of the tile to be fetched next
-    bool in[MASKS];                                   // whether they are there to be shown
+    // Where the tiles' rows lie, found by a thread each two tiles ahead: elements from the pools' starts, NOWHERE for keys that are not to be
+    // shown (past the end, on no page, dropped).
+    uint64_t k_next = 0, v_next = 0;
     const auto look = [&](uint32_t n0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < MASKS; ++i) {
-            const uint32_t at = n0 + i * 64 + lane, j = x.word(at < to ? at : to - 1);
-            page[i] = x.page(j, a.shift);
-            in[i] = at < to;
-            if (!PREFIX) in[i] &= !(a.skip_self && j + 1 == own.hi) && (!a.keep || a.keep[(uint64_t)text * a.room + j]);
-        }
+        if (threadIdx.x >= KEYS) return;
+        const uint32_t at = n0 + threadIdx.x, j = x.word(at < to ? at : to - 1), page = x.page(j, a.shift);
+        bool in = at < to && page < a.n_pages;
+        if (!PREFIX) in &= !(a.skip_self && j + 1 == own.hi) && (!a.keep || a.keep[(uint64_t)text * a.room + j]);
+        const uint32_t place = j & ((1u << a.shift) - 1);
+        k_next = in ? page * a.k.text + place * a.k.token : NOWHERE;
+        v_next = in ? page * a.v.text + place * a.v.token : NOWHERE;
     };
-    struct Kept { uint64_t mask[MASKS]; };
-    const auto fetch = [&](uint32_t n0) __attribute__((always_inline)) {
+    const auto tell = [&](uint32_t turn) __attribute__((always_inline)) {
+        if (threadIdx.x >= KEYS) return;
+        places[turn][0][threadIdx.x] = k_next;
+        places[turn][1][threadIdx.x] = v_next;
+    };
+    const auto fetch = [&](uint32_t turn) __attribute__((always_inline)) {
+        uint32_t gone = 0;
 #pragma unroll
         for (uint32_t n = 0; n < decltype(k)::PER; ++n) {
-            const uint32_t r = k.r0 + n * decltype(k)::RS, j = x.word(n0 + r < to ? n0 + r : to - 1);
-            const uint32_t there = (uint32_t)__shfl((int)page[n * decltype(k)::RS / 64], (int)(r % 64), 64);
-            const uint32_t g = there < a.n_pages ? there : 0, place = j & ((1u << a.shift) - 1);
-            k.at[n] = k.base + g * a.k.text + place * a.k.token;
-            v.at[n] = v.base + g * a.v.text + place * a.v.token;
+            const uint32_t r = k.r0 + n * decltype(k)::RS;
+            const uint64_t at = places[turn][0][r], v_at = places[turn][1][r];
+            gone |= (at == NOWHERE ? 1u : 0u) << n;
+            k.at[n] = k.base + (at == NOWHERE ? 0 : at);
+            v.at[n] = v.base + (at == NOWHERE ? 0 : v_at);
         }
         k.load(a.width);
         v.load(a.width);
-        Kept kept;
-#pragma unroll
-        for (int i = 0; i < MASKS; ++i) kept.mask[i] = __ballot(in[i] && page[i] < a.n_pages);
-        return kept;
+        return gone;
     };
-    Kept kept, kept_next;
     char *const k_tile = tiles, *const v_tile = tiles + Tl::BYTES;
-    const auto store = [&]() __attribute__((always_inline)) {
+    const auto store = [&](uint32_t gone) __attribute__((always_inline)) {
         k.store(k_tile, a.width);
-        uint64_t every = ~0ull;
-#pragma unroll
-        for (int i = 0; i < MASKS; ++i) every &= kept.mask[i];
-        if (!rare(~every)) v.store(v_tile, a.width);
-        else v.store_rows(v_tile, a.width, [&](uint32_t r0, uint32_t r) __attribute__((always_inline)) { return !(kept.mask[r / 64] >> (r % 64 + r0) & 1); });
+        if (!rare(__any(gone != 0))) v.store(v_tile, a.width);
+        else v.store_rows(v_tile, a.width, gone);
     };
+    uint32_t turn = 0;                                // of the tile in work: whose places it has
     if (from < to) {
         look(from);
-        kept = fetch(from);
-        if (from + K < to) look(from + K);
-        store();
+        tell(0);
+        if (from + KEYS < to) {
+            look(from + KEYS);
+            tell(1);
+        }
     }
     __syncthreads();
-    for (uint32_t n0 = from; n0 < to; n0 += K) {
-        const bool more = n0 + K < to;
+    if (from < to) store(fetch(0));
+    __syncthreads();
+    for (uint32_t n0 = from; n0 < to; n0 += KEYS) {
+        const bool more = n0 + KEYS < to;
+        uint32_t gone = 0;
         if (more) {
-            kept_next = fetch(n0 + K);
-            if (n0 + 2 * K < to) look(n0 + 2 * K);
+            gone = fetch(turn ^ 1);
+            if (n0 + 2 * KEYS < to) look(n0 + 2 * KEYS);
         }
+        // P pieces of 32 keys from piece p0 on, together: their products do not wait for each other
+        const auto pieces = [&](auto P, int p0) __attribute__((always_inline)) {
+            Acc s[P.value];
 #pragma unroll
-        for (int p0 = 0; p0 < PIECES; ++p0) {
-            const int p = WK > 1 ? (int)wk : p0;
-            uint64_t mask = kept.mask[0];
-            if constexpr (MASKS > 1) mask = wk < 2 ? mask : kept.mask[1];
-            const uint32_t n = n0 + p * 32, j0 = n + shift, kept32 = (uint32_t)(mask >> (p % 2 * 32));
-            const bool linear = n >= x.sunk;
-            // pieces that none of the wavefront's queries is shown
-            if (!some || n >= to || (PREFIX && linear && !(j0 < hi_most && (j0 + 32 > lo_least || j0 < a.sinks)))) continue;
-            Acc s = {};
+            for (int p = 0; p < P.value; ++p) s[p] = Acc{};
 #pragma unroll
-            for (int c = 0; c < 2 * DB; ++c) mma(Tl::along(k_tile, at_along + p * (32 / 4 * Tl::STRIDE), 0, c), q[c], s);
-            const auto word = [&](int r) __attribute__((always_inline)) { return x.word(n + 4 * h + acc_row(r, 0)); };
-            if constexpr (BIAS) {
-                if (linear && hi_least > a.span && j0 + 31 <= hi_least - 1 - a.span) {
+            for (int c = 0; c < 2 * DB; ++c)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, far);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const uint32_t back = own.hi - 1 - word(r), b = buckets[back < a.span ? back : a.span];      // (words behind the text: masked)
-                        const float w = b < a.n_buckets ? a.bias[(uint64_t)own.head * a.n_buckets + b] : 0.f;
-                        s[r] = fmaf(s[r], a.scale2, fabsf(w) < __builtin_inff() ? fminf(fmaxf(w, -BIAS_HELD), BIAS_HELD) * LOG2E : w);
-                    }
-                }
-            }
-            bool all = kept32 == 0xFFFFFFFFu;
-            if (PREFIX) all &= linear && j0 >= lo_most && j0 + 32 <= hi_least && !a.keep && !(a.skip_self && j0 + 32 >= hi_least);
-            if (!all)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const bool in = (kept32 >> acc_row(r, h) & 1) != 0 && (!PREFIX || shows(a, own, word(r)));
-                    s[r] = in ? s[r] : -__builtin_inff();
-                }
+                for (int p = 0; p < P.value; ++p) mma(Tl::along(k_tile, at_along + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, c), q[c], s[p]);
             float most = -__builtin_inff();
 #pragma unroll
-            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[r]);
+            for (int p = 0; p < P.value; ++p) {
+                const uint32_t n = n0 + (p0 + p) * 32, j0 = n + shift;
+                const uint32_t kept32 = (uint32_t)__ballot(places[turn][0][(p0 + p) * 32 + lane % 32] != NOWHERE);
+                const bool linear = n >= x.sunk;
+                const auto word = [&](int r) __attribute__((always_inline)) { return x.word(n + 4 * h + acc_row(r, 0)); };
+                if constexpr (BIAS) {
+                    if (linear && hi_least > a.span && j0 + 31 <= hi_least - 1 - a.span) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[p][r] = fmaf(s[p][r], a.scale2, far);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const uint32_t back = own.hi - 1 - word(r), b = buckets[back < a.span ? back : a.span];      // (words behind the text: masked)
+                            const float w = b < a.n_buckets ? a.bias[(uint64_t)own.head * a.n_buckets + b] : 0.f;
+                            s[p][r] = fmaf(s[p][r], a.scale2, fabsf(w) < __builtin_inff() ? fminf(fmaxf(w, -BIAS_HELD), BIAS_HELD) * LOG2E : w);
+                        }
+                    }
+                }
+                bool all = kept32 == 0xFFFFFFFFu;
+                if (PREFIX) all &= linear && j0 >= lo_most && j0 + 32 <= hi_least && !a.keep && !(a.skip_self && j0 + 32 >= hi_least);
+                if (!all)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const bool in = (kept32 >> acc_row(r, h) & 1) != 0 && (!PREFIX || shows(a, own, word(r)));
+                        s[p][r] = in ? s[p][r] : -__builtin_inff();
+                    }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, s[p][r]);
+            }
             most = halves_max(most) * unit_scale;
             if (__any(most > m + RISE<T>)) {
                 const float up = fmaxf(m, most);
@@ -299,60 +312,71 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block, ch
             }
             const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
             float sum = 0.f;
+            Acc part[sizeof(T) == 4 ? DB : 1] = {};   // 32 bits: the pieces' sums first, then the whole's: one long chain would lose bits
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], unit_scale, -base));
-                sum += s[r];
+            for (int g = 0; g < 2 * P.value; ++g) {   // 16 keys
+                const int p = g / 2;
+#pragma unroll
+                for (int c = 8 * (g % 2); c < 8 * (g % 2) + 8; ++c) {
+                    s[p][c] = __builtin_amdgcn_exp2f(fmaf(s[p][c], unit_scale, -base));
+                    sum += s[p][c];
+                }
+                const auto w = acc_operand<T>(s[p], g % 2);
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+                    mma(Tl::across(v_tile, at_across + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, g % 2, b), w, sizeof(T) == 4 ? part[b % (sizeof(T) == 4 ? DB : 1)] : o[b]);
             }
             total += sum;
+            if constexpr (sizeof(T) == 4)
 #pragma unroll
-            for (int b = 0; b < DB; ++b) {
-                if constexpr (sizeof(T) == 4) {       // a piece's sum first, then the whole's: one long chain would lose bits
-                    Acc part = {};
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) mma(Tl::across(v_tile, at_across + p * (32 / 4 * Tl::STRIDE), 0, g, b), acc_operand<T>(s, g), part);
-                    o[b] += part;
-                } else {
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) mma(Tl::across(v_tile, at_across + p * (32 / 4 * Tl::STRIDE), 0, g, b), acc_operand<T>(s, g), o[b]);
-                }
+                for (int b = 0; b < DB; ++b) o[b] += part[b];
+        };
+        // whether any of the wavefront's queries is shown any of a piece
+        const auto needs = [&](int p) __attribute__((always_inline)) {
+            const uint32_t n = n0 + p * 32, j0 = n + shift;
+            return some && n < to && (!PREFIX || n < x.sunk || (j0 < hi_most && (j0 + 32 > lo_least || j0 < a.sinks)));
+        };
+        if constexpr (WK == 2) {
+            if (needs(wk)) pieces(std::integral_constant<int, 1>{}, wk);
+        } else {
+            const bool first_piece = needs(0), second_piece = needs(1);
+            if (JOINT && first_piece && second_piece) pieces(std::integral_constant<int, JOINT ? 2 : 1>{}, 0);
+            else {
+                if (first_piece) pieces(std::integral_constant<int, 1>{}, 0);
+                if (second_piece) pieces(std::integral_constant<int, 1>{}, 1);
             }
         }
         if (more) {
             __syncthreads();
-            kept = kept_next;
-            store();
+            store(gone);
+            if (n0 + 2 * KEYS < to) tell(turn);
+            turn ^= 1;
             __syncthreads();
         }
     }
-    if constexpr (WK > 1) {                           // the other parts' sums through LDS to the first, one part after the other
+    if constexpr (WK == 2) {                          // the second half's sums through LDS to the first
         float* const other = (float*)tiles + wr * KEEP * WAVE + lane;
+        __syncthreads();
+        if (wk) {
+            other[0] = m;
+            other[WAVE] = total;
 #pragma unroll
-        for (int part = 1; part < WK; ++part) {
-            __syncthreads();
-            if ((int)wk == part) {
-                other[0] = m;
-                other[WAVE] = total;
+            for (int b = 0; b < DB; ++b)
 #pragma unroll
-                for (int b = 0; b < DB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) other[(2 + b * 16 + r) * WAVE] = o[b][r];
-            }
-            __syncthreads();
-            if (wk == 0) {
-                const float m1 = other[0], up = fmaxf(m, m1);
-                const float f0 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - up);
-                const float f1 = m1 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m1 - up);
-                // (a maximum is -infinity where a part has seen nothing: its sums are zero; not a number stays where it is)
-                total = total * (total == 0.f ? 1.f : f0) + other[WAVE] * (other[WAVE] == 0.f ? 1.f : f1);
-#pragma unroll
-                for (int b = 0; b < DB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[b][r] = o[b][r] * f0 + other[(2 + b * 16 + r) * WAVE] * f1;
-                m = up;
-            }
+                for (int r = 0; r < 16; ++r) other[(2 + b * 16 + r) * WAVE] = o[b][r];
         }
+        __syncthreads();
         if (wk) return;
+        const float m1 = other[0], up = fmaxf(m, m1);
+        const float f0 = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - up);
+        const float f1 = m1 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m1 - up);
+        // (a maximum is -infinity where a half has seen nothing: its sums are zero; not a number stays where it is)
+        total = total * (total == 0.f ? 1.f : f0) + other[WAVE] * (other[WAVE] == 0.f ? 1.f : f1);
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[b][r] = o[b][r] * f0 + other[(2 + b * 16 + r) * WAVE] * f1;
+        m = up;
     }
     if (!some) return;
     total = halves_sum(total);
@@ -415,48 +439,38 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block, ch
     }
 }
 
-// PW: wavefronts of queries in the prefix's blocks, which come first (0: there are none).  OWN: the texts' own words are taken here too.
-template <typename T, int DB, int PW, bool OWN, bool BIAS>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 || DB <= 2 ? 2 : 1)) void tiles_kernel(const StepArgs a, uint32_t prefix_blocks) {
-    constexpr int PK = PW ? 4 / PW : 4, P = PW ? TILES_BYTES<T, DB, PK> : 0, O = OWN ? TILES_BYTES<T, DB, 4> : 0;
-    __shared__ __align__(16) char tiles[P > O ? P : O];
-    __shared__ uint32_t bounds[8];
-    extern __shared__ uint32_t buckets[];             // of distances 0 .. -span
-    if constexpr (PW > 0) {
-        if (!OWN || blockIdx.x < prefix_blocks) {
-            tile_block<T, DB, PW, PK, BIAS, true>(a, blockIdx.x, tiles, bounds, buckets);
-            return;
-        }
-    }
-    if constexpr (OWN) tile_block<T, DB, 1, 4, BIAS, false>(a, blockIdx.x - prefix_blocks, tiles, bounds, buckets);
+template <typename T, int DB, int WR, int WK, bool BIAS, bool PREFIX>
+__global__ __launch_bounds__(64 * WR * WK, (sizeof(T) == 2 || DB <= 2 ? 2 : 1)) void tile_kernel(const StepArgs a) {
+    tile_block<T, DB, WR, WK, BIAS, PREFIX>(a, blockIdx.x);
 }
 
-// Queries of a prefix's block: as many as there are for one key head, up to 128.  (32 bits: 64 at least, the tiles of 32 would not fit.)
+// Queries of a prefix's block: as many as there are for one key head, up to 128.  (32 bits: 64 at least, whose four wavefronts' registers
+// hold a tile on its way.)
 uint32_t prefix_rows(uint32_t type, uint32_t rows) { return rows <= 32 && type != ELEM_F32 ? 32 : rows <= 64 ? 64 : 128; }
 
-template <typename T, int DB, int PW, bool OWN> void tiles_bias(const StepArgs& a, hipStream_t st) {
-    const uint32_t rows = a.batch * a.group, row_tiles = PW ? (rows + 32 * PW - 1) / (32 * PW) : 0, units = a.kv_heads * a.front;
-    const uint32_t prefix = (units + 7) / 8 * 8 * row_tiles, own = OWN ? a.batch * a.kv_heads * ((a.group + 31) / 32) * a.splits : 0;
-    if (a.bias) tiles_kernel<T, DB, PW, OWN, true><<<prefix + own, 256, (a.span + 1) * sizeof(uint32_t), st>>>(a, prefix);
-    else tiles_kernel<T, DB, PW, OWN, false><<<prefix + own, 256, 0, st>>>(a, prefix);
+template <typename T, int DB, int WR, int WK, bool PREFIX> void tiles_bias(const StepArgs& a, hipStream_t st) {
+    const uint32_t rows = PREFIX ? a.batch * a.group : a.group, row_tiles = (rows + 32 * WR - 1) / (32 * WR);
+    const uint32_t blocks = PREFIX ? (a.kv_heads * a.front + 7) / 8 * 8 * row_tiles : a.batch * a.kv_heads * row_tiles * a.splits;
+    if (a.bias) tile_kernel<T, DB, WR, WK, true, PREFIX><<<blocks, 64 * WR * WK, (a.span + 1) * sizeof(uint32_t), st>>>(a);
+    else tile_kernel<T, DB, WR, WK, false, PREFIX><<<blocks, 64 * WR * WK, 0, st>>>(a);
 }
-template <typename T, int DB> void tiles_run(const StepArgs& a, uint32_t type, hipStream_t st) {
-    constexpr bool OWN = sizeof(T) == 2;
-    if (a.front) {
+template <typename T, int DB> void tiles_run(const StepArgs& a, uint32_t type, bool prefix, hipStream_t st) {
+    if (prefix) {
         switch (prefix_rows(type, a.batch * a.group)) {
-            case 128: return tiles_bias<T, DB, 4, OWN>(a, st);
-            case 64: return tiles_bias<T, DB, 2, OWN>(a, st);
+            case 128: return tiles_bias<T, DB, 4, 1, true>(a, st);
+            case 64: return tiles_bias<T, DB, 2, 2, true>(a, st);
         }
-        if constexpr (OWN) return tiles_bias<T, DB, 1, true>(a, st);
+        if constexpr (sizeof(T) == 2) tiles_bias<T, DB, 1, 2, true>(a, st);
+    } else if constexpr (sizeof(T) == 2) {
+        tiles_bias<T, DB, 1, 2, false>(a, st);
     }
-    if constexpr (OWN) tiles_bias<T, DB, 0, true>(a, st);
 }
-template <typename T> void tiles_any(const StepArgs& a, uint32_t type, hipStream_t st) {
+template <typename T> void tiles_any(const StepArgs& a, uint32_t type, bool prefix, hipStream_t st) {
     switch ((a.width + 31) / 32) {
-        case 1: return tiles_run<T, 1>(a, type, st);
-        case 2: return tiles_run<T, 2>(a, type, st);
-        case 3: return tiles_run<T, 3>(a, type, st);
-        default: return tiles_run<T, 4>(a, type, st);
+        case 1: return tiles_run<T, 1>(a, type, prefix, st);
+        case 2: return tiles_run<T, 2>(a, type, prefix, st);
+        case 3: return tiles_run<T, 3>(a, type, prefix, st);
+        default: return tiles_run<T, 4>(a, type, prefix, st);
     }
 }
 
@@ -470,10 +484,15 @@ uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t k
     return want < most ? want : most;
 }
 
-void launch_tiles(const StepArgs& a, uint32_t type, hipStream_t st) {
-    if (type == ELEM_F32) tiles_any<float>(a, type, st);
-    else if (type == ELEM_F16) tiles_any<_Float16>(a, type, st);
-    else tiles_any<__bf16>(a, type, st);
+namespace {
+void launch(const StepArgs& a, uint32_t type, bool prefix, hipStream_t st) {
+    if (type == ELEM_F32) tiles_any<float>(a, type, prefix, st);
+    else if (type == ELEM_F16) tiles_any<_Float16>(a, type, prefix, st);
+    else tiles_any<__bf16>(a, type, prefix, st);
 }
+}  // namespace
+
+void launch_prefix(const StepArgs& a, uint32_t type, hipStream_t st) { launch(a, type, true, st); }
+void launch_own_tiles(const StepArgs& a, uint32_t type, hipStream_t st) { launch(a, type, false, st); }
 
 }  // namespace w2v

@@ -266,7 +266,7 @@ int check_attend_pages(const w2v_attend_spec* s, uint32_t batch, const w2v_page_
 
 // The workspace: partial results where a text's words are read by several blocks.
 PageSplits pages_splits(const w2v_attend_spec* s, uint32_t batch, const w2v_page_table* t, uint32_t shared) {
-    return page_splits((uint32_t)s->type, batch, s->heads, s->kv_heads, t->slots * t->page_words, shared, s->left, s->sinks);
+    return page_splits((uint32_t)s->type, batch, s->heads, s->kv_heads, s->width, t->slots * t->page_words, shared, s->left, s->sinks);
 }
 size_t pages_bytes(const w2v_attend_spec* s, uint32_t batch, const PageSplits& p) {
     const uint32_t parts = p.front + p.own.splits;

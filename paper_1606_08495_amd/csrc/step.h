@@ -53,9 +53,12 @@ __global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(c
     const uint32_t lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, part = lane % L, group = lane / L;
     const uint32_t rounds = (a.group + HEADS - 1) / HEADS;
     uint32_t at = blockIdx.x;
+    // (over pages the heads of the same words follow each other, whose rows lie side by side in memory)
+    const uint32_t paged_head = at % a.kv_heads;
+    if (PAGED) at /= a.kv_heads;
     const uint32_t split = at % a.splits; at /= a.splits;
     const uint32_t round = at % rounds; at /= rounds;
-    const uint32_t kv_head = at % a.kv_heads, text = at / a.kv_heads;
+    const uint32_t kv_head = PAGED ? paged_head : at % a.kv_heads, text = PAGED ? at : at / a.kv_heads;
     const uint32_t head0 = kv_head * a.group + round * HEADS;
     const uint32_t heads = a.group - round * HEADS < HEADS ? a.group - round * HEADS : HEADS;
     const Keys keys = step_keys<PAGED>(a, text);

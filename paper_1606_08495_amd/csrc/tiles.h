@@ -191,13 +191,13 @@ template <typename T, int DB, int ROWS, int THREADS> struct Transit {
         for (uint32_t n = 0; n < PER; ++n) x[n] = chunk_read<T, DB == 1>(at[n], c0, width);
         tile += ROWS * stride;
     }
-    // As store, with zeros in rows that `gone` names; for tiles of more rows than a mask has bits.
-    template <typename F> __device__ __forceinline__ void store_rows(char* to, uint32_t width, const F& gone) {
+    // As store, with zeros in those of this thread's rows whose bit is set.
+    __device__ __forceinline__ void store_rows(char* to, uint32_t width, uint32_t gone) {
         store<false>(to, width);
         if (c0 >= (uint32_t)Tl::CHUNKS * Tl::N || threadIdx.x / LANES >= (uint32_t)ROWS) return;
 #pragma unroll
         for (uint32_t n = 0; n < PER; ++n)
-            if (gone(r0, n * RS)) *(typename Tl::Chunk*)(to + Tl::place(r0 + n * RS, c0 / Tl::N)) = typename Tl::Chunk{};
+            if (gone >> n & 1) *(typename Tl::Chunk*)(to + Tl::place(r0 + n * RS, c0 / Tl::N)) = typename Tl::Chunk{};
     }
     // CLEAN: zeros past the width.  Rows whose bit of `kept` is not set become zeros (tiles of 64 rows).
     template <bool CLEAN = false> __device__ __forceinline__ void store(char* to, uint32_t width, uint64_t kept = ~0ull) {
