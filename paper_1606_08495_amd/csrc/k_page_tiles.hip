@@ -113,11 +113,13 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
     constexpr int THREADS = 64 * WR * WK, KEEP = DB * 16 + 2;
     constexpr bool JOINT = DB <= (sizeof(T) == 2 ? 2 : 1);      // both pieces of a tile at a time, where registers allow
     typedef Tile<T, DB, KEYS> Tl;
-    __shared__ __align__(16) char tiles[2 * Tl::BYTES];
-    __shared__ uint64_t places[2][2][KEYS];
+    // Blocks of the prefix have two of each tile, and one barrier a tile; the others' many small blocks a CU take turns by themselves.
+    constexpr int BUFFERS = WR > 1 ? 2 : 1;
+    __shared__ __align__(16) char tiles[BUFFERS][2 * Tl::BYTES];
+    __shared__ uint64_t places[3][2][KEYS];
     __shared__ uint32_t bounds[2 * WR];
     extern __shared__ uint32_t buckets[];             // of distances 0 .. -span
-    static_assert(WK == 1 || WR * KEEP * 64 * 4 <= 2 * Tl::BYTES, "room to join the parts");
+    static_assert(WK == 1 || WR * KEEP * 64 * 4 <= (int)sizeof(tiles), "room to join the parts");
     const uint32_t lane = threadIdx.x % WAVE, h = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const uint32_t wr = wave % WR, wk = wave / WR;
     uint32_t kv_head, split, row_tile, text = 0;
@@ -140,12 +142,18 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
     const uint32_t first = row_tile * 32 * WR + wr * 32;
     const bool some = first < rows, real = first + lane % 32 < rows;
     const uint32_t row = real ? first + lane % 32 : rows - 1;
-    const Query own = PREFIX ? query_of(a, row / a.group, kv_head * a.group + row % a.group) : query_of(a, text, kv_head * a.group + row);
     Axis x;
     x.row0 = a.table;
     x.shared = PREFIX ? ~0u : a.shared;
     x.pages = a.table + (uint64_t)text * a.table_stride;
-    uint32_t from, to;
+    // Without a window the first words are known before the texts' lengths are: their pages are asked for at once.
+    const bool bounded = a.left < a.room;
+    uint32_t from = split * a.per_split, to, early_page = 0;
+    if (!PREFIX && !bounded) {
+        const uint32_t j = a.begin + from + threadIdx.x;
+        early_page = x.page(j < a.room ? j : a.room - 1, a.shift);
+    }
+    const Query own = PREFIX ? query_of(a, row / a.group, kv_head * a.group + row % a.group) : query_of(a, text, kv_head * a.group + row);
     if constexpr (!PREFIX) {
         x.sunk = own.lo < a.sinks ? own.lo : a.sinks;
         x.first = x.sunk < a.begin ? x.sunk : a.begin;
@@ -156,7 +164,6 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
         x.sunk = __builtin_amdgcn_readfirstlane(x.sunk);
         x.lo = __builtin_amdgcn_readfirstlane(x.lo);
         x.count = __builtin_amdgcn_readfirstlane(x.count);
-        from = split * a.per_split;
         to = x.count < from + a.per_split ? x.count : from + a.per_split;
         if (from >= to && !whole) return;
     }
@@ -168,24 +175,26 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
     if constexpr (BIAS)
         for (uint32_t c = threadIdx.x; c <= a.span; c += THREADS) buckets[c] = a.buckets[a.span - c];
     if constexpr (PREFIX) {
-        lo_least = lanes_least(own.lo), lo_most = ~lanes_least(~own.lo), hi_least = lanes_least(own.hi), hi_most = ~lanes_least(~own.hi);
-        if (lane == 0) {
-            bounds[wr] = lo_least;
-            bounds[WR + wr] = hi_most;
-        }
-        __syncthreads();
-        uint32_t end = 0;
-        x.lo = ~0u;
+        x.first = x.lo = x.sunk = 0;
+        x.count = a.begin;
+        if (bounded) {
+            lo_least = lanes_least(own.lo), lo_most = ~lanes_least(~own.lo), hi_most = ~lanes_least(~own.hi);
+            if (lane == 0) {
+                bounds[wr] = lo_least;
+                bounds[WR + wr] = hi_most;
+            }
+            __syncthreads();
+            uint32_t lo = ~0u, end = 0;
 #pragma unroll
-        for (int w = 0; w < WR; ++w) {
-            x.lo = bounds[w] < x.lo ? bounds[w] : x.lo;
-            end = bounds[WR + w] > end ? bounds[WR + w] : end;
+            for (int w = 0; w < WR; ++w) {
+                lo = bounds[w] < lo ? bounds[w] : lo;
+                end = bounds[WR + w] > end ? bounds[WR + w] : end;
+            }
+            end = __builtin_amdgcn_readfirstlane(end < a.begin ? end : a.begin);
+            x.lo = __builtin_amdgcn_readfirstlane(lo < end ? lo : end);
+            x.sunk = x.lo < a.sinks ? x.lo : a.sinks;
+            x.count = x.sunk + end - x.lo;
         }
-        end = __builtin_amdgcn_readfirstlane(end < a.begin ? end : a.begin);
-        x.first = 0;
-        x.lo = __builtin_amdgcn_readfirstlane(x.lo < end ? x.lo : end);
-        x.sunk = x.lo < a.sinks ? x.lo : a.sinks;
-        x.count = x.sunk + end - x.lo;
         const uint32_t per = ((x.count + KEYS - 1) / KEYS + a.front - 1) / a.front * KEYS;
         from = split * per < x.count ? split * per : x.count;
         to = x.count - from < per ? x.count : from + per;
@@ -208,19 +217,17 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
     // Where the tiles' rows lie, found by a thread each two tiles ahead: elements from the pools' starts, NOWHERE for keys that are not to be
     // shown (past the end, on no page, dropped).
     uint64_t k_next = 0, v_next = 0;
-    const auto look = [&](uint32_t n0) __attribute__((always_inline)) {
-        if (threadIdx.x >= KEYS) return;
-        const uint32_t at = n0 + threadIdx.x, j = x.word(at < to ? at : to - 1), page = x.page(j, a.shift);
+    const auto look = [&](uint32_t at, bool known) __attribute__((always_inline)) {
+        const uint32_t j = x.word(at < to ? at : to - 1), page = known ? early_page : x.page(j, a.shift);
         bool in = at < to && page < a.n_pages;
         if (!PREFIX) in &= !(a.skip_self && j + 1 == own.hi) && (!a.keep || a.keep[(uint64_t)text * a.room + j]);
         const uint32_t place = j & ((1u << a.shift) - 1);
         k_next = in ? page * a.k.text + place * a.k.token : NOWHERE;
         v_next = in ? page * a.v.text + place * a.v.token : NOWHERE;
     };
-    const auto tell = [&](uint32_t turn) __attribute__((always_inline)) {
-        if (threadIdx.x >= KEYS) return;
-        places[turn][0][threadIdx.x] = k_next;
-        places[turn][1][threadIdx.x] = v_next;
+    const auto tell = [&](uint32_t turn, uint32_t r) __attribute__((always_inline)) {
+        places[turn][0][r] = k_next;
+        places[turn][1][r] = v_next;
     };
     const auto fetch = [&](uint32_t turn) __attribute__((always_inline)) {
         uint32_t gone = 0;
@@ -236,40 +243,60 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
         v.load(a.width);
         return gone;
     };
-    char *const k_tile = tiles, *const v_tile = tiles + Tl::BYTES;
-    const auto store = [&](uint32_t gone) __attribute__((always_inline)) {
-        k.store(k_tile, a.width);
-        if (!rare(__any(gone != 0))) v.store(v_tile, a.width);
-        else v.store_rows(v_tile, a.width, gone);
+    const auto store = [&](char* to_tile, uint32_t gone) __attribute__((always_inline)) {
+        k.store(to_tile, a.width);
+        if (!rare(__any(gone != 0))) v.store(to_tile + Tl::BYTES, a.width);
+        else v.store_rows(to_tile + Tl::BYTES, a.width, gone);
     };
-    uint32_t turn = 0;                                // of the tile in work: whose places it has
-    if (from < to) {
-        look(from);
-        tell(0);
-        if (from + KEYS < to) {
-            look(from + KEYS);
-            tell(1);
-        }
+    uint32_t turn = 0, buffer = 0;                    // of the tile in work
+    const auto after = [](uint32_t turn) __attribute__((always_inline)) { return turn == 2 ? 0 : turn + 1; };
+    if (from < to && threadIdx.x < 2 * KEYS) {        // the first two tiles'
+        look(from + threadIdx.x, !PREFIX && !bounded);
+        tell(threadIdx.x / KEYS, threadIdx.x % KEYS);
+    }
+    if (PREFIX) {
+        hi_least = lanes_least(own.hi);
+        if (!bounded) hi_most = ~lanes_least(~own.hi);
     }
     __syncthreads();
-    if (from < to) store(fetch(0));
+    if (from < to) store(tiles[0], fetch(0));
     __syncthreads();
     for (uint32_t n0 = from; n0 < to; n0 += KEYS) {
         const bool more = n0 + KEYS < to;
         uint32_t gone = 0;
         if (more) {
-            gone = fetch(turn ^ 1);
-            if (n0 + 2 * KEYS < to) look(n0 + 2 * KEYS);
+            gone = fetch(after(turn));
+            if (n0 + 2 * KEYS < to && threadIdx.x < KEYS) look(n0 + 2 * KEYS + threadIdx.x, false);
         }
+        const char *const k_tile = tiles[buffer], *const v_tile = k_tile + Tl::BYTES;
         // P pieces of 32 keys from piece p0 on, together: their products do not wait for each other
         const auto pieces = [&](auto P, int p0) __attribute__((always_inline)) {
             Acc s[P.value];
 #pragma unroll
             for (int p = 0; p < P.value; ++p) s[p] = Acc{};
+            // Operands are read from LDS all at once, the values' while the scores are in work: left to itself the compiler has each
+            // product wait for the read before it.
+            constexpr bool EARLY = sizeof(T) == 2 && WR > 1;
+            typename Frag<T>::vec rows[EARLY ? 2 * DB : 1][P.value], columns[EARLY ? 2 * P.value : 1][DB];
+            if constexpr (EARLY) {
+#pragma unroll
+                for (int c = 0; c < 2 * DB; ++c)
+#pragma unroll
+                    for (int p = 0; p < P.value; ++p) rows[c][p] = Tl::along(k_tile, at_along + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, c);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int c = 0; c < 2 * DB; ++c)
 #pragma unroll
-                for (int p = 0; p < P.value; ++p) mma(Tl::along(k_tile, at_along + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, c), q[c], s[p]);
+                for (int p = 0; p < P.value; ++p)
+                    mma(EARLY ? rows[EARLY ? c : 0][p] : Tl::along(k_tile, at_along + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, c), q[c], s[p]);
+            if constexpr (EARLY) {
+#pragma unroll
+                for (int g = 0; g < 2 * P.value; ++g)
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) columns[g][b] = Tl::across(v_tile, at_across + (p0 + g / 2) * (32 / 4 * Tl::STRIDE), 0, g % 2, b);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             float most = -__builtin_inff();
 #pragma unroll
             for (int p = 0; p < P.value; ++p) {
@@ -292,12 +319,19 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
                 }
                 bool all = kept32 == 0xFFFFFFFFu;
                 if (PREFIX) all &= linear && j0 >= lo_most && j0 + 32 <= hi_least && !a.keep && !(a.skip_self && j0 + 32 >= hi_least);
-                if (!all)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const bool in = (kept32 >> acc_row(r, h) & 1) != 0 && (!PREFIX || shows(a, own, word(r)));
-                        s[p][r] = in ? s[p][r] : -__builtin_inff();
+                if (!all) {
+                    // a bit for each of the lane's keys, formed one by one: sixteen at a time would take their registers from the walk
+                    uint32_t in = kept32 >> 4 * h;    // key 8 (r / 4) + r % 4 of the lane's half
+                    if (PREFIX) {
+                        uint32_t shown = 0;
+#pragma clang loop unroll(disable)
+                        for (uint32_t r = 0; r < 32; ++r)
+                            if (!(r & 4) && shows(a, own, x.word(n + 4 * h + r))) shown |= 1u << r;
+                        in &= shown;
                     }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[p][r] = in >> acc_row(r, 0) & 1 ? s[p][r] : -__builtin_inff();
+                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[p][r]);
             }
@@ -312,7 +346,7 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
             }
             const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
             float sum = 0.f;
-            Acc part[sizeof(T) == 4 ? DB : 1] = {};   // 32 bits: the pieces' sums first, then the whole's: one long chain would lose bits
+            Acc part[EARLY ? 1 : DB] = {};   // 32 bits: the pieces' sums first, then the whole's: one long chain would lose bits
 #pragma unroll
             for (int g = 0; g < 2 * P.value; ++g) {   // 16 keys
                 const int p = g / 2;
@@ -323,8 +357,10 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
                 }
                 const auto w = acc_operand<T>(s[p], g % 2);
 #pragma unroll
-                for (int b = 0; b < DB; ++b)
-                    mma(Tl::across(v_tile, at_across + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, g % 2, b), w, sizeof(T) == 4 ? part[b % (sizeof(T) == 4 ? DB : 1)] : o[b]);
+                for (int b = 0; b < DB; ++b) {
+                    if constexpr (EARLY) mma(columns[g][b], w, o[b]);
+                    else mma(Tl::across(v_tile, at_across + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, g % 2, b), w, part[b]);
+                }
             }
             total += sum;
             if constexpr (sizeof(T) == 4)
@@ -347,10 +383,11 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
             }
         }
         if (more) {
-            __syncthreads();
-            store(gone);
-            if (n0 + 2 * KEYS < to) tell(turn);
-            turn ^= 1;
+            if constexpr (BUFFERS == 1) __syncthreads();
+            else buffer ^= 1;
+            store(tiles[buffer], gone);
+            if (n0 + 2 * KEYS < to && threadIdx.x < KEYS) tell(after(after(turn)), threadIdx.x);
+            turn = after(turn);
             __syncthreads();
         }
     }
