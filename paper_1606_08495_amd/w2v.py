@@ -702,26 +702,35 @@ def rotary_turns(rotated, base=10000.0, scaling="plain", factor=1.0, trained=0, 
     return torch.from_numpy(turns[:rotated // 2].view(np.int64).copy()).to(device)
 
 
+def _at(t, dtype, shape, q, name):
+    """Where a contiguous tensor on the device of q begins."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != q.device or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous tensor of %s on the device of q" % (name, dtype))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must be %s" % (name, list(shape)))
+    return t.data_ptr()
+
+
 def _rotary(turns, halves, gain, q):
-    if turns.dim() != 1 or turns.device != q.device:
-        raise ValueError("turns must be [rotated / 2] on the device of q")
-    return Rotary(2 * turns.numel(), 1 if halves else 0, float(gain), _dev(turns, torch.int64, "turns"))
+    if turns.dim() != 1:
+        raise ValueError("turns must be [rotated / 2]")
+    return Rotary(2 * turns.shape[0], 1 if halves else 0, gain, _at(turns, torch.int64, None, q, "turns"))
 
 
-def _positions(positions, q):
-    if positions is None:
-        return None
-    if positions.shape != (q.shape[0],) or positions.device != q.device:
-        raise ValueError("positions must be [tokens] on the device of q")
-    return _dev(positions, IDX, "positions")
+def _as_it_is(x, name):
+    """The heads of the tensor that the others are compared with."""
+    a, b, c = x.stride()
+    if (c != 1 and x.shape[2] > 1) or a < 0 or b < 0:
+        raise ValueError("%s: the elements of a head must lie side by side" % name)
+    return Heads(x.data_ptr(), a, b)
 
 
 def _into(out, x, name):
     """A result of its own making, or the caller's: the tensor and its w2v_heads."""
     n, heads, width = x.shape
     if out is None:
-        out = x.new_empty(x.shape)
-        return out, _dense(out, heads, width)
+        out = torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+        return out, Heads(out.data_ptr(), heads * width, width)
     return out, _heads(out, x, n, heads, name)
 
 
@@ -742,8 +751,8 @@ def rotate(q, turns, k=None, sent_off=None, positions=None, halves=False, gain=1
     T, H, d = q.shape
     with _on(stream, q):
         st, r = _raw_stream(q.device.index), ctypes.byref
-        at = _positions(positions, q)
-        off, n = (None, 0) if sent_off is None else _texts(sent_off, None, q)[:2]
+        at = None if positions is None else _at(positions, IDX, (T,), q, "positions")
+        off, n = (None, 0) if sent_off is None else (_at(sent_off, torch.int64, None, q, "sent_off"), max(sent_off.numel() - 1, 0))
         turned = _rotary(turns, halves, gain, q)
         out, into = _into(out, q, "out")
         G, y, y_into = 0, None, None
@@ -752,33 +761,30 @@ def rotate(q, turns, k=None, sent_off=None, positions=None, halves=False, gain=1
             y = r(_heads(k, q, T, G, "k"))
             k_out, y_into = _into(k_out, k, "k_out")
             y_into = r(y_into)
-        _check(lib().w2v_rotate(TYPES[q.dtype], d, r(turned), 1 if back else 0, r(_heads(q, q, T, H, "q")), H, y, G, off, n, T, at,
+        _check(lib().w2v_rotate(TYPES[q.dtype], d, r(turned), 1 if back else 0, r(_as_it_is(q, "q")), H, y, G, off, n, T, at,
                                 r(into), y_into, st))
     return out if k is None else (out, k_out)
 
 
-def _pages(t, like, heads, name):
+def _pages(t, like, shape, name):
     """A pool [pages, words of a page, heads, width]."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == like.dtype and t.device == like.device and t.dim() == 4 and
-            t.shape[2] == heads and t.shape[3] == like.shape[2]):
-        raise TypeError("%s must be a CUDA tensor [pages, words, %d, %d] of %s" % (name, heads, like.shape[2], like.dtype))
+    if not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.device != like.device or t.shape != shape:
+        raise TypeError("%s must be a CUDA tensor %s of %s" % (name, list(shape), like.dtype))
     a, b, c, e = t.stride()
-    if (e != 1 and t.shape[3] > 1) or min(a, b, c) < 0:
+    if (e != 1 and shape[3] > 1) or a < 0 or b < 0 or c < 0:
         raise ValueError("%s: the elements of a head must lie side by side" % name)
     return Pages(t.data_ptr(), a, b, c)
 
 
-def _table(table, n, k_pages, v_pages, q):
-    if k_pages.shape[:2] != v_pages.shape[:2]:
-        raise ValueError("k_pages and v_pages differ in their pages")
-    if not isinstance(table, torch.Tensor) or table.dtype != IDX or table.dim() != 2 or table.device != q.device:
+def _table(table, n, shape, q):
+    """The table, and where n begins."""
+    if not isinstance(table, torch.Tensor) or table.dtype is not IDX or table.dim() != 2 or table.device != q.device:
         raise TypeError("table must be a CUDA tensor [texts, slots] of int32 on the device of q")
-    if table.stride(1) != 1 and table.shape[1] > 1 or table.stride(0) < 0:
+    texts, slots = table.shape
+    a, b = table.stride()
+    if (b != 1 and slots > 1) or a < 0:
         raise ValueError("table: the pages of a text must lie side by side")
-    if n.shape != (table.shape[0],) or n.device != q.device:
-        raise ValueError("n must be [texts] on the device of q")
-    return PageTable(table.data_ptr(), table.stride(0), _number(table.shape[1], "slots"), _number(k_pages.shape[1], "words of a page"),
-                     _number(k_pages.shape[0], "pages"))
+    return PageTable(table.data_ptr(), a, min(slots, UNBOUNDED), min(shape[1], UNBOUNDED), min(shape[0], UNBOUNDED)), _at(n, IDX, (texts,), q, "n")
 
 
 def pages_append(k, v, k_pages, v_pages, table, n, sent_off=None, turns=None, positions=None, halves=False, gain=1.0, q=None,
@@ -798,21 +804,25 @@ def pages_append(k, v, k_pages, v_pages, table, n, sent_off=None, turns=None, po
     T, G, d = k.shape
     with _on(stream, k):
         st, r = _raw_stream(k.device.index), ctypes.byref
-        spec = _table(table, n, k_pages, v_pages, k)
-        if sent_off is not None and sent_off.numel() != table.shape[0] + 1:
-            raise ValueError("sent_off must have %d entries" % (table.shape[0] + 1))
-        off = None if sent_off is None else _texts(sent_off, None, k)[0]
+        if k_pages.dim() != 4:
+            raise TypeError("k_pages must be [pages, words of a page, kv_heads, width]")
+        shape = torch.Size((*k_pages.shape[:2], G, d))
+        spec, count = _table(table, n, shape, k)
+        texts = table.shape[0]
+        off = None
+        if sent_off is not None:
+            off = _at(sent_off, torch.int64, (texts + 1,), k, "sent_off")
         turned = None if turns is None else r(_rotary(turns, halves, gain, k))
-        at = _positions(positions, k)
+        at = None if positions is None else _at(positions, IDX, (T,), k, "positions")
         H, x, into = 0, None, None
         if q is not None:
             H = q.shape[1]
             x = r(_heads(q, k, T, H, "q"))
             q_out, into = _into(q_out, q, "q_out")
             into = r(into)
-        _check(lib().w2v_pages_append(TYPES[k.dtype], d, turned, r(_heads(k, k, T, G, "k")), r(_heads(v, k, T, G, "v")), G, x, H, into,
-                                      off, table.shape[0], T, _dev(n, IDX, "n"), at, r(spec), r(_pages(k_pages, k, G, "k_pages")),
-                                      r(_pages(v_pages, k, G, "v_pages")), st))
+        _check(lib().w2v_pages_append(TYPES[k.dtype], d, turned, r(_as_it_is(k, "k")), r(_heads(v, k, T, G, "v")), G, x, H, into,
+                                      off, texts, T, count, at, r(spec), r(_pages(k_pages, k, shape, "k_pages")),
+                                      r(_pages(v_pages, k, shape, "v_pages")), st))
     return q_out
 
 
@@ -822,25 +832,28 @@ def attend_pages(q, k_pages, v_pages, table, n, shared=0, left=None, sinks=0, sk
     int32 [texts, slots], n int32 [texts] words each (the newest among them).  The first ``shared`` words of all texts lie in the pages of
     the table's row 0.  keep: uint8 [texts, slots * words of a page].  ``workspace``: optional uint8 device tensor to reuse.  Other
     arguments as for ``attend_step``."""
-    if q.dim() != 3 or k_pages.dim() != 4 or v_pages.dim() != 4:
+    if q.dim() != 3 or k_pages.dim() != 4:
         raise TypeError("q must be [texts, heads, width], k_pages and v_pages [pages, words, heads, width]")
     B, H, d = q.shape
-    G = k_pages.shape[2]
+    shape = k_pages.shape
     with _on(stream, q):
         st, r = _raw_stream(q.device.index), ctypes.byref
-        pages = _table(table, n, k_pages, v_pages, q)
-        if table.shape[0] != B:
-            raise ValueError("table must have a row for each of %d texts" % B)
-        if keep is not None and (keep.shape != (B, table.shape[1] * k_pages.shape[1]) or keep.device != q.device):
-            raise ValueError("keep must be [texts, slots * words of a page] on the device of q")
-        spec = _spec(q, G, left, 0, sinks, skip_self, scale, bias, buckets)
+        pages, count = _table(table, n, shape, q)
+        if table.shape[0] != B or shape[3] != d:
+            raise ValueError("table must have a row for each of %d texts, the pools heads of %d" % (B, d))
+        if keep is not None:
+            keep = _at(keep, torch.uint8, (B, table.shape[1] * shape[1]), q, "keep")
+        spec = _spec(q, shape[2], left, 0, sinks, skip_self, scale, bias, buckets)
         shared = _number(shared, "shared")
         out, into = _into(out, q, "out")
+        at = size = 0
         if workspace is None:
-            need = int(lib().w2v_attend_pages_workspace(r(spec), B, r(pages), shared))
-            workspace = q.new_empty(max(need, 256), dtype=torch.uint8)
-        at, size = _room(workspace, q.device)
-        _check(lib().w2v_attend_pages(r(spec), r(_heads(q, q, B, H, "q")), r(_pages(k_pages, q, G, "k_pages")),
-                                      r(_pages(v_pages, q, G, "v_pages")), r(pages), shared, _dev(n, IDX, "n"), B,
-                                      _dev(keep, torch.uint8, "keep"), r(into), at, size, st))
+            size = lib().w2v_attend_pages_workspace(r(spec), B, r(pages), shared)
+            if size:
+                workspace = q.new_empty(size, dtype=torch.uint8)
+                at = workspace.data_ptr()
+        else:
+            at, size = _room(workspace, q.device)
+        _check(lib().w2v_attend_pages(r(spec), r(_as_it_is(q, "q")), r(_pages(k_pages, q, shape, "k_pages")),
+                                      r(_pages(v_pages, q, shape, "v_pages")), r(pages), shared, count, B, keep, r(into), at, size, st))
     return out
