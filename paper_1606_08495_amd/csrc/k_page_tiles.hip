@@ -346,7 +346,8 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
             }
             const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
             float sum = 0.f;
-            Acc part[EARLY ? 1 : DB] = {};   // 32 bits: the pieces' sums first, then the whole's: one long chain would lose bits
+            constexpr bool PARTS = sizeof(T) == 4;
+            Acc part[PARTS ? DB : 1] = {};            // 32 bits: the pieces' sums first, then the whole's: one long chain would lose bits
 #pragma unroll
             for (int g = 0; g < 2 * P.value; ++g) {   // 16 keys
                 const int p = g / 2;
@@ -358,12 +359,13 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
                 const auto w = acc_operand<T>(s[p], g % 2);
 #pragma unroll
                 for (int b = 0; b < DB; ++b) {
-                    if constexpr (EARLY) mma(columns[g][b], w, o[b]);
-                    else mma(Tl::across(v_tile, at_across + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, g % 2, b), w, part[b]);
+                    Acc& into = PARTS ? part[PARTS ? b : 0] : o[b];
+                    if constexpr (EARLY) mma(columns[g][b], w, into);
+                    else mma(Tl::across(v_tile, at_across + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, g % 2, b), w, into);
                 }
             }
             total += sum;
-            if constexpr (sizeof(T) == 4)
+            if constexpr (PARTS)
 #pragma unroll
                 for (int b = 0; b < DB; ++b) o[b] += part[b];
         };
