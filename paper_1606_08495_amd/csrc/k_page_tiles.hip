@@ -377,11 +377,12 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
         if constexpr (WK == 2) {
             if (needs(wk)) pieces(std::integral_constant<int, 1>{}, wk);
         } else {
-            const bool first_piece = needs(0), second_piece = needs(1);
-            if (JOINT && first_piece && second_piece) pieces(std::integral_constant<int, JOINT ? 2 : 1>{}, 0);
+            const bool joint = JOINT && needs(0) && needs(1);
+            if (joint) pieces(std::integral_constant<int, JOINT ? 2 : 1>{}, 0);
             else {
-                if (first_piece) pieces(std::integral_constant<int, 1>{}, 0);
-                if (second_piece) pieces(std::integral_constant<int, 1>{}, 1);
+#pragma clang loop unroll(disable)
+                for (int p = 0; p < 2; ++p)
+                    if (needs(p)) pieces(std::integral_constant<int, 1>{}, p);
             }
         }
         if (more) {
@@ -515,10 +516,10 @@ template <typename T> void tiles_any(const StepArgs& a, uint32_t type, bool pref
 
 }  // namespace
 
-// Blocks enough to fill the device twice over, of at least 128 words each.
+// Blocks enough to fill the device twice over, of at least a tile each.
 uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t shared) {
     const uint32_t rows = batch * (heads / kv_heads), per_block = prefix_rows(type, rows);
-    const uint32_t blocks = (rows + per_block - 1) / per_block * kv_heads, most = (shared + 127) / 128;
+    const uint32_t blocks = (rows + per_block - 1) / per_block * kv_heads, most = (shared + KEYS - 1) / KEYS;
     const uint32_t want = blocks < 512 ? (512 + blocks - 1) / blocks : 1;
     return want < most ? want : most;
 }

@@ -5,10 +5,11 @@
 namespace w2v {
 namespace {
 
-// In 16 bits and with heads that share keys the texts' own words go through the matrix cores: 32 rows of queries, however few are
-// real, cost less than the conversions and multiply-adds of each head on the vector units (four heads of 128 over 574335 words: 456 us,
-// 505).  A key head of one query head is taken by the vector units (48 windows of 1024, six heads of 100: 37 us, 51), and so are 32 bits.
-bool own_tiles(uint32_t type, uint32_t group) { return type != ELEM_F32 && group > 1; }
+// In 16 bits the texts' own words go through the matrix cores where three query heads or more share a key head: their 32 rows of
+// queries, however few are real, then cost less than the conversions and multiply-adds of each head on the vector units.  32 texts
+// of up to 8192 words, 8 key heads of 128: 140, 150, 175 and 305 us for one, two, three and eight query heads each on the vector units,
+// 138 to 155 on the matrix cores; 48 texts of up to 1000, 6 of 100: 25, 30, 40 and 68, and 35 to 37.
+bool own_tiles(uint32_t type, uint32_t group) { return type != ELEM_F32 && group > 2; }
 
 template <typename T> void pages_any(const StepArgs& a, uint32_t type, hipStream_t st) {
     if (a.front) launch_prefix(a, type, st);
@@ -18,13 +19,18 @@ template <typename T> void pages_any(const StepArgs& a, uint32_t type, hipStream
 }
 
 // A prefix is taken by blocks of its own where reading it once for each text would move this many bytes more: below, their launch and
-// the join cost more than reading it from the caches.
-constexpr uint64_t PREFIX_BYTES = 64 << 20;
+// the join cost more than reading it from the caches.  24 texts in 32 bits, 8 heads of 64: 92 MB more (1024 words) 22 us with
+// blocks of its own and 19 without, 368 MB 23 and 33; 8 texts in 16 bits, 8 key heads of 128: 112 MB 30 and 29, 448 MB 41 and 65.
+constexpr uint64_t PREFIX_BYTES = 128 << 20;
 
 }  // namespace
 
-// Of the texts' own words a block has 512 at least (fewer cost a join that is longer than what they save), or 1024 of the vector units' where
-// there is a block for every compute unit without a split; and blocks are enough to fill the device several times over.
+// How many parts a text's own words are taken in.  The vector units' blocks have 512 words at least, or 1024 where there is a block for
+// every compute unit without a split (48 texts behind windows of 1028, 6 heads of 100: 29 us in one part, 31 to 35 in more), and are
+// enough to fill the device several times over.  The matrix cores' have 128 at least and fill it once, but of long texts, which may
+// be of unequal length, 1024 (16 texts of up to 3000 words, 4 key heads of 96: 23 us in parts of 128 to 192, 32 of 512).
+// Up to 512 words are not split: the join's launch costs more (500 words: 14 us, 17 in parts).  Behind a prefix with blocks of its own, where
+// there is a join in any case, parts are shorter.
 PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t width, uint32_t room, uint32_t shared,
                        uint32_t left, uint32_t sinks) {
     PageSplits p{};
@@ -35,9 +41,16 @@ PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t k
     const uint64_t rest = room > p.begin ? room - p.begin : 1, rows = (uint64_t)batch * kv_heads;
     const uint64_t shown = (uint64_t)left + 1 + sinks < rest ? (uint64_t)left + 1 + sinks : rest;
     const bool tiles = own_tiles(type, heads / kv_heads);
-    const uint64_t least = !tiles && rows >= 256 ? 1024 : 512;
-    uint64_t want = (tiles ? 8192 : 4096) / rows;
-    if (want > shown / least) want = shown / least;
+    uint64_t want;
+    if (tiles) {
+        const uint64_t whole = 1024 / rows, longer = 8192 / rows < shown / 1024 ? 8192 / rows : shown / 1024;
+        want = whole > longer ? whole : longer;
+        if (want > shown / 128) want = shown / 128;
+        if (shown <= 512 && !p.front) want = 1;
+    } else {
+        const uint64_t least = p.front ? 256 : rows >= 256 ? 1024 : 512;
+        want = 4096 / rows < shown / least ? 4096 / rows : shown / least;
+    }
     if (want < 1) want = 1;
     const uint64_t per = ((shown + want - 1) / want + 63) / 64 * 64;
     p.own = StepSplits{(uint32_t)((shown + per - 1) / per), (uint32_t)per};
