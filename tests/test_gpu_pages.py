@@ -7,10 +7,9 @@ import pytest
 import torch
 
 from attend_reference import check
-from pages_reference import as_int32, gather, scatter
+from pages_reference import as_int32, gather, last_rows, scatter
 from paper_1606_08495_amd import w2v
 from rotary_reference import rotate_reference, within
-from test_gpu_step import expected
 
 F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
 i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
@@ -148,7 +147,7 @@ def run(n, page_words, H, G, d, ty, seed=0, buckets=None, span=None, drop=0.0, s
     bmap = w2v.relative_buckets(buckets, span, device="cpu") if buckets else None
     keep = (torch.rand(B, slots * page_words, generator=g) >= drop).to(torch.uint8) if drop else None
     k, v, kept, counts = gather(k_pages, v_pages, table, n, keep, shared)
-    ref = expected(q, k, v, counts, kept, bias, bmap, **see)
+    ref = last_rows(q, k, v, counts, kept, bias, bmap, **see)
     cuda = lambda t: None if t is None else t.cuda()
     out = w2v.attend_pages(q.cuda(), k_pages.cuda(), v_pages.cuda(), table.cuda(), i32(n), shared=shared, keep=cuda(keep), bias=cuda(bias),
                            buckets=cuda(bmap), **see)
