@@ -18,7 +18,8 @@ namespace w2v {
 namespace {
 
 constexpr uint32_t THREADS = 256, TOKENS = 16, PAIRS = HEAD_MAX / 2;
-constexpr int AHEAD = 4;
+// Rows that a thread asks for before it works on any (with a partner's chunk for each, half as many).
+template <bool HALVES> constexpr int ahead = HALVES ? 2 : 4;
 constexpr uint64_t NOWHERE = ~0ull;
 
 __device__ __forceinline__ float2 cos_sin(uint64_t phase) {
@@ -86,13 +87,19 @@ template <typename T, int N> __device__ __forceinline__ void part_write(T* row, 
     for (int e = 0; e < N; ++e) if (e < (int)some) row[e] = v[e];
 }
 
+// Chunks of a row that a thread has one of.
+__host__ __device__ __forceinline__ uint32_t row_units(bool halves, uint32_t width, uint32_t turned, uint32_t n) {
+    return halves ? (turned / 2 + n - 1) / n + (width - turned + n - 1) / n : (width + n - 1) / n;
+}
+
 // All rows of one array of the block's words.
 template <typename T, int N, bool HALVES>
 __device__ __forceinline__ void walk(const TurnArgs& a, const TurnArray& x, uint32_t turned, const uint64_t* to, const Words& w,
                                      uint32_t word0, uint32_t count) {
     typedef typename Pack<T, N>::vec vec;
+    constexpr int AHEAD = ahead<HALVES>;
     const uint32_t half = turned / 2, paired = HALVES ? (half + N - 1) / N : 0;      // chunks that have a partner in the other half
-    const uint32_t units = HALVES ? paired + (a.width - turned + N - 1) / N : (a.width + N - 1) / N;
+    const uint32_t units = row_units(HALVES, a.width, turned, N);
     const uint32_t step = THREADS / units, unit = threadIdx.x % units, first = threadIdx.x / units;
     if (first >= step) return;
     const bool pair = HALVES && unit < paired;
@@ -148,10 +155,11 @@ __device__ __forceinline__ void walk(const TurnArgs& a, const TurnArray& x, uint
 template <typename T, bool HALVES, bool APPEND> __global__ __launch_bounds__(THREADS) void turn_kernel(const TurnArgs a) {
     constexpr int N = pack16<T>;
     __shared__ Words w;
-    const uint32_t word0 = blockIdx.x * a.tokens, count = a.T - word0 < a.tokens ? a.T - word0 : a.tokens;
+    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, pairs = a.rotated / 2;
+    if (block > (a.T - 1) / a.tokens) return;
+    const uint32_t word0 = block * a.tokens, count = a.T - word0 < a.tokens ? a.T - word0 : a.tokens;
     place<APPEND>(a, w, word0, count);
     __syncthreads();
-    const uint32_t pairs = a.rotated / 2;
     for (uint32_t n = threadIdx.x; n < count * pairs; n += THREADS) {
         const uint32_t word = n / pairs, c = n % pairs;
         const float2 t = cos_sin((uint64_t)w.position[word] * a.turns[c]);
@@ -164,13 +172,20 @@ template <typename T, bool HALVES, bool APPEND> __global__ __launch_bounds__(THR
 }
 
 template <typename T, bool APPEND> void turn_run(const TurnArgs& a, hipStream_t st) {
-    const uint32_t blocks = (a.T + a.tokens - 1) / a.tokens;
+    const uint32_t all = (a.T + a.tokens - 1) / a.tokens, wide = all < 1u << 23 ? all : 1u << 23;      // (threads on an axis: below 2^32)
+    const dim3 blocks(wide, (all + wide - 1) / wide);
     if (a.halves) turn_kernel<T, true, APPEND><<<blocks, THREADS, 0, st>>>(a);
     else turn_kernel<T, false, APPEND><<<blocks, THREADS, 0, st>>>(a);
 }
+// Words of a block: as many as fill the threads twice over with the rows of the array that has most heads, or once if that is more than
+// a block holds; fewer where there are few words.  (131333 words of 5 + 5 heads of 60 in 32 bits: 13 words a block 123 us, 8 140, 16 131;
+// 39955 of 16 + 4 of 128 in 16 bits, in halves: 5 words 84 us, 3 93, 16 91.)
 template <bool APPEND> void turn_any(TurnArgs& a, uint32_t type, hipStream_t st) {
-    a.tokens = (a.T + 2047) / 2048;
-    if (a.tokens > TOKENS) a.tokens = TOKENS;
+    const uint32_t units = row_units(a.halves, a.width, a.rotated, 16 / elem_bytes(type)), heads = a.x.heads > a.y.heads ? a.x.heads : a.y.heads;
+    const uint32_t rows = THREADS / units * (a.halves ? ahead<true> : ahead<false>), twice = 2 * rows / heads, few = (a.T + 2047) / 2048;
+    a.tokens = twice <= TOKENS ? twice : rows / heads < TOKENS ? rows / heads : TOKENS;
+    if (a.tokens > few) a.tokens = few;
+    if (a.tokens < 1) a.tokens = 1;
     if (type == ELEM_F32) turn_run<float, APPEND>(a, st);
     else if (type == ELEM_F16) turn_run<_Float16, APPEND>(a, st);
     else turn_run<__bf16, APPEND>(a, st);

@@ -48,6 +48,20 @@ def test_numbers_of_words(tokens):
 
 
 @pytest.mark.gpu
+def test_more_words_than_a_launch_has_blocks_for():
+    """2^23 blocks of 16 words, and some: more than one axis of a launch takes."""
+    T, turns = (1 << 27) + 12_345, w2v.rotary_turns(2)
+    x = torch.randn(1000, 1, 2, device="cuda").to(F16).repeat(T // 1000 + 1, 1, 1)[:T]
+    at = torch.arange(T, dtype=torch.int32, device="cuda") % 5000
+    got = w2v.rotate(x, turns, positions=at)
+    for a in (0, (1 << 27) - 5000, T - 20_000):
+        some = slice(a, a + 20_000)
+        within(got[some], *rotate_reference(x[some].cpu(), at[some].long().cpu(), turns.cpu()))
+    first = got[:5000]                                         # 5000 words on, the same words at the same positions
+    assert torch.equal(got[:T // 5000 * 5000].view(-1, 5000, 2), first.view(1, 5000, 2).expand(T // 5000, -1, -1))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("halves", [False, True])
 def test_far_and_negative_positions(halves):
     at = torch.tensor([0, 1, -1, 100_003, -100_003, 2 ** 30, 2 ** 31 - 1, -2 ** 31, 12_345_678] * 5, dtype=torch.int32)
