@@ -1,14 +1,22 @@
-// Attention of the newest words of many texts over the words that all texts begin with, which lie in pages once.
+// Attention of the newest words of texts over pages on the matrix cores: over the words that all texts begin with, which lie in pages
+// once, and in 16 bits over a text's own words.
 //
 // For a key head the queries of all texts and of the heads that share it are the rows of one product with the prefix's keys,
-// and their weights those of one with its values: the prefix is read once for 32 WR rows and not once for each.  Pages are looked up
-// and rows staged in LDS by tiles of 64 words, as in attention over texts: scores transposed (keys are rows, a query is a lane), the maximum
-// and sum of a query in its two lanes, weights fed to the second product from the registers they are in.  WR wavefronts have 32
-// queries each; with WK = 2 two of them share queries and take a half of every tile each.  A block has a part of the prefix and leaves
-// (maximum, sum, output) of its queries over it in the workspace, where the join finds them beside those of the texts' own words.
+// and their weights those of one with its values: the prefix is read once for 32 WR rows and not once for each.  Of a text's own words the
+// rows are the few heads that share a key head; the rest of the 32 is padding, which costs less than the vector units' work.
+// Rows are staged in LDS by tiles of 64 words, whose places a thread each looks up in the table of pages two tiles ahead.  As in attention
+// over texts scores are transposed (keys are rows, a query is a lane), the maximum and sum of a query lie in its two lanes, and weights
+// feed the second product from the registers they are in.  WR wavefronts have 32 queries each; with WK = 2 two of them share
+// queries and take a half of every tile each.  A block has a part of the words and leaves (maximum, sum, output) of its queries over it in
+// the workspace, where the join finds them (step.h).
 //
 // Scores, maxima, sums and outputs are fp32; weights are rounded to the type of v for the second product, relative to the row's maximum
 // (fp16: lifted by a power of two, so that small ones keep their bits), and summed before that.
+//
+// What bounds it: a text's own words memory (32 texts of 574335 words, 32 heads of 128 over 8, 16 bits: 448 us, 5.3 TB/s; two wavefronts a
+// block, four blocks a CU take turns).  The prefix, where many queries share it, its two products and the exponentials, with
+// two wavefronts a SIMD: 64 texts behind 32768 words, the same heads, 72 us (34 GFLOP, 480 TFLOP/s; the loads alone take 48, the
+// products alone 60), and 43 us for their own 33000 words.  24 texts behind 4096 words in 32 bits, 8 heads of 64, bias: 15 us.
 #include <type_traits>
 
 #include "attend.h"

@@ -275,7 +275,8 @@ template <typename T> __global__ __launch_bounds__(THREADS) void step_join_kerne
 }
 
 // The same over pages, where a row may have many parts: a block per text and head.  A part's columns lie in L lanes, four each, so
-// the block reads 256 / L parts at a time; what the groups of lanes have summed is added in their order.
+// the block reads 256 / L parts at a time; what the groups of lanes have summed is added in their order.  (2048 rows of 34 parts of 128
+// columns: 9 us; a wavefront a row, one part after the other, took 28.)
 template <typename T> __global__ __launch_bounds__(THREADS) void pages_join_kernel(const StepArgs a, uint32_t L) {
     extern __shared__ float factors[];                // of each part
     __shared__ float waves[2][WAVES], sums[THREADS][4];
