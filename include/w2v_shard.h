@@ -443,10 +443,11 @@ int w2v_attend_step(const w2v_attend_spec* spec, const w2v_heads* q, const w2v_c
  * base > 1 and factor >= 1 finite, 0 <= low < high, trained > 0 (these three are read for W2V_ROTARY_PARTS alone).
  *
  * w2v_rotate turns x and, if y is not NULL, y (queries and keys of the same words) into x_out and y_out, which may be x and
- * y; outputs that otherwise overlap inputs, themselves or each other are refused.  A word's position is its place in its text by
- * sent_off_dev[n_sent + 1], as for w2v_attend, or position_dev[n_tokens] (int32, negative ones too) where that is not NULL; sent_off_dev is
- * not read then.  Words that no text has are left as they were in the outputs.  back: by the angles' negatives, gain as
- * before, which gives the gradients by x and y from those by x_out and y_out.  Nothing is allocated or synchronised. */
+ * y; outputs that otherwise overlap inputs, themselves or each other are refused, and so are those that lie among them with other
+ * strides.  A word's position is its place in its text by sent_off_dev[n_sent + 1], as for w2v_attend, or position_dev[n_tokens] (int32,
+ * negative ones too) where that is not NULL; sent_off_dev is not read then.  Words that no text has are left as they were in the
+ * outputs.  back: by the angles' negatives, gain as before, which gives the gradients by x and y from those by x_out and y_out.
+ * Nothing is allocated or synchronised. */
 #define W2V_ROTARY_PLAIN  0
 #define W2V_ROTARY_LINEAR 1
 #define W2V_ROTARY_BASE   2
@@ -475,7 +476,8 @@ int w2v_rotate(int type, uint32_t width, const w2v_rotary* rotary, int back, con
  * text's first or past its room are not kept.  k (turned by the word's number in its text, or by position_dev, unless rotary is NULL)
  * and v go into the pages; q, if not NULL, is turned alike into q_out (which may be q).  Words that no text has, and all other
  * places of the pools, are left as they were.  Two words at one place of the pools: one of them is kept, element by element.  A place that
- * another text's row lists too (a common prefix) is written for both.  Pools that overlap each other or an input are refused.
+ * another text's row lists too (a common prefix) is written for both.  Pools that overlap each other or an input, or lie among them with
+ * other strides, are refused.
  *
  * w2v_attend_pages gives what w2v_attend_step does, over pages: spec, n_dev, q and out are as there (out may be q),
  * keep_dev is [batch][slots * page_words].  shared (a multiple of page_words, at most the room; 0: none): the first `shared` words of all

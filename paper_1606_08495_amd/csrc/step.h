@@ -43,10 +43,10 @@ template <bool PAGED> __device__ inline Keys step_keys(const StepArgs& a, uint32
 // Wavefronts a SIMD that the registers are held to: what the plain walk needs by itself.
 template <typename T, int HEADS> constexpr int step_waves = (HEADS == 1 ? 5 : HEADS == 2 ? 4 : HEADS == 4 ? 3 : 2) + (sizeof(T) == 4);
 
-// PAGED: where a row lies is looked up in the table of pages, one step ahead of the rows.
-template <typename T, int L, int HEADS, bool PAGED>
-__global__ __launch_bounds__(THREADS, (step_waves<T, HEADS>)) void step_kernel(const StepArgs a) {
-    constexpr int N = pack16<T>, GROUPS = WAVE / L;
+// PAGED: where a row lies is looked up in the table of pages, one step ahead of the rows.  WAVES wavefronts a block.
+template <typename T, int L, int HEADS, bool PAGED, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (step_waves<T, HEADS>)) void step_kernel(const StepArgs a) {
+    constexpr int N = pack16<T>, GROUPS = WAVE / L, THREADS = 64 * WAVES;
     typedef typename Pack<T, N>::vec vec;
     extern __shared__ float dynamic[];                // bias by distance 0 .. -span for each head, times log2 e
     __shared__ float joined[WAVES][HEADS][L * N + 2];
@@ -334,7 +334,13 @@ template <typename T> __global__ __launch_bounds__(THREADS) void pages_join_kern
 template <typename T, int L, int HEADS, bool PAGED> void step_run(const StepArgs& a, hipStream_t st) {
     const uint32_t rounds = (a.group + HEADS - 1) / HEADS;
     const size_t table = a.bias ? (size_t)(a.span + 1) * HEADS * sizeof(float) : 0;
-    step_kernel<T, L, HEADS, PAGED><<<a.batch * a.kv_heads * rounds * a.splits, THREADS, table, st>>>(a);
+    const uint32_t blocks = a.batch * a.kv_heads * rounds * a.splits;
+    if constexpr (PAGED) {
+        // Fewer blocks than compute units, each with all of its text's words: twice the wavefronts, whose rows are on their way at the same
+        // time (500 words, 5 heads of 60 in 32 bits: 9.2 us, 12.4; with more blocks than that it costs: 288 of 1028 words 37 us, 33).
+        if (a.front + a.splits == 1 && blocks <= 256) return step_kernel<T, L, HEADS, true, 2 * WAVES><<<blocks, 2 * THREADS, table, st>>>(a);
+    }
+    step_kernel<T, L, HEADS, PAGED, WAVES><<<blocks, THREADS, table, st>>>(a);
 }
 template <typename T, int L, bool PAGED> void step_heads(const StepArgs& a, hipStream_t st) {
     if (a.group == 1) step_run<T, L, 1, PAGED>(a, st);

@@ -107,6 +107,45 @@ def test_append_many_words_and_rows_no_text_has():
 
 
 @pytest.mark.gpu
+def test_append_two_words_to_one_place():
+    """Texts that list the same page, and a row of the table that lists one page twice: each element is one of the two words'."""
+    k, v = torch.randn(40, 2, 36, device="cuda"), torch.randn(40, 2, 36, device="cuda")
+    pools = [torch.zeros(5, 8, 2, 36, device="cuda") for _ in range(2)]
+    w2v.pages_append(k, v, *pools, i32([[3, 1, 3], [3, 0, 2]]), i32([20, 20]), sent_off=torch.tensor([0, 20, 40]).cuda())
+    for pool, x in zip(pools, (k, v)):
+        for place in range(8):
+            writers = [place, 20 + place] + ([16 + place] if place < 4 else [])
+            assert (pool[3, place][None] == x[writers]).any(0).all()
+        assert torch.equal(pool[1], x[8:16]) and torch.equal(pool[0], x[28:36]) and torch.equal(pool[2, :4], x[36:40])
+        assert (pool[4] == 0).all() and (pool[2, 4:] == 0).all()
+    q = torch.randn(2, 4, 36, device="cuda")                     # read: both texts' words, some twice
+    got = w2v.attend_pages(q, *pools, i32([[3, 1, 3], [3, 0, 2]]), i32([20, 20]))
+    for b, pages in enumerate(([3, 1, 3], [3, 0, 2])):
+        flat = [p[pages].flatten(0, 1)[None] for p in pools]
+        want = w2v.attend_step(q[b:b + 1], *flat, i32([20]))
+        assert torch.allclose(got[b], want[0], atol=1e-5)
+
+
+@pytest.mark.gpu
+def test_calls_on_two_streams_at_once():
+    """Calls that share inputs and nothing else: results and workspaces of their own."""
+    words, G, d = 16, 2, 64
+    pool = torch.randn(300, words, G, d, device="cuda").to(BF16)
+    table, n = torch.randperm(300, device="cuda")[:288].view(4, 72).to(torch.int32), i32([1100, 900, 17, 1152])
+    q = torch.randn(4, 8, d, device="cuda").to(BF16)
+    want = w2v.attend_pages(q, pool, pool, table, n)
+    turns, off = w2v.rotary_turns(64), torch.tensor([0, 4]).cuda()
+    turned = w2v.rotate(q, turns, sent_off=off)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for i in range(20):
+        got.append((w2v.attend_pages(q, pool, pool, table, n, stream=streams[i % 2]), w2v.rotate(q, turns, sent_off=off, stream=streams[1 - i % 2])))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want) and torch.equal(b, turned) for a, b in got)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("ty", [F32, BF16])
 def test_append_strides_in_place_and_another_stream(ty):
     B, H, G, d, words, pages = 5, 4, 2, 20, 16, 12
