@@ -10,8 +10,8 @@
 // heads of 128, half of each turned, 16 bits, there and back: 167 us (4.9 TB/s).  26016 words of 40 prompts into pages, 32 query heads and 8
 // keys and values of 128, 16 bits: 124 us (5.2 TB/s).  One word: 5 us, of which the launch is most.
 //
-// An angle is a whole number of 2^-64 turns times the position, modulo 2^64: exact, whatever the position.  Its nearest quarter turn
-// is taken off as a whole number too, and what is left, at most an eighth of a turn, goes through the power series of sine and
+// An angle is a whole number of 2^-64 turns times the position, modulo 2^64: exact, whatever the position.  Of its upper 32 bits (2^-32
+// of a turn is 1.5e-9) the nearest quarter turn is taken off as a whole number too, and what is left, at most an eighth of a turn, goes through the power series of sine and
 // cosine, whose first terms left out are below 2^-25 there.  All products are fp32, the result is rounded once.
 #include <type_traits>
 
