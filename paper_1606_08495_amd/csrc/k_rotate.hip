@@ -11,8 +11,9 @@
 // keys and values of 128, 16 bits: 124 us (5.2 TB/s).  One word: 5 us, of which the launch is most.
 //
 // An angle is a whole number of 2^-64 turns times the position, modulo 2^64: exact, whatever the position.  Of its upper 32 bits (2^-32
-// of a turn is 1.5e-9) the nearest quarter turn is taken off as a whole number too, and what is left, at most an eighth of a turn, goes through the power series of sine and
-// cosine, whose first terms left out are below 2^-25 there.  All products are fp32, the result is rounded once.
+// of a turn is 1.5e-9) the nearest quarter turn is taken off as a whole number too, and what is left, at most an eighth of a turn,
+// goes through the power series of sine and cosine, whose first terms left out are below 2^-25 there.  All products are fp32, the
+// result is rounded once.
 #include <type_traits>
 
 #include "attend.h"
@@ -20,7 +21,8 @@
 namespace w2v {
 namespace {
 
-constexpr uint32_t THREADS = 256, TOKENS = 16, PAIRS = HEAD_MAX / 2;
+constexpr uint32_t THREADS = 256, TOKENS = 64, ANGLES = 1024;      // words of a block, and words times pairs, at most
+static_assert(ANGLES >= HEAD_MAX / 2, "one word's");
 // Rows that a thread asks for before it works on any (with a partner's chunk for each, half as many).
 template <bool HALVES> constexpr int ahead = HALVES ? 2 : 4;
 constexpr uint64_t NOWHERE = ~0ull;
@@ -39,7 +41,7 @@ __device__ __forceinline__ float2 cos_sin(uint64_t phase) {
 struct Words {
     int64_t position[TOKENS];
     uint64_t x[TOKENS], y[TOKENS], z[TOKENS];
-    float2 table[TOKENS][PAIRS];
+    float2 table[ANGLES];                             // [words][pairs]
 };
 
 // The text of token i (the same in 16 lanes that look for it together), and whether it has it.
@@ -52,25 +54,27 @@ __device__ __forceinline__ Found find(const TurnArgs& a, uint32_t i, uint32_t la
 }
 
 template <bool APPEND> __device__ __forceinline__ void place(const TurnArgs& a, Words& w, uint32_t word0, uint32_t count) {
-    const uint32_t lane = threadIdx.x % WAVE, slot = threadIdx.x / 16;
-    const uint32_t i = word0 + (slot < count ? slot : count - 1);
-    Found f{i, 0, 1, true};
-    if (APPEND || !a.position) f = find(a, i, lane);
-    int64_t at = f.at;
-    uint64_t y = (uint64_t)i * a.y.out_token, z = 0;
-    if constexpr (APPEND) {
-        at = f.in ? (int64_t)a.n[f.text] - f.behind : 0;
-        uint32_t page = a.n_pages;
-        if (f.in && at >= 0 && at < (int64_t)a.room) page = a.table[(uint64_t)f.text * a.table_stride + ((uint32_t)at >> a.shift)];
-        const uint32_t place = (uint32_t)at & ((1u << a.shift) - 1);
-        y = page < a.n_pages ? page * a.y_page + place * a.y.out_token : NOWHERE;
-        z = page < a.n_pages ? page * a.z_page + place * a.z.out_token : NOWHERE;
+    const uint32_t lane = threadIdx.x % WAVE;
+    for (uint32_t slot = threadIdx.x / 16; slot < (count + 3) / 4 * 4; slot += THREADS / 16) {      // (a wavefront's four words together)
+        const uint32_t i = word0 + (slot < count ? slot : count - 1);
+        Found f{i, 0, 1, true};
+        if (APPEND || !a.position) f = find(a, i, lane);
+        int64_t at = f.at;
+        uint64_t y = (uint64_t)i * a.y.out_token, z = 0;
+        if constexpr (APPEND) {
+            at = f.in ? (int64_t)a.n[f.text] - f.behind : 0;
+            uint32_t page = a.n_pages;
+            if (f.in && at >= 0 && at < (int64_t)a.room) page = a.table[(uint64_t)f.text * a.table_stride + ((uint32_t)at >> a.shift)];
+            const uint32_t place = (uint32_t)at & ((1u << a.shift) - 1);
+            y = page < a.n_pages ? page * a.y_page + place * a.y.out_token : NOWHERE;
+            z = page < a.n_pages ? page * a.z_page + place * a.z.out_token : NOWHERE;
+        }
+        if (lane % 16 || slot >= count) continue;
+        w.position[slot] = a.position ? (int64_t)a.position[i] : at;
+        w.x[slot] = f.in ? (uint64_t)i * a.x.out_token : NOWHERE;
+        w.y[slot] = f.in ? y : NOWHERE;
+        w.z[slot] = z;
     }
-    if (lane % 16 || slot >= count) return;
-    w.position[slot] = a.position ? (int64_t)a.position[i] : at;
-    w.x[slot] = f.in ? (uint64_t)i * a.x.out_token : NOWHERE;
-    w.y[slot] = f.in ? y : NOWHERE;
-    w.z[slot] = z;
 }
 
 // N elements of a row from c0 on, `some` of which are to be had.
@@ -106,12 +110,25 @@ __device__ __forceinline__ void walk(const TurnArgs& a, const TurnArray& x, uint
     const uint32_t step = THREADS / units, unit = threadIdx.x % units, first = threadIdx.x / units;
     if (first >= step) return;
     const bool pair = HALVES && unit < paired;
-    const uint32_t c0 = !HALVES ? unit * N : pair ? unit * N : turned + (unit - paired) * N;
-    const uint32_t some = (pair ? half : a.width) - c0;
+    uint32_t c0 = !HALVES ? unit * N : pair ? unit * N : turned + (unit - paired) * N;
+    uint32_t some = (pair ? half : a.width) - c0;
+    // A chunk that the row's end cuts begins earlier instead and does some of its neighbour's again, where that is nothing that it reads: in
+    // another place than the input's.  (Pairs side by side stay together: the last element of an odd width then goes by itself.  Half a GB in 16
+    // bits there and back: rows of 60 in halves 102 us, element by element 266; of 37 in pairs 150, 330.)
+    bool single = false;
+    if (some < (uint32_t)N && x.in.p != x.out) {
+        const uint32_t back = N - some + (!HALVES && a.width % 2), begin = HALVES && !pair ? turned : 0;
+        if (c0 >= begin + back) {
+            c0 -= back;
+            some = N;
+            single = !HALVES && a.width % 2;
+        }
+    }
     const uint32_t step_words = step / x.heads, step_heads = step % x.heads, rows = count * x.heads;
     uint32_t word = first / x.heads, head = first % x.heads;
     for (uint32_t r = first; r < rows; r += AHEAD * step) {
         vec low[AHEAD], high[AHEAD];
+        T last[AHEAD];
         uint32_t words[AHEAD], heads[AHEAD];
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
@@ -120,6 +137,7 @@ __device__ __forceinline__ void walk(const TurnArgs& a, const TurnArray& x, uint
             const T* row = (const T*)x.in.p + (uint64_t)(word0 + words[n]) * x.in.token + (uint64_t)head * x.in.head + c0;
             low[n] = part_read<T, N>(row, some);
             if (pair) high[n] = part_read<T, N>(row + half, some);
+            if (!HALVES && single) last[n] = row[N];
             word += step_words;
             head += step_heads;
             if (head >= x.heads) { head -= x.heads; ++word; }
@@ -129,7 +147,7 @@ __device__ __forceinline__ void walk(const TurnArgs& a, const TurnArray& x, uint
             const uint64_t at = to[words[n]];
             if (r + n * step >= rows || at == NOWHERE) continue;
             T* row = (T*)x.out + at + (uint64_t)heads[n] * x.out_head + c0;
-            const float2* table = w.table[words[n]];
+            const float2* table = w.table + words[n] * half;
             if (pair) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
@@ -151,6 +169,7 @@ __device__ __forceinline__ void walk(const TurnArgs& a, const TurnArray& x, uint
                 }
             }
             part_write<T, N>(row, some, low[n]);
+            if (!HALVES && single) row[N] = last[n];
         }
     }
 }
@@ -164,9 +183,8 @@ template <typename T, bool HALVES, bool APPEND> __global__ __launch_bounds__(THR
     place<APPEND>(a, w, word0, count);
     __syncthreads();
     for (uint32_t n = threadIdx.x; n < count * pairs; n += THREADS) {
-        const uint32_t word = n / pairs, c = n % pairs;
-        const float2 t = cos_sin((uint64_t)w.position[word] * a.turns[c]);
-        w.table[word][c] = make_float2(a.gain * t.x, a.back ? -a.gain * t.y : a.gain * t.y);
+        const float2 t = cos_sin((uint64_t)w.position[n / pairs] * a.turns[n % pairs]);
+        w.table[n] = make_float2(a.gain * t.x, a.back ? -a.gain * t.y : a.gain * t.y);
     }
     __syncthreads();
     if (a.x.heads) walk<T, N, HALVES>(a, a.x, a.rotated, w.x, w, word0, count);
@@ -180,13 +198,14 @@ template <typename T, bool APPEND> void turn_run(const TurnArgs& a, hipStream_t 
     if (a.halves) turn_kernel<T, true, APPEND><<<blocks, THREADS, 0, st>>>(a);
     else turn_kernel<T, false, APPEND><<<blocks, THREADS, 0, st>>>(a);
 }
-// Words of a block: as many as fill the threads twice over with the rows of the array that has most heads, or once if that is more than
-// a block holds; fewer where there are few words.  (131333 words of 5 + 5 heads of 60 in 32 bits: 13 words a block 123 us, 8 140, 16 131;
+// Words of a block: as many as fill the threads with the rows of the array that has most heads, twice over where that is less than four
+// words; fewer where there are few words.  (131333 words of 5 + 5 heads of 60 in 32 bits: 13 words a block 123 us, 8 140, 27 134;
 // 39955 of 16 + 4 of 128 in 16 bits, in halves: 5 words 84 us, 3 93, 16 91.)
 template <bool APPEND> void turn_any(TurnArgs& a, uint32_t type, hipStream_t st) {
     const uint32_t units = row_units(a.halves, a.width, a.rotated, 16 / elem_bytes(type)), heads = a.x.heads > a.y.heads ? a.x.heads : a.y.heads;
-    const uint32_t rows = THREADS / units * (a.halves ? ahead<true> : ahead<false>), twice = 2 * rows / heads, few = (a.T + 2047) / 2048;
-    a.tokens = twice <= TOKENS ? twice : rows / heads < TOKENS ? rows / heads : TOKENS;
+    const uint32_t rows = THREADS / units * (a.halves ? ahead<true> : ahead<false>), few = (a.T + 2047) / 2048;
+    const uint32_t most = a.rotated > 2 * ANGLES / TOKENS ? 2 * ANGLES / a.rotated : TOKENS;
+    a.tokens = rows / heads < 4 ? 2 * rows / heads : rows / heads < most ? rows / heads : most;
     if (a.tokens > few) a.tokens = few;
     if (a.tokens < 1) a.tokens = 1;
     if (type == ELEM_F32) turn_run<float, APPEND>(a, st);

@@ -37,9 +37,9 @@ def test_heads_widths_and_layouts(H, G, d, r, ty):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("tokens", [1, 2, 15, 16, 17, 2048, 2049, 4097, 40000])
+@pytest.mark.parametrize("tokens", [1, 2, 15, 16, 17, 2048, 2049, 4097, 40000, 140000])
 def test_numbers_of_words(tokens):
-    """Blocks of 1 to 16 words, the last one not full; texts of every length up to all words, and many without any."""
+    """Blocks of 1 to 64 words, the last one not full; texts of every length up to all words, and many without any."""
     print("rotate", tokens, flush=True)
     run([0, tokens], 2, 1, 20, 20, F32, halves=True)
     g = torch.Generator().manual_seed(tokens)
@@ -49,12 +49,12 @@ def test_numbers_of_words(tokens):
 
 @pytest.mark.gpu
 def test_more_words_than_a_launch_has_blocks_for():
-    """2^23 blocks of 16 words, and some: more than one axis of a launch takes."""
-    T, turns = (1 << 27) + 12_345, w2v.rotary_turns(2)
+    """2^23 blocks of 64 words, and some: more than one axis of a launch takes."""
+    T, turns = (1 << 29) + 12_345, w2v.rotary_turns(2)
     x = torch.randn(1000, 1, 2, device="cuda").to(F16).repeat(T // 1000 + 1, 1, 1)[:T]
-    at = torch.arange(T, dtype=torch.int32, device="cuda") % 5000
+    at = torch.arange(5000, dtype=torch.int32, device="cuda").repeat(T // 5000 + 1)[:T]
     got = w2v.rotate(x, turns, positions=at)
-    for a in (0, (1 << 27) - 5000, T - 20_000):
+    for a in (0, (1 << 29) - 5000, T - 20_000):
         some = slice(a, a + 20_000)
         within(got[some], *rotate_reference(x[some].cpu(), at[some].long().cpu(), turns.cpu()))
     first = got[:5000]                                         # 5000 words on, the same words at the same positions
