@@ -11,9 +11,11 @@
 // the workspace, where the join finds them (step.h).
 //
 // Scores, maxima, sums and outputs are fp32; weights are rounded to the type of v for the second product, relative to the row's maximum
-// (fp16: lifted by a power of two, so that small ones keep their bits), and summed before that.
+// (fp16: lifted by a power of two, so that small ones keep their bits), and summed before that.  Of a text's own words what the
+// rounding left is multiplied too, where the matrix cores wait for memory anyway (458 us for 455 below); of a prefix that would cost
+// 130 us for 120, and its weights' rounding is left: results 1.35 times as far off as one rounding at the end makes them.
 //
-// What bounds it: a text's own words memory (32 texts of 574335 words, 32 heads of 128 over 8, 16 bits: 448 us, 5.3 TB/s; two wavefronts a
+// What bounds it: a text's own words memory (32 texts of 574335 words, 32 heads of 128 over 8, 16 bits: 452 us, 5.2 TB/s; two wavefronts a
 // block, four blocks a CU take turns).  The prefix, where many queries share it, its two products and the exponentials, with
 // two wavefronts a SIMD: 64 texts behind 32768 words, the same heads, 72 us (34 GFLOP, 480 TFLOP/s; the loads alone take 48, the
 // products alone 60), and 43 us for their own 33000 words.  24 texts behind 4096 words in 32 bits, 8 heads of 64, bias: 15 us.
@@ -354,7 +356,7 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
             }
             const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
             float sum = 0.f;
-            constexpr bool PARTS = sizeof(T) == 4;
+            constexpr bool PARTS = sizeof(T) == 4, REST = sizeof(T) == 2 && !PREFIX;
             Acc part[PARTS ? DB : 1] = {};            // 32 bits: the pieces' sums first, then the whole's: one long chain would lose bits
 #pragma unroll
             for (int g = 0; g < 2 * P.value; ++g) {   // 16 keys
@@ -365,11 +367,16 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
                     sum += s[p][c];
                 }
                 const auto w = acc_operand<T>(s[p], g % 2);
+                typename Frag<T>::vec rest;           // what the rounding left of the weights
+                if constexpr (REST)
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) rest[c] = (T)(s[p][8 * (g % 2) + c] - (float)w[c]);
 #pragma unroll
                 for (int b = 0; b < DB; ++b) {
                     Acc& into = PARTS ? part[PARTS ? b : 0] : o[b];
-                    if constexpr (EARLY) mma(columns[g][b], w, into);
-                    else mma(Tl::across(v_tile, at_across + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, g % 2, b), w, into);
+                    const auto column = EARLY ? columns[EARLY ? g : 0][b] : Tl::across(v_tile, at_across + (p0 + p) * (32 / 4 * Tl::STRIDE), 0, g % 2, b);
+                    mma(column, w, into);
+                    if constexpr (REST) mma(column, rest, into);
                 }
             }
             total += sum;
