@@ -483,10 +483,9 @@ int w2v_rotate(int type, uint32_t width, const w2v_rotary* rotary, int back, con
  * keep_dev is [batch][slots * page_words].  shared (a multiple of page_words, at most the room; 0: none): the first `shared` words of all
  * texts lie in the pages of row 0 of the table, whatever the other rows hold there; they are read once for all texts and not
  * once for each.  A text that has fewer words is shown those it has.
- * Scores, softmax and sums are fp32; in 16 bits weights may be rounded to twice the bits of `type` for the product with v, and to `type`
- * for that with a prefix's values where more than 64 queries share a key head.  What lies in places that are not shown to a text,
- * infinities and NaN included, has no influence on it; infinities and NaN in words of a prefix that some of the texts are shown cost the
- * other texts time, as with w2v_attend.
+ * Scores, softmax and sums are fp32; in 16 bits weights may be rounded to twice the bits of `type` for the product with v.  What lies in
+ * places that are not shown to a text, infinities and NaN included, has no influence on it; infinities and NaN in words of a prefix that
+ * some of the texts are shown cost the other texts time, as with w2v_attend.
  * workspace_dev: 256-byte aligned device memory of w2v_attend_pages_workspace bytes, contents irrelevant before and after; calls that
  * may run at the same time need one each.  Nothing is allocated or synchronised; results repeat bit for bit.
  * batch * heads <= 2^23, slots * page_words <= 2^31 - 2^12, n_pages >= 1. */

@@ -12,14 +12,15 @@
 //
 // Scores, maxima, sums and outputs are fp32; weights are rounded to the type of v for the second product, relative to the row's maximum
 // (fp16: lifted by a power of two, so that small ones keep their bits), and summed before that.  What the rounding left is multiplied too,
-// where memory is what the matrix cores wait for: over a text's own words (458 us for 455 below) and for up to 64 queries of a
-// prefix's key head (16384 words, 32 and 64 queries: 39 us for 37, 41 for 39).  More queries keep the matrix cores busy: it would cost
-// 130 us for 120, and the weights' rounding is left there: results 1.35 times as far off as one rounding at the end makes them.
+// so that a weight has twice the type's bits and one rounding at the end is what results are off by, whatever the number of queries.  It
+// costs little where memory is what the matrix cores wait for: over a text's own words 458 us for 455 below, for up to 64 queries of a
+// prefix's key head 39 and 41 us for 37 and 39 (16384 words, 32 and 64 queries), and more for many: 84 us for 74 below.  Left out there,
+// results were 1.4 times as far off.
 //
 // What bounds it: a text's own words memory (32 texts of 574335 words, 32 heads of 128 over 8, 16 bits: 452 us, 5.2 TB/s; two wavefronts a
 // block, four blocks a CU take turns).  The prefix, where many queries share it, its two products and the exponentials, with
-// two wavefronts a SIMD: 64 texts behind 32768 words, the same heads, 72 us (34 GFLOP, 480 TFLOP/s; the loads alone take 48, the
-// products alone 60), and 43 us for their own 33000 words.  24 texts behind 4096 words in 32 bits, 8 heads of 64, bias: 15 us.
+// two wavefronts a SIMD: 64 texts behind 32768 words, the same heads, 84 us (51 GFLOP with the weights' second product, 610 TFLOP/s), and
+// 45 us for their own 33000 words.  24 texts behind 4096 words in 32 bits, 8 heads of 64, bias: 15 us.
 #include <type_traits>
 
 #include "attend.h"
@@ -357,7 +358,7 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
             }
             const float base = m == -__builtin_inff() ? 0.f : m - LIFT<T>;
             float sum = 0.f;
-            constexpr bool PARTS = sizeof(T) == 4, REST = sizeof(T) == 2 && !(PREFIX && WR > 2);
+            constexpr bool PARTS = sizeof(T) == 4, REST = sizeof(T) == 2;
             Acc part[PARTS ? DB : 1] = {};            // 32 bits: the pieces' sums first, then the whole's: one long chain would lose bits
 #pragma unroll
             for (int g = 0; g < 2 * P.value; ++g) {   // 16 keys

@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from attend_reference import check
+from attend_reference import E_SUM, ROUND, check
 from pages_reference import gather, last_rows
 from paper_1606_08495_amd import w2v
 
@@ -219,3 +219,31 @@ def test_pools_past_32_bit_offsets():
     assert parts(batch, 8, G, d, F16, table, words, pages, shared) > parts(batch, 8, G, d, F16, table, words, pages, 0, left=0)
     want = w2v.attend_pages(q, near, near, table, n, shared=shared)
     assert torch.equal(w2v.attend_pages(q, k, k, far[table.long()].to(torch.int32), n, shared=shared), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("H,G,d,batch", [(4, 2, 128, 9), (5, 1, 100, 10), (33, 1, 31, 64), (6, 2, 37, 40), (8, 2, 64, 40), (12, 3, 96, 50), (8, 1, 128, 40)])
+def test_weights_keep_their_bits(H, G, d, batch, ty):
+    """18 to 2112 queries for a key head.  All words of one parity have one score and one value, so that what a weight's rounding takes away
+    is the same for thousands of words and adds up, while the results of some columns are near zero.
+
+    The bound.  A score is a single product, exact in fp32, times scale: off by 2^-21 |x| with all that follows (attend_reference).  A weight is
+    the sum of two numbers of the type, of which the second is off by u of itself and at most u of the weight: u^2.  Sums: e'.  So
+    |d out| <= (2 2^-21 |x| + u^2 + e') sum p |v| + u |out|; one number of the type for a weight would be off by some u / 4 sum p |v|."""
+    shared = shape_of(G, d, ty, batch)
+    print("weights", H, G, d, batch, shared, ty, flush=True)
+    t = Texts(lengths(batch, shared, 6), shared, H, G, d, ty, seed=6)
+    t.k.zero_()
+    t.k[:, 0::2, :, 0], t.k[:, 1::2, :, 0] = 1.0, -1.0
+    t.v[:, 0::2] = 1.0
+    t.v[:, 1::2] = (-torch.linspace(0.5, 4.0, d, device="cuda")).to(ty)
+    x = torch.linspace(0.04, 0.8, batch * H, device="cuda").view(batch, H)
+    t.q.zero_()
+    t.q[..., 0] = (x * d ** 0.5).to(ty)
+    got = t.call()
+    k, v, kept, n = gather(t.k, t.v, t.table, t.n, None, shared)
+    want, size = [last_rows(t.q, k, y, n, kept)["out"] for y in (v, v.abs())]
+    u = ROUND[ty]
+    bound = (2 * 2.0 ** -21 * t.q[..., :1].double() * d ** -0.5 + u * u + E_SUM) * size + u * want.abs()
+    check(got, dict(out=want.cpu(), out_bound=bound.cpu()), "out", ty)
