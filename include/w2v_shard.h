@@ -484,8 +484,8 @@ int w2v_rotate(int type, uint32_t width, const w2v_rotary* rotary, int back, con
  * texts lie in the pages of row 0 of the table, whatever the other rows hold there; they are read once for all texts and not
  * once for each.  A text that has fewer words is shown those it has.
  * Scores, softmax and sums are fp32; in 16 bits weights may be rounded to twice the bits of `type` for the product with v.  What lies in
- * places that are not shown to a text, infinities and NaN included, has no influence on it; infinities and NaN in words of a prefix that
- * some of the texts are shown cost the other texts time, as with w2v_attend.
+ * places that are not shown to a text, infinities and NaN included, has no influence on it; infinities and NaN in a prefix's words, up to
+ * the last one that the longest text has, cost the texts time that are not shown them (by keep, window or length), as with w2v_attend.
  * workspace_dev: 256-byte aligned device memory of w2v_attend_pages_workspace bytes, contents irrelevant before and after; calls that
  * may run at the same time need one each.  Nothing is allocated or synchronised; results repeat bit for bit.
  * batch * heads <= 2^23, slots * page_words <= 2^31 - 2^12, n_pages >= 1. */

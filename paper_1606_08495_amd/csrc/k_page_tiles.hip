@@ -268,9 +268,26 @@ __device__ __forceinline__ void tile_block(const StepArgs& a, uint32_t block) {
     }
     if (PREFIX) {
         hi_least = lanes_least(own.hi);
-        if (!bounded) hi_most = ~lanes_least(~own.hi);
+        if (!bounded) {
+            hi_most = ~lanes_least(~own.hi);
+            if (lane == 0) bounds[wr] = hi_most;
+        }
     }
     __syncthreads();
+    if (PREFIX && !bounded) {                         // where all texts end within the prefix, so does the block: nothing is known of later places
+        uint32_t end = 0;
+#pragma unroll
+        for (int w = 0; w < WR; ++w) end = bounds[w] > end ? bounds[w] : end;
+        end = __builtin_amdgcn_readfirstlane(end);
+        if (end < to) {
+            to = end > from ? end : from;
+            if (threadIdx.x < 2 * KEYS && from + threadIdx.x >= to) {
+                k_next = v_next = NOWHERE;
+                tell(threadIdx.x / KEYS, threadIdx.x % KEYS);
+            }
+            __syncthreads();
+        }
+    }
     if (from < to) store(tiles[0], fetch(0));
     __syncthreads();
     for (uint32_t n0 = from; n0 < to; n0 += KEYS) {

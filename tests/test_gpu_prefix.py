@@ -247,3 +247,23 @@ def test_weights_keep_their_bits(H, G, d, batch, ty):
     u = ROUND[ty]
     bound = (2 * 2.0 ** -21 * t.q[..., :1].double() * d ** -0.5 + u * u + E_SUM) * size + u * want.abs()
     check(got, dict(out=want.cpu(), out_bound=bound.cpu()), "out", ty)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("H,G,d,batch", [(6, 2, 64, 40), (4, 2, 128, 9), (5, 1, 100, 10), (8, 1, 60, 50)])
+def test_places_past_all_texts_are_not_seen(H, G, d, batch, ty):
+    """Texts that all end within the prefix: what its later places hold changes no bit (rows formed again word by word would)."""
+    shared = shape_of(G, d, ty, batch)
+    longest = shared // 2 // 64 * 64 + 5
+    t = Texts([longest - x % 3 - 64 * (x % 2) for x in range(batch)], shared, H, G, d, ty, seed=7)
+    end = t.table[0, longest // 64].long()
+    rest = t.table[0, longest // 64 + 1:shared // 64].long()
+    got = []
+    for hold in (0.0, float("nan"), float("inf")):
+        for x in (t.k, t.v):
+            x[end, longest % 64:] = hold
+            x[rest] = hold
+        got.append(t.call())
+    t.check(got[0])
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
