@@ -267,3 +267,95 @@ def test_places_past_all_texts_are_not_seen(H, G, d, batch, ty):
         got.append(t.call())
     t.check(got[0])
     assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+# ---- windows of which most lies in the prefix, for few and for many queries --------------------------------
+
+def window_of(G, d, ty, batch):
+    """Words of a window that the prefix's own blocks serve: 384 MB more to read if every text read them."""
+    return -(-3 * MORE // ((batch - 1) * G * d * 2 * torch.finfo(ty).bits // 8))
+
+
+def call_with_own_blocks(t, left=None, sinks=0, **see):
+    """The call, once it has been seen to split into other parts than one without a prefix does."""
+    size = []
+    for shared in (0, t.shared):
+        spec = w2v._spec(t.q, t.k.shape[2], left, 0, sinks, False, None, None, None)
+        table = w2v.PageTable(4096, t.table.shape[1], t.table.shape[1], t.words, t.k.shape[0])
+        size.append(w2v.lib().w2v_attend_pages_workspace(ctypes.byref(spec), len(t.n), ctypes.byref(table), shared))
+    assert size[0] != size[1], "no blocks of its own"
+    return w2v.attend_pages(t.q, t.k, t.v, t.table, i32(t.n), shared=t.shared, left=left, sinks=sinks, **see)
+
+
+FEW_AND_MANY = [(1, 1, 31, 30), (4, 2, 128, 9), (8, 4, 96, 20), (2, 2, 64, 60), (6, 2, 127, 40), (3, 1, 90, 50), (5, 1, 32, 33)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("H,G,d,batch", FEW_AND_MANY)
+def test_windows_masks_and_bias_by_queries(H, G, d, batch, ty):
+    """18 to 165 queries for a key head, each width of tile, windows that begin in the prefix, first words before them, a bias, dropped words
+    and numbers that are no page."""
+    left = window_of(G, d, ty, batch)
+    shared = (left + 1500) // 64 * 64
+    print("prefix", H, G, d, batch, shared, left, ty, flush=True)
+    n = lengths(batch, shared, 8)
+    n[0] = shared + 1                                        # one word of its own
+    t = Texts(n, shared, H, G, d, ty, words=16, seed=8)
+    plain = [dict(), dict(left=left), dict(left=left, sinks=64), dict(left=left + 700, sinks=3, skip_self=True)]
+    for see in plain:
+        t.check(call_with_own_blocks(t, **see), **see)
+    t.table[0, 3::7] = t.k.shape[0]                           # numbers that are no page, in the prefix and behind it
+    t.table[5::2, -3] = -1
+    more = dict(bias=torch.randn(H, 32, device="cuda"), buckets=w2v.relative_buckets(32, 128),
+                keep=(torch.rand(batch, t.table.shape[1] * 16, device="cuda") > 0.6).to(torch.uint8))
+    for see in plain:
+        t.check(call_with_own_blocks(t, **see, **more), **see, **more)
+    del more["keep"]
+    t.check(call_with_own_blocks(t, **plain[2], **more), **plain[2], **more)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("H,G,d,batch", [(2, 2, 40, 20), (4, 2, 128, 12), (4, 2, 40, 24), (6, 2, 40, 60)])
+def test_infinities_that_some_windows_see(H, G, d, batch, ty):
+    """20 to 180 queries for a key head: texts whose window shows an infinite value or a key that is not a number have it, the others do not."""
+    left = window_of(G, d, ty, batch)
+    shared, group = (left + 700) // 64 * 64 + 64, H // G
+    n = [shared + 10 * b for b in range(batch)]
+    t = Texts(n, shared, H, G, d, ty, seed=9)
+    want = call_with_own_blocks(t, left=left)
+    far, near = n[batch // 3] - 1 - left, n[batch // 2] - 1 - left      # the first word that these texts are shown
+    t.v[int(t.table[0, near // 64]), near % 64, 1, 3] = float("inf")
+    t.k[int(t.table[0, far // 64]), far % 64, 0, 5] = float("nan")
+    got = call_with_own_blocks(t, left=left)
+    sees = torch.zeros(batch, H, d, dtype=torch.bool, device="cuda")
+    sees[:batch // 2 + 1, group:, 3] = True
+    sees[:batch // 3 + 1, :group] = True
+    assert torch.equal(torch.isfinite(got), ~sees)
+    assert torch.allclose(got[~sees].float(), want[~sees].float(), atol={F32: 1e-5, F16: 4e-3, BF16: 3e-2}[ty])
+    infinite, nan = got[:, group:, 3][sees[:, group:, 3]], got[:, :group][sees[:, :group]]
+    assert (infinite == float("inf")).all() and torch.isnan(nan).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ty", [F32, F16, BF16])
+@pytest.mark.parametrize("H,G,d,batch", [(2, 2, 64, 20), (4, 2, 100, 24), (3, 1, 128, 40)])
+def test_large_scores_and_masks_by_queries(H, G, d, batch, ty):
+    """As test_large_scores_and_masks_of_the_lowest_value, for 20, 48 and 120 queries a key head, and in a window."""
+    left = window_of(G, d, ty, batch)
+    shared = (left + 700) // 64 * 64
+    t = Texts([shared + x for x in range(batch)], shared, H, G, d, ty, seed=10)
+    t.q = (t.q.float() * 30).to(ty)
+    whole = t.table.clone()
+    whole[:, :shared // 64] = t.table[0, :shared // 64]
+    bmap = w2v.relative_buckets(32, 200)
+    for low in (-math.inf, torch.finfo(F32).min, -1e9):
+        bias = torch.randn(H, 32, device="cuda")
+        bias[:, 15] = low
+        bias[1] = low
+        for see in (dict(), dict(left=left, sinks=5)):
+            want = w2v.attend_pages(t.q, t.k, t.v, whole, i32(t.n), bias=bias, buckets=bmap, **see)
+            tol = {F32: 2e-3, F16: 4e-3, BF16: 3e-2}[ty]
+            got = call_with_own_blocks(t, bias=bias, buckets=bmap, **see)
+            assert torch.allclose(got.float(), want.float(), atol=tol, rtol=tol), (low, see)
