@@ -81,7 +81,7 @@ StepSplits step_splits(uint32_t batch, uint32_t kv_heads, uint32_t room, uint32_
 void launch_step(const StepArgs& a, uint32_t type, hipStream_t st);
 
 // Over pages.  What a call splits into, by sizes alone.
-uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t shared);
+uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t words);
 struct PageSplits { uint32_t begin, front; StepSplits own; };
 PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t width, uint32_t room, uint32_t shared,
                        uint32_t left, uint32_t sinks);

@@ -550,10 +550,10 @@ template <typename T> void tiles_any(const StepArgs& a, uint32_t type, bool pref
 
 }  // namespace
 
-// Blocks enough to fill the device twice over, of at least a tile each.
-uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t shared) {
+// Parts of a prefix of which a text is shown so many words: blocks enough to fill the device twice over, of at least a tile each.
+uint32_t prefix_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t words) {
     const uint32_t rows = batch * (heads / kv_heads), per_block = prefix_rows(type, rows);
-    const uint32_t blocks = (rows + per_block - 1) / per_block * kv_heads, most = (shared + KEYS - 1) / KEYS;
+    const uint32_t blocks = (rows + per_block - 1) / per_block * kv_heads, most = (words + KEYS - 1) / KEYS;
     const uint32_t want = blocks < 512 ? (512 + blocks - 1) / blocks : 1;
     return want < most ? want : most;
 }

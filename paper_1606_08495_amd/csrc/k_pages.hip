@@ -21,7 +21,11 @@ template <typename T> void pages_any(const StepArgs& a, uint32_t type, hipStream
 // A prefix is taken by blocks of its own where reading it once for each text would move this many bytes more: below, their launch and
 // the join cost more than reading it from the caches.  24 texts in 32 bits, 8 heads of 64: 92 MB more (1024 words) 22 us with
 // blocks of its own and 19 without, 368 MB 23 and 33; 8 texts in 16 bits, 8 key heads of 128: 112 MB 30 and 29, 448 MB 41 and 65.
-constexpr uint64_t PREFIX_BYTES = 128 << 20;
+// Of a window only so much is in the prefix as the texts have not moved on behind it, and texts of unequal length are shown different
+// words of it: windows that are shorter than the prefix have to be four times as large.  64 texts with up to 900 words behind 32768,
+// 16 bits, 8 key heads of 128: windows of 1040 words (256 MB) 63 us with blocks of the prefix's own and 41 without, 2080 (512 MB) 64 and
+// 62, 6241 82 and 175; 6 heads of 100 behind 16384: 887 words (128 MB) 49 and 27, 3550 (512 MB) 51 and 73.
+constexpr uint64_t PREFIX_BYTES = 128 << 20, PREFIX_BYTES_WINDOW = 512 << 20;
 
 }  // namespace
 
@@ -34,9 +38,11 @@ constexpr uint64_t PREFIX_BYTES = 128 << 20;
 PageSplits page_splits(uint32_t type, uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t width, uint32_t room, uint32_t shared,
                        uint32_t left, uint32_t sinks) {
     PageSplits p{};
-    if (batch > 1 && (uint64_t)(batch - 1) * shared * kv_heads * width * 2 * elem_bytes(type) >= PREFIX_BYTES) {
+    const bool windowed = (uint64_t)left + 1 + sinks < shared;
+    const uint32_t seen = windowed ? left + 1 + sinks : shared;      // words of the prefix that a text is shown at most
+    if (batch > 1 && (uint64_t)(batch - 1) * seen * kv_heads * width * 2 * elem_bytes(type) >= (windowed ? PREFIX_BYTES_WINDOW : PREFIX_BYTES)) {
         p.begin = shared;
-        p.front = prefix_splits(type, batch, heads, kv_heads, shared);
+        p.front = prefix_splits(type, batch, heads, kv_heads, seen);
     }
     const uint64_t rest = room > p.begin ? room - p.begin : 1, rows = (uint64_t)batch * kv_heads;
     const uint64_t shown = (uint64_t)left + 1 + sinks < rest ? (uint64_t)left + 1 + sinks : rest;

@@ -272,8 +272,8 @@ def test_places_past_all_texts_are_not_seen(H, G, d, batch, ty):
 # ---- windows of which most lies in the prefix, for few and for many queries --------------------------------
 
 def window_of(G, d, ty, batch):
-    """Words of a window that the prefix's own blocks serve: 384 MB more to read if every text read them."""
-    return -(-3 * MORE // ((batch - 1) * G * d * 2 * torch.finfo(ty).bits // 8))
+    """Words of a window that the prefix's own blocks serve: 512 MB more to read if every text read them."""
+    return -(-4 * MORE // ((batch - 1) * G * d * 2 * torch.finfo(ty).bits // 8))
 
 
 def call_with_own_blocks(t, left=None, sinks=0, **see):
@@ -359,3 +359,18 @@ def test_large_scores_and_masks_by_queries(H, G, d, batch, ty):
             tol = {F32: 2e-3, F16: 4e-3, BF16: 3e-2}[ty]
             got = call_with_own_blocks(t, bias=bias, buckets=bmap, **see)
             assert torch.allclose(got.float(), want.float(), atol=tol, rtol=tol), (low, see)
+
+
+@pytest.mark.parametrize("ty,H,G,d,batch,words,shared", [(2, 32, 8, 128, 64, 16, 32768), (0, 8, 8, 64, 24, 64, 32768), (1, 6, 6, 100, 64, 64, 16384)])
+def test_what_a_window_shows_of_a_prefix_counts(ty, H, G, d, batch, words, shared):
+    """A prefix has blocks of its own by what a text can be shown of it, not by its length: a call splits otherwise for it, or does not."""
+    table = w2v.PageTable(4096, shared // words + 64, shared // words + 64, words, 1 << 16)
+
+    def size(shared, left, sinks=0):
+        spec = w2v.AttendSpec(type=ty, heads=H, kv_heads=G, width=d, left=left, right=0, sinks=sinks, skip_self=0, scale=0.1)
+        return w2v.lib().w2v_attend_pages_workspace(ctypes.byref(spec), batch, ctypes.byref(table), shared)
+    for left in (0, 99, 800):
+        for sinks in (0, 64):
+            assert size(shared, left, sinks) == size(0, left, sinks)
+    for left in (shared // 2, shared - 2, shared - 1, shared, w2v.UNBOUNDED):
+        assert size(shared, left) != size(0, left)
