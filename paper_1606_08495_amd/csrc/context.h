@@ -91,7 +91,6 @@ void launch_prefix(const StepArgs& a, uint32_t type, hipStream_t st);
 void launch_own_tiles(const StepArgs& a, uint32_t type, hipStream_t st);      // (16 bits)
 
 // ---- positions that turn, and words on their way into pages ------------------------------------------
-struct Pages { void* p; uint64_t page, token, head; };
 struct TurnArray { Heads in; void* out; uint64_t out_token, out_head; uint32_t heads; };      // heads = 0: none
 struct TurnArgs {
     // rotate: x, y turned.  append: q, k turned, v as it is; k and v go into pages, out_token leading from place to place there
