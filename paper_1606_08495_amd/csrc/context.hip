@@ -277,7 +277,7 @@ extern "C" int w2v_attend_step(const w2v_attend_spec* spec, const w2v_heads* q, 
         if (workspace_bytes < need)
             return fail(W2V_ERR_ARG, "workspace of %zu bytes is too small: %zu are needed", workspace_bytes, need);
     }
-    StepArgs a;
+    StepArgs a{};
     a.q = heads_of(q); a.o = heads_out(out);
     a.k = Cache{k->p, k->text_stride, k->token_stride, k->head_stride};
     a.v = Cache{v->p, v->text_stride, v->token_stride, v->head_stride};
