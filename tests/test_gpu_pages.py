@@ -519,3 +519,12 @@ def test_refusals_of_the_binding():
     for bad in (dict(q=q), dict(positions=n), dict(q_out=q)):
         with pytest.raises(ValueError):
             w2v.pages_append(q[:, :1], q[:, :1], pool, pool, n, n, **bad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,G,ty", [(8, 1, F32), (16, 2, F32), (9, 1, F32), (8, 1, F16), (2, 2, BF16)])
+def test_the_widest_bias(H, G, ty):
+    """As many distances as there may be, for eight heads of 128 columns a block: more than 64 KB of LDS."""
+    print("pages", H, G, ty, flush=True)
+    run([300, 1500, 1, 0], 16, H, G, 128, ty, buckets=64, span=1023)
+    run([300, 400], 16, H, G, 128, ty, buckets=1024, span=1023)
