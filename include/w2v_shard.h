@@ -479,8 +479,9 @@ int w2v_rotate(int type, uint32_t width, const w2v_rotary* rotary, int back, con
  * another text's row lists too (a common prefix) is written for both.  Pools that overlap each other or an input, or lie among them with
  * other strides, are refused.
  *
- * w2v_attend_pages gives what w2v_attend_step does, over pages: spec, n_dev, q and out are as there (out may be q),
- * keep_dev is [batch][slots * page_words].  shared (a multiple of page_words, at most the room; 0: none): the first `shared` words of all
+ * w2v_attend_pages gives what w2v_attend_step does, over pages, for one word of each text a call (several new words of a text look
+ * back over its pages one after the other, n_dev counting up to each): spec, n_dev, q and out are as there (out may be q), keep_dev is
+ * [batch][slots * page_words].  shared (a multiple of page_words, at most the room; 0: none): the first `shared` words of all
  * texts lie in the pages of row 0 of the table, whatever the other rows hold there; they are read once for all texts and not
  * once for each.  A text that has fewer words is shown those it has.
  * Scores, softmax and sums are fp32; in 16 bits weights may be rounded to twice the bits of `type` for the product with v.  What lies in

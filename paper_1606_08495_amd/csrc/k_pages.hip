@@ -19,8 +19,9 @@ template <typename T> void pages_any(const StepArgs& a, uint32_t type, hipStream
 }
 
 // A prefix is taken by blocks of its own where reading it once for each text would move this many bytes more: below, their launch and
-// the join cost more than reading it from the caches.  24 texts in 32 bits, 8 heads of 64: 92 MB more (1024 words) 22 us with
-// blocks of its own and 19 without, 368 MB 23 and 33; 8 texts in 16 bits, 8 key heads of 128: 112 MB 30 and 29, 448 MB 41 and 65.
+// the join cost more than reading it from the caches.  24 texts with up to 900 words behind it in 32 bits, 8 heads of 64: 126 MB more
+// (1408 words) 23 us with blocks of its own and 23 without, 368 MB 27 and 38.  In 16 bits both are level at 250 MB: 64 texts, 32 heads of 128
+// over 8, 130 MB 54 and 47, 252 MB 56 and 57, 504 MB 63 and 77; 8 texts, 128 MB 39 and 30, 427 MB 42 and 63.
 // Of a window only so much is in the prefix as the texts have not moved on behind it, and texts of unequal length are shown different
 // words of it: windows that are shorter than the prefix have to be four times as large.  64 texts with up to 900 words behind 32768,
 // 16 bits, 8 key heads of 128: windows of 1040 words (256 MB) 63 us with blocks of the prefix's own and 41 without, 2080 (512 MB) 64 and
@@ -30,8 +31,8 @@ constexpr uint64_t PREFIX_BYTES = 128 << 20, PREFIX_BYTES_WINDOW = 512 << 20;
 }  // namespace
 
 // How many parts a text's own words are taken in.  The vector units' blocks have 512 words at least, or 1024 where there is a block for
-// every compute unit without a split (48 texts behind windows of 1028, 6 heads of 100: 29 us in one part, 31 to 35 in more), and are
-// enough to fill the device several times over.  The matrix cores' have 128 at least and fill it once, but of long texts, which may
+// every compute unit without a split (48 texts behind windows of 1028, 6 heads of 100: 33 us in one part, 33 and 4.5 for the join in two
+// or four), and are enough to fill the device several times over.  The matrix cores' have 128 at least and fill it once, but of long texts, which may
 // be of unequal length, 1024 (16 texts of up to 3000 words, 4 key heads of 96: 23 us in parts of 128 to 192, 32 of 512).
 // Up to 512 words are not split: the join's launch costs more (500 words: 14 us, 17 in parts).  Behind a prefix with blocks of its own, where
 // there is a join in any case, parts are shorter.

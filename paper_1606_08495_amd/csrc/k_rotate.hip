@@ -6,9 +6,9 @@
 // What bounds it is the rows' way through memory, once in and once out.  A block takes a few words: it finds their texts, positions
 // and places, fills a table of their sines and cosines in LDS once for all heads of queries and keys, and then walks over all rows
 // of those words, 16 bytes a thread, a thread's column fixed and some rows asked for before any is worked on.
-// Measured: 131333 words in texts of 10 to 40, 5 + 5 heads of 60, 32 bits: 123 us (5.1 TB/s; a large copy moves 4.8).  39955 words of 16 + 4
-// heads of 128, half of each turned, 16 bits, there and back: 167 us (4.9 TB/s).  26016 words of 40 prompts into pages, 32 query heads and 8
-// keys and values of 128, 16 bits: 124 us (5.2 TB/s).  One word: 5 us, of which the launch is most.
+// Measured: 131333 words in texts of 10 to 40, 5 + 5 heads of 60, 32 bits: 120 us (5.2 TB/s; a large copy moves 4.8).  39955 words of 16 + 4
+// heads of 128, half of each turned, 16 bits, there and back: 161 us (5.1 TB/s).  26016 words of 40 prompts into pages, 32 query heads and 8
+// keys and values of 128, 16 bits: 126 us (5.1 TB/s).  One word: 5 us, of which the launch is most.
 //
 // An angle is a whole number of 2^-64 turns times the position, modulo 2^64: exact, whatever the position.  Of its upper 32 bits (2^-32
 // of a turn is 1.5e-9) the nearest quarter turn is taken off as a whole number too, and what is left, at most an eighth of a turn,
